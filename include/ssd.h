@@ -325,6 +325,148 @@ SSD_API ssd_status ssd_conv1d_step(int32_t batch, int32_t ksize, int32_t io_dtyp
                            void *hip_stream);
 
 /*
+ * The norms on either side of a Mamba-2 block (Alg. 1 and 2 name the block's
+ * projections and residual stream around the core; section "Mapping SSD onto
+ * JAX primitives" keeps residual and norm arithmetic in fp32).
+ *
+ * ssd_norm_gated stands between the core's output y and the output projection.
+ * Each of `groups` equal ranges of a row's `width` values is normalised by itself:
+ *     norm_first = 0:  u = y * silu(z);  out = u * rsqrt(mean(u^2) + eps) * weight
+ *     norm_first = 1:  out = y * rsqrt(mean(y^2) + eps) * weight * silu(z)
+ *   y, out            (rows, width) io dtype, dense; out may be y
+ *   z                 (rows, width) io dtype, rows z_stride >= width elements apart
+ *                     (a slice of the input projection's output); must not
+ *                     overlap out, unless it is out with z_stride = width
+ *   weight            (width) fp32;  groups divides width;  eps >= 0
+ *
+ * ssd_norm_residual joins a block's output x to the residual stream and
+ * normalises the stream for the next block:
+ *     r = residual + scale * x;  residual_out = r;  out = r * rsqrt(mean(r^2) + eps) * weight
+ *   x, out            (rows, width) io dtype, dense; out may be x
+ *   residual          (rows, width) residual_dtype, or NULL = zeros (the first
+ *                     block's input);  residual_out may be residual
+ *   residual_dtype    SSD_F32, or io_dtype.  The norm takes r before it is
+ *                     rounded to residual_dtype.
+ * Arithmetic and sums are fp32, one rounding (RNE) per output.  Any number of
+ * rows and any width; y, x, out, residual* and weight are 16-byte aligned, z is
+ * aligned to its elements.
+ * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _HIP.
+ */
+SSD_API ssd_status ssd_norm_gated(int64_t rows, int32_t width, int32_t groups, int32_t io_dtype,
+                          const void *y, const void *z, int64_t z_stride,
+                          const float *weight, float eps, int32_t norm_first,
+                          void *out, void *hip_stream);
+SSD_API ssd_status ssd_norm_residual(int64_t rows, int32_t width, int32_t io_dtype, int32_t residual_dtype,
+                             const void *x, const void *residual, float scale,
+                             const float *weight, float eps, void *out,
+                             void *residual_out, void *hip_stream);
+
+/*
+ * Attention layers of a hybrid stack: some of its blocks keep every token's key
+ * and value where a Mamba-2 block keeps a state.  Keys and values live in pages
+ * that sequences take from a common pool as they grow:
+ *     k_cache, v_cache  (npages, nkvheads, page_size, headdim)  io dtype
+ *     page_table        (batch, max_pages) int32: token t of sequence b is in
+ *                       page page_table[b][t / page_size], at t % page_size
+ *     seq_lens          (batch) int32: tokens of the sequence, those of this call
+ *                       included (one array serves all three calls of a layer,
+ *                       and all layers)
+ *     cu_seqlens        (batch + 1) int32: the call's new tokens, packed: sequence
+ *                       b's are [cu_seqlens[b], cu_seqlens[b+1]), the last ones
+ *                       of its seq_lens[b]
+ * all of them device arrays, 4-byte aligned.  Query head h reads key head h / (nheads / nkvheads).
+ * headdim is a multiple of 8 up to 256, page_size a power of two up to 65536.
+ * A token sees the tokens of its sequence up to itself; with window > 0 only the
+ * last `window` of them.  io dtype is fp32 or bf16; scores, softmax and sums are
+ * fp32 (bf16 io: the probabilities are rounded to bf16 for their product with the
+ * values), results are rounded once.
+ *
+ * What the device arrays hold is not checked on the host, and cannot make a
+ * kernel leave its tensors: seq_lens is cut to [0, max_pages * page_size];
+ * boundaries to [0, tokens] (a sequence whose end precedes its beginning has no
+ * new tokens); tokens whose page table entry is not in [0, npages) are not
+ * appended and not seen.  A new token in front of its sequence's beginning
+ * (seq_lens[b] smaller than the number of its new tokens) is not appended and
+ * sees nothing.  A token that sees nothing gets y = 0.  What lies in a page
+ * behind a sequence's end is never used, whatever its value.
+ */
+typedef struct {
+  int32_t batch;     /* sequences */
+  int32_t tokens;    /* new tokens of the call, all sequences together (ssd_attn_step: ignored, one each) */
+  int32_t nheads;    /* query heads */
+  int32_t nkvheads;  /* key and value heads, divides nheads */
+  int32_t headdim;
+  int32_t npages;    /* pages in the caches */
+  int32_t page_size; /* tokens per page */
+  int32_t max_pages; /* entries in a row of the page table */
+  int32_t window;    /* 0 = no limit */
+  int32_t io_dtype;  /* ssd_dtype of q, k, v, the caches and y */
+} ssd_attn_shape;
+
+/*
+ * Appends the new tokens' keys and values to the cache and rotates queries and
+ * keys by their positions on the way.  Position p's rotation of head values
+ * (a, b) is (a cos - b sin, b cos + a sin), with rope_cos[p][i], rope_sin[p][i]
+ * for pair i < rotary / 2: values (i, i + rotary/2), or (2i, 2i + 1) if
+ * interleaved; values from `rotary` on are copied.
+ *   cu_seqlens        or NULL: one new token for every sequence (tokens = batch)
+ *   q                 (tokens, nheads, headdim), tokens q_stride elements apart;
+ *                     k, v (tokens, nkvheads, headdim) likewise: slices of one
+ *                     projection's output.  q (with q_out) may be NULL
+ *   q_out             (tokens, nheads, headdim) dense, rotated; must not overlap q, k, v
+ *   rope_cos, rope_sin  (rope_positions, rotary / 2) fp32, for every position
+ *                     that a row of the page table can hold (rope_positions >=
+ *                     max_pages * page_size); both NULL if rotary is 0
+ *   rotary            even, <= headdim
+ * q_out is left untouched for tokens outside every sequence and in front of its
+ * beginning.  All tensors are 16-byte aligned, strides a multiple of 16 bytes.
+ * k_cache and v_cache must not overlap anything else.
+ * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _HIP.
+ */
+typedef struct {
+  const float *cos, *sin;
+  int32_t rotary;
+  int32_t positions;
+  int32_t interleaved;
+} ssd_rope;
+SSD_API ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *rope, const int32_t *cu_seqlens,
+                           const int32_t *seq_lens, const int32_t *page_table,
+                           const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                           const void *v, int64_t v_stride, void *q_out,
+                           void *k_cache, void *v_cache, void *hip_stream);
+
+/*
+ * Attention of one new token of each sequence over its cache:
+ *     y[b][h] = sum_t softmax_t(scale * q[b][h] . K[t]) V[t]
+ *   q, y              (batch, nheads, headdim) dense; y must not be q
+ *   workspace         at least ssd_attn_step_workspace_bytes() bytes, 256-byte
+ *                     aligned; its size depends on the shape alone
+ * Work is dealt to the workgroups by the lengths as the device holds them, so a
+ * captured call follows seq_lens as they grow.
+ * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _WORKSPACE, _HIP.
+ */
+SSD_API size_t ssd_attn_step_workspace_bytes(const ssd_attn_shape *shape);
+SSD_API ssd_status ssd_attn_step(const ssd_attn_shape *shape, const int32_t *seq_lens, const int32_t *page_table,
+                         const void *q, const void *k_cache, const void *v_cache,
+                         float scale, void *y, void *workspace, size_t workspace_bytes,
+                         void *hip_stream);
+
+/*
+ * Causal attention of the packed new tokens (prompts, or pieces of prompts behind
+ * what is cached) over the cache, to which they have been appended.
+ *   q, y              (tokens, nheads, headdim) dense; y must not be q; y of
+ *                     tokens outside every sequence is left untouched
+ *   workspace         at least ssd_attn_prefill_workspace_bytes() bytes, 256-byte aligned
+ * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _WORKSPACE, _HIP.
+ */
+SSD_API size_t ssd_attn_prefill_workspace_bytes(const ssd_attn_shape *shape);
+SSD_API ssd_status ssd_attn_prefill(const ssd_attn_shape *shape, const int32_t *cu_seqlens,
+                            const int32_t *seq_lens, const int32_t *page_table,
+                            const void *q, const void *k_cache, const void *v_cache,
+                            float scale, void *y, void *workspace, size_t workspace_bytes,
+                            void *hip_stream);
+
+/*
  * Name of the kernel family ssd_prefill would use for this shape:
  * "mfma_bf16" (bf16 io: bf16 MFMA contractions over LDS-staged tiles, fp32
  * accumulation), "mfma_f32" (fp32 io, headdim a multiple of 32, dstate a multiple

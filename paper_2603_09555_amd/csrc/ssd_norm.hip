@@ -1,0 +1,195 @@
+// The norms on either side of a Mamba-2 block:
+//
+//   gated, gate first:   u = y silu(z),  out = u rsqrt(mean(u^2) + eps) w
+//   gated, norm first:   out = y rsqrt(mean(y^2) + eps) w silu(z)
+//   residual:            r = residual + scale x,  residual_out = r,  out = r rsqrt(mean(r^2) + eps) w
+//
+// A unit -- a row, or one group of a row -- is read once, kept in registers as fp32 while its squares are summed, and written
+// once.  A thread owns pieces of 8 neighbouring values (bf16: 16 bytes; fp32: 32).  Both are streams; with few rows they are a
+// chain of two memory latencies and a reduction, and the unit is spread over as many threads as it has pieces for.
+#include "ssd_block.hpp"
+
+namespace ssd {
+namespace {
+
+using namespace block;
+
+constexpr int kPiece = 8;
+
+enum Mode { kGateFirst = 0, kNormFirst = 1, kResidual = 2 };
+
+struct NormArgs {
+  const void *in;        // y or x
+  const void *side;      // z or residual (nullptr: zeros)
+  const float *weight;
+  void *out;
+  void *side_out;        // residual_out
+  int64_t units;
+  int64_t side_stride;   // of z, in elements
+  int width, n;          // values in a row, and in a unit
+  int groups;
+  float scale, eps, inv_n;
+};
+
+// What a piece becomes before the norm (v), and the factor it gets behind it (g; norm first only).
+template <int kMode>
+__device__ __forceinline__ void combine(float v[kPiece], float s[kPiece], float scale) {
+#pragma unroll
+  for (int i = 0; i < kPiece; ++i) {
+    if (kMode == kResidual) {
+      v[i] = fmaf(scale, v[i], s[i]);
+    } else {
+      s[i] = silu(s[i]);
+      if (kMode == kGateFirst) v[i] *= s[i];
+    }
+  }
+}
+
+// kThreads threads a unit, kHold pieces a thread in registers (0: units too wide for that are read a second time, from the
+// caches).  Units of one wave share a workgroup of four.
+template <typename Io, typename Side, int kMode, int kThreads, int kHold>
+__global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(const NormArgs a) {
+  constexpr int kBlock = kThreads < 256 ? 256 : kThreads, kUnits = kBlock / kThreads, kWaves = kThreads / 64;
+  const int t = threadIdx.x % kThreads;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kUnits + threadIdx.x / kThreads;
+  if (unit >= a.units) return;  // (a whole wave; workgroups of several waves a unit have one unit)
+  int64_t row = unit;
+  int first = 0;
+  if (a.groups > 1) {
+    row = static_cast<uint32_t>(unit) / static_cast<uint32_t>(a.groups);
+    first = static_cast<int>(unit - row * a.groups) * a.n;
+  }
+  const typename Io::type *in = static_cast<const typename Io::type *>(a.in) + row * a.width + first;
+  typename Io::type *out = static_cast<typename Io::type *>(a.out) + row * a.width + first;
+  const typename Side::type *side = a.side == nullptr ? nullptr : static_cast<const typename Side::type *>(a.side) + row * a.side_stride + first;
+  typename Side::type *side_out = kMode == kResidual ? static_cast<typename Side::type *>(a.side_out) + row * a.width + first : nullptr;
+  const float *w = a.weight + first;
+
+  const int pieces = (a.n + kPiece - 1) / kPiece;
+  constexpr int kKeep = kHold > 0 ? kHold : 1;
+  float v[kKeep][kPiece], g[kMode == kNormFirst ? kKeep : 1][kPiece];
+  float sum = 0.f;
+  auto fetch = [&](int p, float x[kPiece], float s[kPiece]) {
+    const int at = p * kPiece, left = a.n - at;
+    Io::load(in + at, left, x);
+    if (side != nullptr) {
+      Side::load(side + at, left, s);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) s[i] = 0.f;
+    }
+  };
+  if (kHold > 0) {
+    float s[kKeep][kPiece];
+#pragma unroll
+    for (int k = 0; k < kKeep; ++k)
+      if (t + k * kThreads < pieces) fetch(t + k * kThreads, v[k], s[k]);
+#pragma unroll
+    for (int k = 0; k < kKeep; ++k)
+      if (t + k * kThreads < pieces) {
+        combine<kMode>(v[k], s[k], a.scale);
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) {
+          sum = fmaf(v[k][i], v[k][i], sum);
+          if (kMode == kNormFirst) g[k][i] = s[k][i];
+        }
+      }
+  } else {
+    for (int p = t; p < pieces; p += kThreads) {
+      float s[kPiece];
+      fetch(p, v[0], s);
+      combine<kMode>(v[0], s, a.scale);
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) sum = fmaf(v[0][i], v[0][i], sum);
+    }
+  }
+  sum = wave_sum(sum);
+  if (kWaves > 1) {
+    __shared__ float part[kWaves];
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = sum;
+    __syncthreads();
+    sum = part[0];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) sum += part[i];
+  }
+  const float r = 1.f / sqrtf(fmaf(sum, a.inv_n, a.eps));
+  auto finish = [&](int p, const float x[kPiece], const float *gate) {
+    const int at = p * kPiece, left = a.n - at;
+    float wv[kPiece], o[kPiece];
+    F32::load(w + at, left, wv);
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) o[i] = x[i] * r * wv[i] * (kMode == kNormFirst ? gate[i] : 1.f);
+    Io::store(out + at, left, o);
+    if (kMode == kResidual) Side::store(side_out + at, left, x);
+  };
+  if (kHold > 0) {
+#pragma unroll
+    for (int k = 0; k < kKeep; ++k)
+      if (t + k * kThreads < pieces) finish(t + k * kThreads, v[k], g[kMode == kNormFirst ? k : 0]);
+  } else {
+    // (a thread reads again what it read before, and writes there only: outputs that are inputs are no hazard)
+    for (int p = t; p < pieces; p += kThreads) {
+      float s[kPiece];
+      fetch(p, v[0], s);
+      combine<kMode>(v[0], s, a.scale);
+      finish(p, v[0], s);
+    }
+  }
+}
+
+template <typename Io, typename Side, int kMode>
+hipError_t launch_mode(const NormArgs &a, hipStream_t stream) {
+  const int pieces = (a.n + kPiece - 1) / kPiece;
+  const dim3 one(static_cast<unsigned>(a.units)), four(static_cast<unsigned>((a.units + 3) / 4));
+  if (pieces <= 64)
+    hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, 64, 1>), four, dim3(256), 0, stream, a);
+  else if (pieces <= 256)
+    hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, 256, 1>), one, dim3(256), 0, stream, a);
+  else if (pieces <= 1024)
+    hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, 256, 4>), one, dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, 1024, 0>), one, dim3(1024), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm_gated(int64_t rows, int width, int groups, bool bf16, const void *y, const void *z, int64_t z_stride,
+                             const float *weight, float eps, bool norm_first, void *out, hipStream_t stream) {
+  NormArgs a = {};
+  a.in = y;
+  a.side = z;
+  a.weight = weight;
+  a.out = out;
+  a.units = rows * groups;
+  a.side_stride = z_stride;
+  a.width = width;
+  a.n = width / groups;
+  a.groups = groups;
+  a.eps = eps;
+  a.inv_n = 1.f / static_cast<float>(a.n);
+  if (bf16) return norm_first ? launch_mode<Bf16, Bf16, kNormFirst>(a, stream) : launch_mode<Bf16, Bf16, kGateFirst>(a, stream);
+  return norm_first ? launch_mode<F32, F32, kNormFirst>(a, stream) : launch_mode<F32, F32, kGateFirst>(a, stream);
+}
+
+hipError_t launch_norm_residual(int64_t rows, int width, bool bf16, bool stream_bf16, const void *x, const void *residual,
+                                float scale, const float *weight, float eps, void *out, void *residual_out, hipStream_t stream) {
+  NormArgs a = {};
+  a.in = x;
+  a.side = residual;
+  a.weight = weight;
+  a.out = out;
+  a.side_out = residual_out;
+  a.units = rows;
+  a.side_stride = width;
+  a.width = width;
+  a.n = width;
+  a.groups = 1;
+  a.scale = scale;
+  a.eps = eps;
+  a.inv_n = 1.f / static_cast<float>(width);
+  if (!bf16) return launch_mode<F32, F32, kResidual>(a, stream);
+  return stream_bf16 ? launch_mode<Bf16, Bf16, kResidual>(a, stream) : launch_mode<Bf16, F32, kResidual>(a, stream);
+}
+
+}  // namespace ssd

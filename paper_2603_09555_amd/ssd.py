@@ -24,6 +24,8 @@ EXPORTS = ["ssd_prefill_workspace_bytes", "ssd_prefill", "ssd_prefill_static", "
            "ssd_decode_steps_layers", "ssd_prefill_varlen_workspace_bytes", "ssd_prefill_varlen",
            "ssd_conv1d_prefill", "ssd_conv1d_step", "ssd_prefill_dt", "ssd_prefill_varlen_dt",
            "ssd_decode_step_layers_dt", "ssd_decode_steps_layers_dt",
+           "ssd_norm_gated", "ssd_norm_residual", "ssd_attn_append", "ssd_attn_step", "ssd_attn_step_workspace_bytes",
+           "ssd_attn_prefill", "ssd_attn_prefill_workspace_bytes",
            "ssd_prefill_path", "ssd_status_string", "ssd_version",
            "ssd_testing_set_knob", "ssd_testing_reset_knobs", "ssd_testing_prefill_plan", "ssd_testing_varlen_plan",
            "ssd_testing_prefill_chunks", "ssd_testing_prefill_pair_plan"]
@@ -32,6 +34,16 @@ EXPORTS = ["ssd_prefill_workspace_bytes", "ssd_prefill", "ssd_prefill_static", "
 class ssd_shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("batch", "seqlen", "nheads", "headdim", "dstate", "ngroups", "chunk", "io_dtype")]
+
+
+class ssd_attn_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("batch", "tokens", "nheads", "nkvheads", "headdim", "npages", "page_size", "max_pages", "window", "io_dtype")]
+
+
+class ssd_rope(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("rotary", ctypes.c_int32), ("positions", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
 
 
 class SSDError(RuntimeError):
@@ -94,6 +106,20 @@ _lib.ssd_decode_step_layers_dt.restype = ctypes.c_int
 _lib.ssd_decode_step_layers_dt.argtypes = [ctypes.c_int32, _sp, ctypes.POINTER(ssd_dt_transform)] + [_vp] * 9
 _lib.ssd_decode_steps_layers_dt.restype = ctypes.c_int
 _lib.ssd_decode_steps_layers_dt.argtypes = [ctypes.c_int32, ctypes.c_int32, _sp, ctypes.POINTER(ssd_dt_transform)] + [_vp] * 9
+_i64, _f32, _ap = ctypes.c_int64, ctypes.c_float, ctypes.POINTER(ssd_attn_shape)
+_lib.ssd_norm_gated.restype = ctypes.c_int
+_lib.ssd_norm_gated.argtypes = [_i64, _i32, _i32, _i32, _vp, _vp, _i64, _vp, _f32, _i32, _vp, _vp]
+_lib.ssd_norm_residual.restype = ctypes.c_int
+_lib.ssd_norm_residual.argtypes = [_i64, _i32, _i32, _i32, _vp, _vp, _f32, _vp, _f32, _vp, _vp, _vp]
+_lib.ssd_attn_append.restype = ctypes.c_int
+_lib.ssd_attn_append.argtypes = [_ap, ctypes.POINTER(ssd_rope), _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp]
+for _name in ("ssd_attn_step_workspace_bytes", "ssd_attn_prefill_workspace_bytes"):
+    getattr(_lib, _name).restype = _sz
+    getattr(_lib, _name).argtypes = [_ap]
+_lib.ssd_attn_step.restype = ctypes.c_int
+_lib.ssd_attn_step.argtypes = [_ap] + [_vp] * 5 + [_f32, _vp, _vp, _sz, _vp]
+_lib.ssd_attn_prefill.restype = ctypes.c_int
+_lib.ssd_attn_prefill.argtypes = [_ap] + [_vp] * 6 + [_f32, _vp, _vp, _sz, _vp]
 _lib.ssd_prefill_path.restype = ctypes.c_char_p
 _lib.ssd_prefill_path.argtypes = [_sp]
 _lib.ssd_status_string.restype = ctypes.c_char_p
@@ -454,6 +480,157 @@ def ssd_conv1d_step(conv_state, u, weight, bias=None, split=None, activation="si
     if st != SSD_OK:
         raise SSDError(st, "ssd_conv1d_step")
     return [o for o in outs if o is not None]
+
+
+def ssd_norm_gated(y, z, weight, eps=1e-5, groups=1, norm_first=False, out=None):
+    """``ssd_norm_gated``: ``y (rows,width)`` and its gate ``z (rows,width)`` in fp32 or bf16, ``weight (width)`` fp32.  ``z`` may
+    be a slice of wider rows.  Each of ``groups`` ranges of a row is normalised by itself, ``y * silu(z)`` or, with
+    ``norm_first``, ``y``, which is gated afterwards.  Returns ``out (rows,width)``, which may be ``y``."""
+    rows, width = y.shape
+    if z.shape != y.shape or z.dtype != y.dtype or weight.shape != (width,) or weight.dtype != torch.float32:
+        raise ValueError("z must be like y, and weight fp32 of the rows' width")
+    if not z.is_cuda or (width > 1 and z.stride(1) != 1) or (rows > 1 and z.stride(0) < width):
+        raise ValueError("z must be a device tensor of dense rows")
+    _check_output(out, y.dtype, y.numel())
+    if out is None:
+        out = torch.empty_like(y)
+    _check_dev(y, weight, out)
+    st = _lib.ssd_norm_gated(rows, width, groups, _IO_DTYPES.get(y.dtype, -1), _ptr(y), _ptr(z), z.stride(0) if rows > 1 else width,
+                             _ptr(weight), eps, int(bool(norm_first)), _ptr(out), _stream_ptr())
+    if st != SSD_OK:
+        raise SSDError(st, "ssd_norm_gated")
+    return out
+
+
+def ssd_norm_residual(residual, x, weight, scale=1.0, eps=1e-5, out=None, residual_out=None):
+    """``ssd_norm_residual``: ``residual + scale * x`` and its norm times ``weight (width)`` fp32.  ``x (rows,width)`` in fp32 or
+    bf16; ``residual`` of the same shape in fp32 or the type of ``x``, or None for zeros (``residual_out`` is then fp32 unless
+    given).  Returns ``(out, residual_out)``; ``residual_out`` may be ``residual``, ``out`` may be ``x``."""
+    rows, width = x.shape
+    if weight.shape != (width,) or weight.dtype != torch.float32 or (residual is not None and residual.shape != x.shape):
+        raise ValueError("residual must have the shape of x, and weight must be fp32 of the rows' width")
+    stream = residual.dtype if residual is not None else residual_out.dtype if residual_out is not None else torch.float32
+    _check_output(out, x.dtype, x.numel())
+    _check_output(residual_out, stream, x.numel())
+    if out is None:
+        out = torch.empty_like(x)
+    if residual_out is None:
+        residual_out = torch.empty(x.shape, dtype=stream, device=x.device)
+    _check_dev(x, residual, weight, out, residual_out)
+    st = _lib.ssd_norm_residual(rows, width, _IO_DTYPES.get(x.dtype, -1), _IO_DTYPES.get(stream, -1), _ptr(x), _ptr(residual), scale,
+                                _ptr(weight), eps, _ptr(out), _ptr(residual_out), _stream_ptr())
+    if st != SSD_OK:
+        raise SSDError(st, "ssd_norm_residual")
+    return out, residual_out
+
+
+def make_attn_shape(batch, tokens, nheads, k_cache, page_table, window=0) -> ssd_attn_shape:
+    """The ``ssd_attn_shape`` of a call on ``k_cache (npages,nkvheads,page_size,headdim)`` and ``page_table (batch,max_pages)``."""
+    npages, nkv, page, headdim = k_cache.shape
+    return ssd_attn_shape(batch, tokens, nheads, nkv, headdim, npages, page, page_table.shape[1], window, _IO_DTYPES.get(k_cache.dtype, -1))
+
+
+def attn_step_workspace_bytes(shape: ssd_attn_shape) -> int:
+    return int(_lib.ssd_attn_step_workspace_bytes(ctypes.byref(shape)))
+
+
+def attn_prefill_workspace_bytes(shape: ssd_attn_shape) -> int:
+    return int(_lib.ssd_attn_prefill_workspace_bytes(ctypes.byref(shape)))
+
+
+def _check_cache(io, k_cache, v_cache, page_table, seq_lens, cu_seqlens, headdim):
+    if k_cache.dtype != io or v_cache.dtype != io:
+        raise ValueError("queries, keys, values and the caches must share one dtype")
+    if any(t is not None and t.dtype != torch.int32 for t in (page_table, seq_lens, cu_seqlens)):
+        raise ValueError("page_table, seq_lens and cu_seqlens must be int32")
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape or k_cache.shape[3] != headdim or page_table.dim() != 2 \
+            or seq_lens.shape != (page_table.shape[0],) or (cu_seqlens is not None and cu_seqlens.shape != (page_table.shape[0] + 1,)):
+        raise ValueError("inconsistent tensor shapes")
+    _check_dev(k_cache, v_cache, page_table, seq_lens, cu_seqlens)
+
+
+def _token_stride(t, heads, headdim):
+    """Elements between the tokens of ``t (tokens,heads,headdim)``, whose heads are dense."""
+    if not t.is_cuda or t.stride(2) != 1 or (heads > 1 and t.stride(1) != headdim):
+        raise ValueError("a token's heads must be dense on the device")
+    return t.stride(0) if t.shape[0] > 1 else heads * headdim
+
+
+def ssd_attn_append(q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens=None, rope=None, interleaved=False, q_out=None):
+    """``ssd_attn_append``: ``k, v (tokens,nkvheads,headdim)`` go to the caches ``(npages,nkvheads,page_size,headdim)``, rotated
+    as ``q (tokens,nheads,headdim)`` (or None) is on its way to ``q_out``.  ``rope = (cos, sin)``, each ``(positions,rotary/2)``
+    fp32 with a row for every position that ``page_table (batch,max_pages)`` can hold, or None.  ``seq_lens (batch)`` counts the new
+    tokens too; without ``cu_seqlens (batch+1)`` every sequence has one.  ``q``, ``k`` and ``v`` may be slices of one projection's
+    output.  Returns ``q_out``, or None without ``q``."""
+    tokens, nkv, D = k.shape
+    if v.shape != k.shape or v.dtype != k.dtype or (q is not None and (q.dtype != k.dtype or q.dim() != 3 or q.shape[0] != tokens or q.shape[2] != D)):
+        raise ValueError("q, k and v must share one dtype, and agree in tokens and headdim")
+    _check_cache(k.dtype, k_cache, v_cache, page_table, seq_lens, cu_seqlens, D)
+    if k_cache.shape[1] != nkv or (cu_seqlens is None and tokens != page_table.shape[0]):
+        raise ValueError("inconsistent tensor shapes")
+    xr = ssd_rope(None, None, 0, 0, int(bool(interleaved)))
+    if rope is not None:
+        cos, sin = rope
+        if cos.dim() != 2 or sin.shape != cos.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32:
+            raise ValueError("rope must be two fp32 tensors (positions, rotary / 2)")
+        _check_dev(cos, sin)
+        xr = ssd_rope(_ptr(cos), _ptr(sin), 2 * cos.shape[1], cos.shape[0], int(bool(interleaved)))
+    heads, q_stride = nkv, 0
+    if q is not None:
+        heads = q.shape[1]
+        q_stride = _token_stride(q, heads, D)
+        _check_output(q_out, q.dtype, q.numel())
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _check_dev(q_out)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    shape = make_attn_shape(page_table.shape[0], tokens, heads, k_cache, page_table)
+    st = _lib.ssd_attn_append(ctypes.byref(shape), ctypes.byref(xr), _ptr(cu_seqlens), _ptr(seq_lens), _ptr(page_table), _ptr(q), q_stride,
+                              _ptr(k), _token_stride(k, nkv, D), _ptr(v), _token_stride(v, nkv, D), _ptr(q_out), _ptr(k_cache),
+                              _ptr(v_cache), _stream_ptr())
+    if st != SSD_OK:
+        raise SSDError(st, "ssd_attn_append")
+    return q_out
+
+
+def _attn(where, q, k_cache, v_cache, page_table, seq_lens, cu_seqlens, scale, window, y, workspace):
+    tokens, heads, D = q.shape
+    _check_cache(q.dtype, k_cache, v_cache, page_table, seq_lens, cu_seqlens, D)
+    if cu_seqlens is None and tokens != page_table.shape[0]:
+        raise ValueError("inconsistent tensor shapes")
+    _check_output(y, q.dtype, q.numel())
+    if y is None:
+        y = torch.empty_like(q)
+    shape = make_attn_shape(page_table.shape[0], tokens, heads, k_cache, page_table, window)
+    need = (attn_step_workspace_bytes if cu_seqlens is None else attn_prefill_workspace_bytes)(shape)
+    if workspace is None:
+        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=q.device)
+    _check_dev(q, y, workspace)
+    scale = D ** -0.5 if scale is None else scale
+    tail = (_ptr(seq_lens), _ptr(page_table), _ptr(q), _ptr(k_cache), _ptr(v_cache), scale, _ptr(y), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream_ptr())
+    st = _lib.ssd_attn_step(ctypes.byref(shape), *tail) if cu_seqlens is None else \
+        _lib.ssd_attn_prefill(ctypes.byref(shape), _ptr(cu_seqlens), *tail)
+    if st != SSD_OK:
+        raise SSDError(st, where)
+    return y
+
+
+def ssd_attn_step(q, k_cache, v_cache, page_table, seq_lens, scale=None, window=0, y=None, workspace=None):
+    """``ssd_attn_step``: attention of one new token of each sequence, ``q (batch,nheads,headdim)``, over its ``seq_lens (batch)``
+    tokens in the caches ``(npages,nkvheads,page_size,headdim)``, the last ``window`` of them if that is not 0.  ``scale`` is
+    ``headdim ** -0.5`` unless given.  Returns ``y`` like ``q``."""
+    return _attn("ssd_attn_step", q, k_cache, v_cache, page_table, seq_lens, None, scale, window, y, workspace)
+
+
+def ssd_attn_prefill(q, k_cache, v_cache, page_table, seq_lens, cu_seqlens, scale=None, window=0, y=None, workspace=None):
+    """``ssd_attn_prefill``: causal attention of packed new tokens ``q (tokens,nheads,headdim)``, sequence b's being
+    ``cu_seqlens[b]`` to ``cu_seqlens[b+1]`` and the last of its ``seq_lens[b]``, over the caches they were appended to.
+    Otherwise as ``ssd_attn_step``."""
+    if cu_seqlens is None:
+        raise ValueError("ssd_attn_prefill needs cu_seqlens")
+    return _attn("ssd_attn_prefill", q, k_cache, v_cache, page_table, seq_lens, cu_seqlens, scale, window, y, workspace)
 
 
 KNOBS = {"force_generic": 0, "seg_chunks": 1, "seg_blocks": 2, "seg_parts": 3, "y_stream": 4, "decode_stream": 5,
