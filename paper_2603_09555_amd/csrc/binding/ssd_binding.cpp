@@ -14,6 +14,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 
+#include <cmath>
 #include <cstdint>
 
 #include "ssd.h"
@@ -35,6 +36,17 @@ struct Api {
   decltype(&ssd_conv1d_prefill) conv_prefill;
   decltype(&ssd_conv1d_step) conv_step;
 } api;
+
+// The operators of a hybrid stack's other layers, handed over by a call of their own.
+struct BlockApi {
+  decltype(&ssd_norm_gated) norm_gated;
+  decltype(&ssd_norm_residual) norm_residual;
+  decltype(&ssd_attn_append) attn_append;
+  decltype(&ssd_attn_step_workspace_bytes) attn_step_workspace_bytes;
+  decltype(&ssd_attn_step) attn_step;
+  decltype(&ssd_attn_prefill_workspace_bytes) attn_prefill_workspace_bytes;
+  decltype(&ssd_attn_prefill) attn_prefill;
+} block_api;
 
 // An argument: a plain dense device tensor, or None.
 struct Arg {
@@ -335,14 +347,226 @@ PyObject *conv1d(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// init(addresses): the functions of the C ABI in the order of Api
+// a device tensor of `dims` dimensions whose last one is dense
+Arg rows_of(PyObject *o, int64_t dims) {
+  Arg a;
+  if (THPVariable_CheckExact(o)) {
+    a.t = &THPVariable_Unpack(o);
+    a.ok = a.t->is_cuda() && a.t->layout() == at::kStrided && a.t->dim() == dims && a.t->stride(dims - 1) == 1;
+  }
+  return a;
+}
+bool number_of(PyObject *o, float *out) {
+  if (!PyFloat_CheckExact(o)) return false;
+  *out = static_cast<float>(PyFloat_AS_DOUBLE(o));
+  return true;
+}
+bool int_of(PyObject *o, int32_t *out) {
+  if (!PyLong_CheckExact(o)) return false;
+  int over = 0;
+  const long long v = PyLong_AsLongLongAndOverflow(o, &over);
+  if (over || v < INT32_MIN || v > INT32_MAX) return false;
+  *out = static_cast<int32_t>(v);
+  return true;
+}
+
+// (y, z, weight, eps, groups, norm_first, out)
+PyObject *norm_gated(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  SSD_ARGS(7);
+  const Arg y = tensor(a[0]), z = rows_of(a[1], 2), weight = tensor(a[2]);
+  float eps;
+  int32_t groups;
+  const int first = a[5] == Py_True ? 1 : a[5] == Py_False ? 0 : -1;
+  if (!y.ok || !z.ok || !weight.ok || first < 0 || !number_of(a[3], &eps) || !int_of(a[4], &groups) || y.t->dim() != 2) return none();
+  const int64_t rows = y.t->size(0), width = y.t->size(1);
+  const int io = io_of(y);
+  if (io < 0 || io_of(z) != io || !is(z, {rows, width}) || !f32(weight) || !is(weight, {width}) || !fits({width}) ||
+      (rows > 1 && z.t->stride(0) < width))
+    return none();
+  at::Tensor own;
+  Arg out;
+  if (!output_like(a[6], y, own, out)) return none();
+  const int64_t stride = rows > 1 ? z.t->stride(0) : width;
+  void *const s = stream(), *const op = out.ptr();
+  const void *const yp = y.ptr(), *const zp = z.ptr();
+  const float *const wp = (const float *)weight.ptr();
+  const ssd_status st = released([&] { return block_api.norm_gated(rows, (int32_t)width, groups, io, yp, zp, stride, wp, eps, first, op, s); });
+  return st != SSD_OK ? failed(st) : result(a[6], own);
+  END_HANDLE_TH_ERRORS
+}
+
+// (residual, x, weight, scale, eps, out, residual_out)
+PyObject *norm_residual(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  SSD_ARGS(7);
+  const Arg residual = tensor_or_none(a[0]), x = tensor(a[1]), weight = tensor(a[2]);
+  float scale, eps;
+  if (!residual.ok || !x.ok || !weight.ok || !number_of(a[3], &scale) || !number_of(a[4], &eps) || x.t->dim() != 2) return none();
+  const int64_t rows = x.t->size(0), width = x.t->size(1);
+  const int io = io_of(x);
+  if (io < 0 || !f32(weight) || !is(weight, {width}) || !fits({width}) || (residual.t != nullptr && !is(residual, {rows, width}))) return none();
+  Arg out, ro;
+  if (a[6] != Py_None && !(ro = tensor(a[6])).ok) return none();
+  const Arg &like = residual.t != nullptr ? residual : ro;
+  const int rio = like.t != nullptr ? io_of(like) : SSD_F32;
+  if (rio < 0 || (ro.t != nullptr && (io_of(ro) != rio || ro.t->numel() < rows * width))) return none();
+  at::Tensor own, own_r;
+  if (!output_like(a[5], x, own, out)) return none();
+  if (ro.t == nullptr) {
+    own_r = at::empty({rows, width}, x.t->options().dtype(rio == SSD_F32 ? at::kFloat : at::kBFloat16));
+    ro.t = &own_r;
+  }
+  void *const s = stream(), *const op = out.ptr(), *const rp = ro.ptr();
+  const void *const xp = x.ptr(), *const ip = residual.ptr();
+  const float *const wp = (const float *)weight.ptr();
+  const ssd_status st =
+      released([&] { return block_api.norm_residual(rows, (int32_t)width, io, rio, xp, ip, scale, wp, eps, op, rp, s); });
+  if (st != SSD_OK) return failed(st);
+  PyObject *const r0 = result(a[5], own), *const r1 = result(a[6], own_r);
+  PyObject *const both = r0 != nullptr && r1 != nullptr ? PyTuple_Pack(2, r0, r1) : nullptr;
+  Py_XDECREF(r0);
+  Py_XDECREF(r1);
+  return both;
+  END_HANDLE_TH_ERRORS
+}
+
+// The caches and the device arrays of an attention call, and its shape but for the tokens, heads and window.
+struct Cache {
+  Arg k, v, table, lens, cu;
+  ssd_attn_shape shape = {};
+  bool ok = false;
+};
+bool i32(const Arg &a) { return a.t->scalar_type() == at::kInt; }
+Cache cache_of(PyObject *k, PyObject *v, PyObject *table, PyObject *lens, PyObject *cu, int io, int64_t headdim) {
+  Cache c;
+  c.k = tensor(k);
+  c.v = tensor(v);
+  c.table = tensor(table);
+  c.lens = tensor(lens);
+  c.cu = tensor_or_none(cu);
+  if (!c.k.ok || !c.v.ok || !c.table.ok || !c.lens.ok || !c.cu.ok || c.k.t->dim() != 4 || c.table.t->dim() != 2) return c;
+  const int64_t batch = c.table.t->size(0);
+  if (io < 0 || io_of(c.k) != io || io_of(c.v) != io || c.v.t->sizes() != c.k.t->sizes() || c.k.t->size(3) != headdim || !i32(c.table) ||
+      !i32(c.lens) || !is(c.lens, {batch}) || (c.cu.t != nullptr && (!i32(c.cu) || !is(c.cu, {batch + 1}))) ||
+      !fits({batch, c.k.t->size(0), c.k.t->size(1), c.k.t->size(2), headdim, c.table.t->size(1)}))
+    return c;
+  c.shape.batch = (int32_t)batch;
+  c.shape.nkvheads = (int32_t)c.k.t->size(1);
+  c.shape.headdim = (int32_t)headdim;
+  c.shape.npages = (int32_t)c.k.t->size(0);
+  c.shape.page_size = (int32_t)c.k.t->size(2);
+  c.shape.max_pages = (int32_t)c.table.t->size(1);
+  c.shape.io_dtype = io;
+  c.ok = true;
+  return c;
+}
+
+// (q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved, q_out)
+PyObject *attn_append(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  SSD_ARGS(11);
+  const Arg q = a[0] == Py_None ? Arg() : rows_of(a[0], 3), k = rows_of(a[1], 3), v = rows_of(a[2], 3);
+  const bool queries = a[0] != Py_None;
+  if ((queries && !q.ok) || !k.ok || !v.ok || (!queries && a[10] != Py_None)) return none();
+  const int64_t tokens = k.t->size(0), nkv = k.t->size(1), D = k.t->size(2), heads = queries ? q.t->size(1) : nkv;
+  const int io = io_of(k), inter = a[9] == Py_True ? 1 : a[9] == Py_False ? 0 : -1;
+  if (io < 0 || inter < 0 || io_of(v) != io || !is(v, {tokens, nkv, D}) || (queries && (io_of(q) != io || !is(q, {tokens, heads, D}))))
+    return none();
+  Cache c = cache_of(a[3], a[4], a[5], a[6], a[7], io, D);
+  if (!c.ok || c.shape.nkvheads != nkv || !fits({tokens, heads}) || (c.cu.t == nullptr && tokens != c.shape.batch)) return none();
+  // a token's heads are dense, tokens are any distance apart
+  for (const Arg *t : {&q, &k, &v})
+    if (t->t != nullptr && t->t->size(1) > 1 && t->t->stride(1) != D) return none();
+  const auto stride = [&](const Arg &t) { return t.t == nullptr ? (int64_t)0 : tokens > 1 ? t.t->stride(0) : t.t->size(1) * D; };
+  ssd_rope rope = {};
+  rope.interleaved = inter;
+  if (a[8] != Py_None) {
+    const bool tup = PyTuple_CheckExact(a[8]);
+    if ((!tup && !PyList_CheckExact(a[8])) || (tup ? PyTuple_GET_SIZE(a[8]) : PyList_GET_SIZE(a[8])) != 2) return none();
+    const Arg cs = tensor(tup ? PyTuple_GET_ITEM(a[8], 0) : PyList_GET_ITEM(a[8], 0)), sn = tensor(tup ? PyTuple_GET_ITEM(a[8], 1) : PyList_GET_ITEM(a[8], 1));
+    if (!cs.ok || !sn.ok || !f32(cs) || !f32(sn) || cs.t->dim() != 2 || sn.t->sizes() != cs.t->sizes() || !fits({cs.t->size(0), 2 * cs.t->size(1)}))
+      return none();
+    rope.cos = (const float *)cs.ptr();
+    rope.sin = (const float *)sn.ptr();
+    rope.rotary = (int32_t)(2 * cs.t->size(1));
+    rope.positions = (int32_t)cs.t->size(0);
+  }
+  at::Tensor own;
+  Arg out;
+  if (queries) {
+    if (a[10] == Py_None) {
+      own = at::empty({tokens, heads, D}, q.t->options());
+      out.t = &own;
+    } else if (!(out = tensor(a[10])).ok || io_of(out) != io || out.t->numel() < q.t->numel()) {
+      return none();
+    }
+  }
+  c.shape.tokens = (int32_t)tokens;
+  c.shape.nheads = (int32_t)heads;
+  void *const s = stream();
+  const void *const qp = q.ptr(), *const kp = k.ptr(), *const vp = v.ptr();
+  void *const op = out.ptr(), *const kc = c.k.ptr(), *const vc = c.v.ptr();
+  const int32_t *const cu = (const int32_t *)c.cu.ptr(), *const lens = (const int32_t *)c.lens.ptr(), *const table = (const int32_t *)c.table.ptr();
+  const int64_t qs = stride(q), ks = stride(k), vs = stride(v);
+  const ssd_status st =
+      released([&] { return block_api.attn_append(&c.shape, &rope, cu, lens, table, qp, qs, kp, ks, vp, vs, op, kc, vc, s); });
+  if (st != SSD_OK) return failed(st);
+  // (nothing to return is not the same as nothing done: False)
+  if (!queries) Py_RETURN_FALSE;
+  return result(a[10], own);
+  END_HANDLE_TH_ERRORS
+}
+
+// (q, k_cache, v_cache, page_table, seq_lens, scale, window, y, workspace); prefill: cu_seqlens before scale
+template <bool kStep>
+PyObject *attn(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  constexpr int k = kStep ? 0 : 1;
+  SSD_ARGS(9 + k);
+  const Arg q = tensor(a[0]);
+  if (!q.ok || q.t->dim() != 3 || (!kStep && a[5] == Py_None)) return none();
+  const int64_t tokens = q.t->size(0), heads = q.t->size(1), D = q.t->size(2);
+  Cache c = cache_of(a[1], a[2], a[3], a[4], kStep ? Py_None : a[5], io_of(q), D);
+  float scale = 0.f;
+  if (!c.ok || !fits({tokens, heads}) || (kStep && tokens != c.shape.batch) || !int_of(a[6 + k], &c.shape.window)) return none();
+  if (a[5 + k] == Py_None)
+    scale = D > 0 ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(D))) : 0.f;
+  else if (!number_of(a[5 + k], &scale))
+    return none();
+  c.shape.tokens = (int32_t)tokens;
+  c.shape.nheads = (int32_t)heads;
+  at::Tensor own, own_w;
+  Arg y, w;
+  if (a[8 + k] != Py_None && !(w = tensor(a[8 + k])).ok) return none();
+  if (!output_like(a[7 + k], q, own, y)) return none();
+  if (a[8 + k] == Py_None) {
+    const size_t need = kStep ? block_api.attn_step_workspace_bytes(&c.shape) : block_api.attn_prefill_workspace_bytes(&c.shape);
+    own_w = at::empty({(int64_t)(need > 256 ? need : 256)}, q.t->options().dtype(at::kByte));
+    w.t = &own_w;
+  }
+  const size_t bytes = w.t->nbytes();
+  void *const s = stream();
+  const void *const qp = q.ptr(), *const kc = c.k.ptr(), *const vc = c.v.ptr();
+  void *const yp = y.ptr(), *const wp = w.ptr();
+  const int32_t *const cu = (const int32_t *)c.cu.ptr(), *const lens = (const int32_t *)c.lens.ptr(), *const table = (const int32_t *)c.table.ptr();
+  const ssd_status st = released([&] {
+    return kStep ? block_api.attn_step(&c.shape, lens, table, qp, kc, vc, scale, yp, wp, bytes, s)
+                 : block_api.attn_prefill(&c.shape, cu, lens, table, qp, kc, vc, scale, yp, wp, bytes, s);
+  });
+  return st != SSD_OK ? failed(st) : result(a[7 + k], own);
+  END_HANDLE_TH_ERRORS
+}
+
+// init(addresses), init_block(addresses): the functions of the C ABI in the order of Api, of BlockApi
+template <typename A, A *kTo>
 PyObject *init(PyObject *, PyObject *list) {
-  constexpr Py_ssize_t kCount = sizeof(Api) / sizeof(void *);
+  constexpr Py_ssize_t kCount = sizeof(A) / sizeof(void *);
   if (!PyList_Check(list) || PyList_GET_SIZE(list) != kCount) {
     PyErr_SetString(PyExc_ValueError, "a list of the addresses of the C ABI is expected");
     return nullptr;
   }
-  void **const at = reinterpret_cast<void **>(&api);
+  void **const at = reinterpret_cast<void **>(kTo);
   for (Py_ssize_t i = 0; i < kCount; ++i) {
     at[i] = PyLong_AsVoidPtr(PyList_GET_ITEM(list, i));
     if (at[i] == nullptr) {
@@ -355,7 +579,8 @@ PyObject *init(PyObject *, PyObject *list) {
 
 #define SSD_FAST(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
-    {"init", init, METH_O, nullptr},
+    {"init", init<Api, &api>, METH_O, nullptr},
+    {"init_block", init<BlockApi, &block_api>, METH_O, nullptr},
     SSD_FAST("decode_step", decode_step),
     SSD_FAST("decode_step_layers", decode_layers<false>),
     SSD_FAST("decode_steps_layers", decode_layers<true>),
@@ -363,6 +588,11 @@ PyMethodDef methods[] = {
     SSD_FAST("prefill_varlen", prefill<true>),
     SSD_FAST("conv1d_prefill", conv1d<false>),
     SSD_FAST("conv1d_step", conv1d<true>),
+    SSD_FAST("norm_gated", norm_gated),
+    SSD_FAST("norm_residual", norm_residual),
+    SSD_FAST("attn_append", attn_append),
+    SSD_FAST("attn_step", attn<true>),
+    SSD_FAST("attn_prefill", attn<false>),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ssd_binding", "Native marshalling of paper_2603_09555_amd.ssd, built for torch " SSD_TORCH_VERSION ";", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

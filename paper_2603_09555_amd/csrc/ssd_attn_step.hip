@@ -1,13 +1,496 @@
-// Attention of one new token of each sequence over a paged cache.
-#include "ssd_attn_simple.hpp"
+// Attention of one new token of each sequence over a paged cache:  y[b][h] = sum_t softmax_t(scale q[b][h] . K[t]) V[t].
+//
+// Bound by the one pass over K and V.  The query heads of a key head (16 at a time) are the columns of 16 x 16 matrix products,
+// so that K and V are read once for all of them:
+//
+//   S^T (tokens x heads) = K Q^T,   p = 2^(S - running maximum),   O^T (values x heads) = V^T P^T
+//
+// A wave walks tiles of 32 tokens by itself, with the running maximum m, sum l and O^T of its heads in registers, and no LDS:
+//   * K's rows go from memory into the first operand as they lie (a lane holds 8 values of bf16, or 4 of fp32, of one token);
+//   * the product leaves a lane with 8 of the 32 tokens of one head -- tokens 4j..4j+3 of either half, j = lane / 16 --, and a
+//     contraction does not mind the order of its tokens: these eight are what the lane supplies as the second operand of V^T P^T;
+//   * the first operand is then eight values of one column of V, from eight tokens.  A lane reads its eight tokens' rows, some
+//     neighbouring columns of each, and makes the columns' operands by exchanging halves of registers (bf16; fp32 needs none).
+//
+// Work is dealt by length: the visible tokens of all sequences and key heads, in blocks of 128, make one long list of which every
+// workgroup takes an equal run, whatever the lengths are; the four waves of a workgroup take every fourth tile of a block's 32
+// tokens and are joined through LDS at the end of a unit (a sequence and key head).  A unit within one workgroup is finished
+// there; the others leave (m, l, O) in the workspace, which a second launch joins.
+#include "ssd_attn.hpp"
 
 namespace ssd {
+namespace {
 
-size_t attn_step_workspace_bytes(const AttnDims &) { return 256; }
+using namespace block;
+
+constexpr int kThreads = 256, kWaves = 4, kTile = 32, kBlock = kWaves * kTile, kRows = 16;
+constexpr int kWorkgroups = 1024;  // a power of two
+constexpr int kLgWorkgroups = 10;
+constexpr unsigned kFewUnits = 256;
+constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
+
+struct StepArgs {
+  const int32_t *lens, *table;
+  const void *q, *k, *v;
+  void *y;
+  float *part;       // per workgroup two slots of kRows x (D + 2): O, m, l of a unit that began before its run, and of its last one
+  AttnDims d;
+  int row_tiles;     // of 16 heads, of a key head's heads
+  int units;         // of a sequence
+  float scale_log2;  // scale * log2(e)
+};
+
+struct Span {
+  int lo, len, base, blocks;  // tokens seen: [lo, len), in blocks of 128 from base on
+};
+__device__ __forceinline__ Span span_of(const StepArgs &a, int b) {
+  Span s;
+  s.len = cut_length(a.d, a.lens[b]);
+  s.lo = a.d.window > 0 ? max(0, s.len - a.d.window) : 0;
+  s.base = s.lo & ~(kTile - 1);
+  s.blocks = (s.len - s.base + kBlock - 1) / kBlock;
+  return s;
+}
+
+// Blocks (of one unit each) of the sequences in front of each thread's share of them; [kThreads]: of all.
+struct Prefix {
+  int64_t at[kThreads + 1];
+  int64_t wave[kWaves];
+};
+__device__ __forceinline__ void count_blocks(const StepArgs &a, Prefix &s) {
+  const int t = threadIdx.x, lane = t & 63, share = (a.d.B + kThreads - 1) / kThreads;
+  int64_t mine = 0;
+  for (int b = t * share; b < min((t + 1) * share, a.d.B); ++b) mine += span_of(a, b).blocks;
+  int64_t sum = mine;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const int64_t o = __shfl_up(sum, k);
+    if (lane >= k) sum += o;
+  }
+  if (lane == 63) s.wave[t / 64] = sum;
+  __syncthreads();
+  for (int w = 0; w < t / 64; ++w) sum += s.wave[w];
+  s.at[t + 1] = sum;
+  if (t == 0) s.at[0] = 0;
+  __syncthreads();
+}
+
+// Exchanges halves: the low (or high) 16 bits of two registers.
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// One wave's operands for head vectors of up to DP values (a multiple of 64; D are there, the others are zeros).  A lane is
+// (j = lane / 16, n = lane % 16).
+//   key piece i of a token: its 16 bytes at byte 64 i + 16 j;  a lane's columns of V: columns(c) for c < DP / 16
+template <bool kBf16, int DP>
+struct Tile {
+  static constexpr int kSize = kBf16 ? 2 : 4;
+  static constexpr int kKeyPieces = DP * kSize / 64;
+  static constexpr int kCols = DP / 16;                         // of V, a lane
+  static constexpr int kValuePieces = kCols * kSize / 16 > 0 ? kCols * kSize / 16 : 1;  // of 16 bytes (one of 8 if that is less)
+  static constexpr bool kHalfPiece = kCols * kSize == 8;
+
+  u32x4 key[2][kKeyPieces];
+  u32x4 val[8][kValuePieces];
+
+  // Byte of a row where the lane's piece p of V begins.
+  static __device__ __forceinline__ int value_byte(int p, int n) { return kBf16 ? n * kCols * 2 + 16 * p : 256 * p + 16 * n; }
+  // Column of V that element c of the lane n's operands stands for.
+  static __device__ __forceinline__ int column(int c, int n) { return kBf16 ? n * kCols + c : 64 * (c / 4) + 4 * n + c % 4; }
+
+  __device__ __forceinline__ void load_key(int half, const char *row, int j, int bytes) {
+#pragma unroll
+    for (int i = 0; i < kKeyPieces; ++i) {
+      const int at = 64 * i + 16 * j;
+      u32x4 q = {0u, 0u, 0u, 0u};
+      if (at < bytes) q = *reinterpret_cast<const u32x4 *>(row + at);
+      key[half][i] = q;
+    }
+  }
+  __device__ __forceinline__ void load_value(int i, const char *row, int n, int bytes) {
+#pragma unroll
+    for (int p = 0; p < kValuePieces; ++p) {
+      const int at = value_byte(p, n);
+      u32x4 q = {0u, 0u, 0u, 0u};
+      if (at < bytes) {
+        if (kHalfPiece) {
+          const u32x2 h = *reinterpret_cast<const u32x2 *>(row + at);
+          q[0] = h[0];
+          q[1] = h[1];
+        } else {
+          q = *reinterpret_cast<const u32x4 *>(row + at);
+        }
+      }
+      val[i][p] = q;
+    }
+  }
+  __device__ __forceinline__ void clear_value(int i) {
+#pragma unroll
+    for (int p = 0; p < kValuePieces; ++p) val[i][p] = u32x4{0u, 0u, 0u, 0u};
+  }
+
+  __device__ __forceinline__ f32x4 scores(int half, const u32x4 (&query)[kKeyPieces]) const {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kKeyPieces; ++i) {
+      if (kBf16) {
+        s = mfma_bf16(key[half][i], query[i], s);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = mfma_f32(__uint_as_float(key[half][i][e]), __uint_as_float(query[i][e]), s);
+      }
+    }
+    return s;
+  }
+  // O^T += V^T P^T; p: the lane's eight tokens
+  __device__ __forceinline__ void add(const float (&p)[8], f32x4 (&o)[kCols]) const {
+    if (kBf16) {
+      u32x4 pb;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pb[i] = pack2(p[2 * i], p[2 * i + 1]);
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) {
+        u32x4 a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = val[2 * i][c / 8][(c / 2) % 4], y = val[2 * i + 1][c / 8][(c / 2) % 4];
+          a[i] = c % 2 == 0 ? low_halves(x, y) : high_halves(x, y);
+        }
+        o[c] = mfma_bf16(a, pb, o[c]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) o[c] = mfma_f32(__uint_as_float(val[i][c / 4][c % 4]), p[i], o[c]);
+    }
+  }
+};
+
+template <bool kBf16, int DP>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void step_kernel(const StepArgs a) {
+  using T = Tile<kBf16, DP>;
+  __shared__ union {
+    Prefix prefix;
+    struct {
+      float o[kWaves][kRows][DP + 4];
+      float m[kWaves][kRows], l[kWaves][kRows];
+    } join;
+  } lds;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, j = lane / 16, n = lane % 16;
+  const int rows_of_heads = a.d.G, bytes = a.d.D * T::kSize;
+  const int64_t page_bytes = (static_cast<int64_t>(a.d.Hk) << a.d.lg_page) * bytes;
+  const int page_mask = (1 << a.d.lg_page) - 1;
+
+  // the run of this workgroup, and where it begins
+  count_blocks(a, lds.prefix);
+  const int64_t total = lds.prefix.at[kThreads] * a.units;
+  const int64_t run = (total + kWorkgroups - 1) >> kLgWorkgroups;
+  int64_t at = blockIdx.x * run;
+  const int64_t end = min(total, at + run);
+  if (at >= end) return;
+  int share = 0;
+#pragma unroll
+  for (int s = kThreads / 2; s > 0; s >>= 1)
+    if (lds.prefix.at[share + s] * a.units <= at) share += s;
+  int b = share * ((a.d.B + kThreads - 1) / kThreads);
+  int64_t left = at - lds.prefix.at[share] * a.units;
+  Span sp = span_of(a, b);
+  while (left >= static_cast<int64_t>(sp.blocks) * a.units) {
+    left -= static_cast<int64_t>(sp.blocks) * a.units;
+    sp = span_of(a, ++b);
+  }
+  int unit = static_cast<int>(left / sp.blocks), block = static_cast<int>(left - static_cast<int64_t>(unit) * sp.blocks);
+  bool continued = block > 0;
+  __syncthreads();
+
+  while (true) {
+    const int blocks = static_cast<int>(min(static_cast<int64_t>(sp.blocks - block), end - at));
+    const int hk = unit / a.row_tiles, first_row = (unit - hk * a.row_tiles) * kRows;
+    const int rows = min(kRows, rows_of_heads - first_row);
+    const int64_t row0 = static_cast<int64_t>(b) * a.d.H + hk * a.d.G + first_row;  // of q and y
+    const int32_t *table = a.table + static_cast<int64_t>(b) * a.d.max_pages;
+    const char *kh = static_cast<const char *>(a.k) + (static_cast<int64_t>(hk) << a.d.lg_page) * bytes;
+    const char *vh = static_cast<const char *>(a.v) + (static_cast<int64_t>(hk) << a.d.lg_page) * bytes;
+
+    u32x4 query[T::kKeyPieces];
+#pragma unroll
+    for (int i = 0; i < T::kKeyPieces; ++i) {
+      const int byte = 64 * i + 16 * j;
+      query[i] = u32x4{0u, 0u, 0u, 0u};
+      if (n < rows && byte < bytes)
+        query[i] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q) + (row0 + n) * bytes + byte);
+    }
+    f32x4 o[T::kCols];
+#pragma unroll
+    for (int c = 0; c < T::kCols; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = kNone, l = 0.f;
+
+    for (int first = sp.base + block * kBlock + wave * kTile; first < min(sp.len, sp.base + (block + blocks) * kBlock); first += kBlock) {
+      T t;
+      // pages of tokens n and 16 + n of the tile (tokens that aren't seen: of the nearest one that is)
+      int page[2];
+      uint32_t seen = 0xffffffffu;
+      {
+        uint32_t gone = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int token = min(max(first + 16 * h + n, sp.lo), sp.len - 1);
+          page[h] = table[token >> a.d.lg_page];
+          const bool bad = static_cast<unsigned>(page[h]) >= static_cast<unsigned>(a.d.npages);
+          gone |= static_cast<uint32_t>(__ballot(bad) & 0xffffu) << (16 * h);
+          if (bad) page[h] = 0;
+          t.load_key(h, kh + page[h] * page_bytes + (token & page_mask) * bytes, j, bytes);
+        }
+        if (first < sp.lo) seen &= 0xffffffffu << (sp.lo - first);
+        if (first + kTile > sp.len) seen &= 0xffffffffu >> (first + kTile - sp.len);
+        seen &= ~gone;
+      }
+      if (a.d.lg_page >= 2) {  // four neighbouring tokens of an aligned tile are on one page
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int64_t where = __shfl(page[h], 4 * j) * page_bytes;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int token = min(max(first + 16 * h + 4 * j + r, sp.lo), sp.len - 1);
+            const int64_t row = token >> 2 == (first + 16 * h + 4 * j) >> 2 ? where + (token & page_mask) * bytes : where;
+            t.load_value(4 * h + r, vh + row, n, bytes);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int token = min(max(first + 16 * h + 4 * j + r, sp.lo), sp.len - 1);
+            t.load_value(4 * h + r, vh + __shfl(page[h], 4 * j + r) * page_bytes + (token & page_mask) * bytes, n, bytes);
+          }
+      }
+      f32x4 s[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s[h] = t.scores(h, query);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[h][r] *= a.scale_log2;
+      }
+      if (seen != 0xffffffffu) {  // (what isn't seen may hold anything: no product with it is kept)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (!((seen >> (16 * h + 4 * j + r)) & 1u)) {
+              s[h][r] = -INFINITY;
+              t.clear_value(4 * h + r);
+            }
+      }
+      float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > m)) {
+        const float next = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(m - next);
+        m = next;
+        l *= keep;
+#pragma unroll
+        for (int c = 0; c < T::kCols; ++c)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[c][r] *= keep;
+      }
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(s[i / 4][i % 4] - m);
+        l += p[i];
+      }
+      t.add(p, o);
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // join the waves
+    if (j == 0) {
+      lds.join.m[wave][n] = m;
+      lds.join.l[wave][n] = l;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < T::kCols; c += 4) {
+        const f32x4 q = {o[c][r], o[c + 1][r], o[c + 2][r], o[c + 3][r]};
+        *reinterpret_cast<f32x4 *>(&lds.join.o[wave][n][T::column(c, 4 * j + r)]) = q;
+      }
+    __syncthreads();
+    const bool whole = blocks == sp.blocks;
+    const int slot_row = (2 * static_cast<int>(blockIdx.x) + (continued ? 0 : 1)) * kRows;
+    for (int e = threadIdx.x; e < rows * (DP / 4); e += kThreads) {
+      const int row = e / (DP / 4), col = (e % (DP / 4)) * 4;
+      if (col >= a.d.D) continue;
+      float top = kNone, f[kWaves], sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds.join.m[w][row]);
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(lds.join.m[w][row] - top);
+        sum = fmaf(lds.join.l[w][row], f[w], sum);
+        const f32x4 ow = *reinterpret_cast<const f32x4 *>(&lds.join.o[w][row][col]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = fmaf(ow[r], f[w], v[r]);
+      }
+      if (whole) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (kBf16) {
+          const u32x2 q = {pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
+          *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + (row0 + row) * a.d.D + col) = q;
+        } else {
+          const f32x4 q = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+          *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + (row0 + row) * a.d.D + col) = q;
+        }
+      } else {
+        float *part = a.part + static_cast<int64_t>(slot_row + row) * (a.d.D + 4);
+        *reinterpret_cast<f32x4 *>(part + col) = v;
+        if (col == 0) {
+          part[a.d.D] = top;
+          part[a.d.D + 1] = sum;
+        }
+      }
+    }
+    at += blocks;
+    if (at >= end) break;
+    __syncthreads();
+    block = 0;
+    continued = false;
+    if (++unit == a.units) {
+      unit = 0;
+      do sp = span_of(a, ++b);
+      while (sp.blocks == 0);
+    }
+  }
+}
+
+// Joins what the workgroups of a unit left.  A workgroup takes `rows` heads and `cols` pieces of four values of a unit (all of
+// them where there are many units), and as many of the parts at a time as it has threads for.
+template <bool kBf16>
+__global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int rows, int cols, int row_cuts, int col_cuts) {
+  __shared__ Prefix prefix;
+  __shared__ float got[kThreads][6];
+  unsigned id = blockIdx.x;
+  const int col_cut = static_cast<int>(id % col_cuts), row_cut = static_cast<int>(id / col_cuts % row_cuts);
+  id /= static_cast<unsigned>(col_cuts * row_cuts);
+  const int b = static_cast<int>(id / static_cast<unsigned>(a.units)), unit = static_cast<int>(id) - b * a.units;
+  count_blocks(a, prefix);
+  const int64_t total = prefix.at[kThreads] * a.units, run = (total + kWorkgroups - 1) >> kLgWorkgroups;
+  const int share = (a.d.B + kThreads - 1) / kThreads;
+  int64_t before = prefix.at[b / share];
+  for (int i = b / share * share; i < b; ++i) before += span_of(a, i).blocks;
+  const Span sp = span_of(a, b);
+  const int hk = unit / a.row_tiles, first_row = (unit - hk * a.row_tiles) * kRows;
+  const int64_t row0 = static_cast<int64_t>(b) * a.d.H + hk * a.d.G + first_row;
+  const int row_end = min(min(kRows, a.d.G - first_row), (row_cut + 1) * rows), col_end = min(a.d.D / 4, (col_cut + 1) * cols);
+  int first = 0, last = -1;
+  int64_t begin = 0;
+  if (sp.blocks > 0) {
+    begin = before * a.units + static_cast<int64_t>(unit) * sp.blocks;
+    first = static_cast<int>(begin / run);
+    last = static_cast<int>((begin + sp.blocks - 1) / run);
+    if (first == last) return;  // finished where it was computed
+  }
+  const int items = rows * cols, abreast = max(1, kThreads / items);
+  for (int e0 = 0; e0 < items; e0 += kThreads) {
+    const int e = e0 + (items < kThreads ? threadIdx.x % items : threadIdx.x), lane = items < kThreads ? threadIdx.x / items : 0;
+    const int row = row_cut * rows + e / cols, col = 4 * (col_cut * cols + e % cols);
+    const bool mine = e < items && lane < abreast && row < row_end && col < 4 * col_end;
+    float top = kNone, sum = 0.f;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (mine) {
+#pragma unroll 4
+      for (int w = first + lane; w <= last; w += abreast) {
+        const int slot_row = (2 * w + (begin >= w * run ? 1 : 0)) * kRows + row;
+        const float *part = a.part + static_cast<int64_t>(slot_row) * (a.d.D + 4);
+        const float m = part[a.d.D], l = part[a.d.D + 1];
+        const f32x4 o = *reinterpret_cast<const f32x4 *>(part + col);
+        const float next = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(top - next), f = __builtin_amdgcn_exp2f(m - next);
+        top = next;
+        sum = fmaf(sum, keep, l * f);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = fmaf(v[r], keep, o[r] * f);
+      }
+    }
+    if (abreast > 1) {
+      float *g = got[threadIdx.x];
+      g[0] = top;
+      g[1] = sum;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) g[2 + r] = v[r];
+      __syncthreads();
+      if (mine && lane == 0)
+        for (int i = 1; i < abreast; ++i) {
+          const float *p = got[threadIdx.x + i * items];
+          const float next = fmaxf(top, p[0]), keep = __builtin_amdgcn_exp2f(top - next), f = __builtin_amdgcn_exp2f(p[0] - next);
+          top = next;
+          sum = fmaf(sum, keep, p[1] * f);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = fmaf(v[r], keep, p[2 + r] * f);
+        }
+    }
+    if (mine && lane == 0) {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      if (kBf16) {
+        const u32x2 q = {pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
+        *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + (row0 + row) * a.d.D + col) = q;
+      } else {
+        const f32x4 q = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + (row0 + row) * a.d.D + col) = q;
+      }
+    }
+  }
+}
+
+template <bool kBf16>
+hipError_t launch(const StepArgs &a, hipStream_t stream) {
+  const dim3 grid(kWorkgroups), threads(kThreads);
+  if (a.d.D <= 64)
+    hipLaunchKernelGGL((step_kernel<kBf16, 64>), grid, threads, 0, stream, a);
+  else if (a.d.D <= 128)
+    hipLaunchKernelGGL((step_kernel<kBf16, 128>), grid, threads, 0, stream, a);
+  else
+    hipLaunchKernelGGL((step_kernel<kBf16, 256>), grid, threads, 0, stream, a);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  // Few units have many parts each, up to one of every workgroup: a workgroup for 32 values of a head.
+  const unsigned units = static_cast<unsigned>(a.units) * a.d.B;
+  const int tile_rows = a.d.G < kRows ? a.d.G : kRows, all_cols = a.d.D / 4;
+  const bool few = units < kFewUnits;
+  const int rows = few ? 1 : tile_rows, cols = few && all_cols > 8 ? 8 : all_cols;
+  const int row_cuts = (tile_rows + rows - 1) / rows, col_cuts = (all_cols + cols - 1) / cols;
+  hipLaunchKernelGGL(join_kernel<kBf16>, dim3(units * row_cuts * col_cuts), threads, 0, stream, a, rows, cols, row_cuts, col_cuts);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attn_step_workspace_bytes(const AttnDims &d) {
+  return (static_cast<size_t>(2 * kWorkgroups * kRows) * (d.D + 4) * 4 + 255) / 256 * 256;
+}
 
 hipError_t launch_attn_step(const AttnDims &d, const int32_t *lens, const int32_t *table, const void *q, const void *k_cache,
-                            const void *v_cache, float scale, void *y, void *, hipStream_t stream) {
-  return launch_attn_rows(d, nullptr, lens, table, q, k_cache, v_cache, scale, y, stream);
+                            const void *v_cache, float scale, void *y, void *workspace, hipStream_t stream) {
+  StepArgs a = {};
+  a.lens = lens;
+  a.table = table;
+  a.q = q;
+  a.k = k_cache;
+  a.v = v_cache;
+  a.y = y;
+  a.part = static_cast<float *>(workspace);
+  a.d = d;
+  a.row_tiles = (d.G + kRows - 1) / kRows;
+  a.units = d.Hk * a.row_tiles;
+  a.scale_log2 = scale * 1.44269504f;
+  return d.bf16 ? launch<true>(a, stream) : launch<false>(a, stream);
 }
 
 }  // namespace ssd

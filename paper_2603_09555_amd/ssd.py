@@ -135,6 +135,9 @@ try:
                    "ssd_prefill_varlen", "ssd_prefill_varlen_dt", "ssd_decode_step", "ssd_decode_step_layers",
                    "ssd_decode_step_layers_dt", "ssd_decode_steps_layers", "ssd_decode_steps_layers_dt", "ssd_conv1d_prefill",
                    "ssd_conv1d_step")])
+    _native.init_block([ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in
+                        ("ssd_norm_gated", "ssd_norm_residual", "ssd_attn_append", "ssd_attn_step_workspace_bytes", "ssd_attn_step",
+                         "ssd_attn_prefill_workspace_bytes", "ssd_attn_prefill")])
 except ImportError as e:
     warnings.warn("_ssd_binding.so is missing or does not fit, calls go through Python (some 5 us more host time each): build it "
                   "with `python -m paper_2603_09555_amd.build` (%s)" % e, RuntimeWarning)
@@ -142,6 +145,7 @@ except ImportError as e:
     class _native:
         """Leaves every call to the Python below."""
         prefill = prefill_varlen = decode_step = decode_step_layers = decode_steps_layers = conv1d_prefill = conv1d_step = \
+            norm_gated = norm_residual = attn_append = attn_step = attn_prefill = \
             staticmethod(lambda *args: None)
 
 
@@ -486,6 +490,9 @@ def ssd_norm_gated(y, z, weight, eps=1e-5, groups=1, norm_first=False, out=None)
     """``ssd_norm_gated``: ``y (rows,width)`` and its gate ``z (rows,width)`` in fp32 or bf16, ``weight (width)`` fp32.  ``z`` may
     be a slice of wider rows.  Each of ``groups`` ranges of a row is normalised by itself, ``y * silu(z)`` or, with
     ``norm_first``, ``y``, which is gated afterwards.  Returns ``out (rows,width)``, which may be ``y``."""
+    done = _native.norm_gated(y, z, weight, eps, groups, norm_first, out)
+    if done is not None:
+        return _done(done, "ssd_norm_gated")
     rows, width = y.shape
     if z.shape != y.shape or z.dtype != y.dtype or weight.shape != (width,) or weight.dtype != torch.float32:
         raise ValueError("z must be like y, and weight fp32 of the rows' width")
@@ -506,6 +513,9 @@ def ssd_norm_residual(residual, x, weight, scale=1.0, eps=1e-5, out=None, residu
     """``ssd_norm_residual``: ``residual + scale * x`` and its norm times ``weight (width)`` fp32.  ``x (rows,width)`` in fp32 or
     bf16; ``residual`` of the same shape in fp32 or the type of ``x``, or None for zeros (``residual_out`` is then fp32 unless
     given).  Returns ``(out, residual_out)``; ``residual_out`` may be ``residual``, ``out`` may be ``x``."""
+    done = _native.norm_residual(residual, x, weight, scale, eps, out, residual_out)
+    if done is not None:
+        return _done(done, "ssd_norm_residual")
     rows, width = x.shape
     if weight.shape != (width,) or weight.dtype != torch.float32 or (residual is not None and residual.shape != x.shape):
         raise ValueError("residual must have the shape of x, and weight must be fp32 of the rows' width")
@@ -562,6 +572,9 @@ def ssd_attn_append(q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens=
     fp32 with a row for every position that ``page_table (batch,max_pages)`` can hold, or None.  ``seq_lens (batch)`` counts the new
     tokens too; without ``cu_seqlens (batch+1)`` every sequence has one.  ``q``, ``k`` and ``v`` may be slices of one projection's
     output.  Returns ``q_out``, or None without ``q``."""
+    out = _native.attn_append(q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved, q_out)
+    if out is not None:
+        return None if out is False else _done(out, "ssd_attn_append")
     tokens, nkv, D = k.shape
     if v.shape != k.shape or v.dtype != k.dtype or (q is not None and (q.dtype != k.dtype or q.dim() != 3 or q.shape[0] != tokens or q.shape[2] != D)):
         raise ValueError("q, k and v must share one dtype, and agree in tokens and headdim")
@@ -621,6 +634,9 @@ def ssd_attn_step(q, k_cache, v_cache, page_table, seq_lens, scale=None, window=
     """``ssd_attn_step``: attention of one new token of each sequence, ``q (batch,nheads,headdim)``, over its ``seq_lens (batch)``
     tokens in the caches ``(npages,nkvheads,page_size,headdim)``, the last ``window`` of them if that is not 0.  ``scale`` is
     ``headdim ** -0.5`` unless given.  Returns ``y`` like ``q``."""
+    out = _native.attn_step(q, k_cache, v_cache, page_table, seq_lens, scale, window, y, workspace)
+    if out is not None:
+        return _done(out, "ssd_attn_step")
     return _attn("ssd_attn_step", q, k_cache, v_cache, page_table, seq_lens, None, scale, window, y, workspace)
 
 
@@ -628,6 +644,9 @@ def ssd_attn_prefill(q, k_cache, v_cache, page_table, seq_lens, cu_seqlens, scal
     """``ssd_attn_prefill``: causal attention of packed new tokens ``q (tokens,nheads,headdim)``, sequence b's being
     ``cu_seqlens[b]`` to ``cu_seqlens[b+1]`` and the last of its ``seq_lens[b]``, over the caches they were appended to.
     Otherwise as ``ssd_attn_step``."""
+    out = _native.attn_prefill(q, k_cache, v_cache, page_table, seq_lens, cu_seqlens, scale, window, y, workspace)
+    if out is not None:
+        return _done(out, "ssd_attn_prefill")
     if cu_seqlens is None:
         raise ValueError("ssd_attn_prefill needs cu_seqlens")
     return _attn("ssd_attn_prefill", q, k_cache, v_cache, page_table, seq_lens, cu_seqlens, scale, window, y, workspace)
