@@ -60,6 +60,9 @@ ssd_status attn_pointers(const int32_t *seq_lens, const int32_t *page_table, con
   return SSD_OK;
 }
 
+// A scale of the logits: positive and finite.
+bool scale_ok(float scale) { return scale > 0.f && scale <= 1.0e30f; }
+
 bool workspace_ok(const void *workspace, size_t given, size_t need) {
   return workspace && given >= need && (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0;
 }
@@ -133,6 +136,7 @@ ssd_status ssd_attn_step(const ssd_attn_shape *shape, const int32_t *seq_lens, c
                          void *hip_stream) {
   AttnDims d;
   if (const ssd_status st = make_dims(shape, false, &d); st != SSD_OK) return st;
+  if (!scale_ok(scale)) return SSD_ERR_SHAPE;
   if (const ssd_status st = attn_pointers(seq_lens, page_table, q, k_cache, v_cache, y); st != SSD_OK) return st;
   if (!workspace_ok(workspace, workspace_bytes, ssd::attn_step_workspace_bytes(d))) return SSD_ERR_WORKSPACE;
   return status_of(ssd::launch_attn_step(d, seq_lens, page_table, q, k_cache, v_cache, scale, y, workspace,
@@ -149,6 +153,7 @@ ssd_status ssd_attn_prefill(const ssd_attn_shape *shape, const int32_t *cu_seqle
                             void *y, void *workspace, size_t workspace_bytes, void *hip_stream) {
   AttnDims d;
   if (const ssd_status st = make_dims(shape, true, &d); st != SSD_OK) return st;
+  if (!scale_ok(scale)) return SSD_ERR_SHAPE;
   if (!cu_seqlens) return SSD_ERR_NULL;
   if (const ssd_status st = attn_pointers(seq_lens, page_table, q, k_cache, v_cache, y); st != SSD_OK) return st;
   if (!aligned4(cu_seqlens)) return SSD_ERR_ALIGN;

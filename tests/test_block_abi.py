@@ -24,11 +24,11 @@ def test_attention_refuses():
     need_s, need_p = ssd.attn_step_workspace_bytes(shape()), ssd.attn_prefill_workspace_bytes(shape())
     assert need_s > 0 and need_p > 0 and need_s % 256 == 0 and need_p % 256 == 0
 
-    def step(s=shape(), lens=FAKE, table=FAKE, q=FAKE, k=FAKE, v=FAKE, y=FAKE, w=FAKE, wb=need_s):
-        return lib.ssd_attn_step(ctypes.byref(s) if s is not None else None, lens, table, q, k, v, 0.1, y, w, ctypes.c_size_t(wb), None)
+    def step(s=shape(), lens=FAKE, table=FAKE, q=FAKE, k=FAKE, v=FAKE, y=FAKE, w=FAKE, wb=need_s, scale=0.1):
+        return lib.ssd_attn_step(ctypes.byref(s) if s is not None else None, lens, table, q, k, v, scale, y, w, ctypes.c_size_t(wb), None)
 
-    def prefill(s=shape(), lens=FAKE, table=FAKE, q=FAKE, k=FAKE, v=FAKE, y=FAKE, w=FAKE, wb=need_p, cu=FAKE):
-        return lib.ssd_attn_prefill(ctypes.byref(s) if s is not None else None, cu, lens, table, q, k, v, 0.1, y, w, ctypes.c_size_t(wb), None)
+    def prefill(s=shape(), lens=FAKE, table=FAKE, q=FAKE, k=FAKE, v=FAKE, y=FAKE, w=FAKE, wb=need_p, cu=FAKE, scale=0.1):
+        return lib.ssd_attn_prefill(ctypes.byref(s) if s is not None else None, cu, lens, table, q, k, v, scale, y, w, ctypes.c_size_t(wb), None)
 
     odd, half = ctypes.c_void_p(4104), ctypes.c_void_p(4098)
     for f, need in ((step, need_s), (prefill, need_p)):
@@ -39,6 +39,7 @@ def test_attention_refuses():
         for name in ("lens", "table", "q", "k", "v", "y"):
             assert f(**{name: None}) == -1, name
             assert f(**{name: half if name in ("lens", "table") else odd}) == -7, name
+        assert f(scale=0.0) == -2 and f(scale=-1.0) == -2 and f(scale=float("nan")) == -2 and f(scale=float("inf")) == -2
         assert f(w=None) == -5 and f(wb=need - 1) == -5 and f(w=ctypes.c_void_p(4096 + 16)) == -5
     assert prefill(cu=None) == -1 and prefill(cu=half) == -7 and prefill(s=shape(tokens=0)) == -2
     assert ssd.attn_step_workspace_bytes(shape(tokens=0)) == need_s   # (the step ignores tokens)
