@@ -375,7 +375,8 @@ SSD_API ssd_status ssd_norm_residual(int64_t rows, int32_t width, int32_t io_dty
  *                       b's are [cu_seqlens[b], cu_seqlens[b+1]), the last ones
  *                       of its seq_lens[b]
  * all of them device arrays, 4-byte aligned.  Query head h reads key head h / (nheads / nkvheads).
- * headdim is a multiple of 8 up to 256, page_size a power of two up to 65536.
+ * headdim is a multiple of 8 up to 256, page_size a power of two up to 65536; a
+ * page (all its key heads) is smaller than 2 GiB.
  * A token sees the tokens of its sequence up to itself; with window > 0 only the
  * last `window` of them.  io dtype is fp32 or bf16; scores, softmax and sums are
  * fp32 (bf16 io: the probabilities are rounded to bf16 for their product with the

@@ -26,6 +26,9 @@ constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that diff
 // The running maximum follows a larger one only when that is 2^kSlack times more: until then probabilities are up to 2^kSlack,
 // which costs no accuracy, and O need not be scaled again.
 constexpr float kSlack = 8.f;
+// bf16 does without looking for the largest score of a step: the sum of a lane's probabilities, which is needed anyway, says
+// whether one is too large for the running maximum.
+constexpr float kMost = 65536.f;
 
 struct PrefillArgs {
   const int32_t *cu, *lens, *table;
@@ -90,6 +93,17 @@ __device__ __forceinline__ u32x2 lds_transposed(const char *p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uint32_t)(uintptr_t)p));
 }
 
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)); }
+// 16 bytes from each lane's address to LDS, in the order of the lanes from `to` (of the wave) on.  An LDS read behind it in the
+// program does not wait for it: that is for the one who reads.
+__device__ __forceinline__ void load_to_lds(const void *from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(to) : "m0", "memory");
+}
+// The same from a lane's offset behind the wave's address.
+__device__ __forceinline__ void load_to_lds(const void *wave_from, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(wave_from), "s"(to) : "m0", "memory");
+}
+
 // Geometry of a tile in LDS for head vectors of up to DP values (D are there, the others are zeros): rows of kPieces pieces of 16
 // bytes, in an order that depends on the row so that the reads of either product go to all banks.
 template <bool kBf16, int DP>
@@ -107,10 +121,304 @@ struct Geometry {
   }
 };
 
+// A row's end: to y, or as a split's part to the workspace.  o: columns 32 c + 8 (r / 4) + 4 h + r % 4 of the row
 template <bool kBf16, int DP>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_kernel(const PrefillArgs a) {
-  using Geo = Geometry<kBf16, DP>;
-  constexpr int kTokens = Geo::kTokens, kHalves = kTokens / 32, kColTiles = DP / 32;
+__device__ __forceinline__ void finish(const PrefillArgs &a, const Unit &unit, int local, int unit_rows, int64_t out_row, int h,
+                                       const f32x16 (&o)[DP / 32], float m, float l) {
+  if (unit.splits == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int col = 32 * c + 2 * r + 4 * h;
+        if (col >= a.d.D) continue;
+        if constexpr (kBf16) {
+          const u32x2 q = {pack2(o[c][r] * inv, o[c][r + 1] * inv), pack2(o[c][r + 2] * inv, o[c][r + 3] * inv)};
+          *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + out_row * a.d.D + col) = q;
+        } else {
+          const f32x4 q = {o[c][r] * inv, o[c][r + 1] * inv, o[c][r + 2] * inv, o[c][r + 3] * inv};
+          *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + out_row * a.d.D + col) = q;
+        }
+      }
+    return;
+  }
+  float *part = a.part + (static_cast<int64_t>(blockIdx.x) * unit_rows + local) * (a.d.D + 4);
+#pragma unroll
+  for (int c = 0; c < DP / 32; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const int col = 32 * c + 2 * r + 4 * h;
+      if (col < a.d.D) *reinterpret_cast<f32x4 *>(part + col) = f32x4{o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
+    }
+  if (h == 0) {
+    part[a.d.D] = m;
+    part[a.d.D + 1] = l;
+  }
+}
+
+// The larger of the two values that lanes l and l + 32 hold, in both.
+__device__ __forceinline__ float both_halves_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// The kernel of bf16.  Step by step, 32 tokens at a time, with a product between each request to LDS and its use: the scores of
+// the next step are computed beside the softmax of this one, and its values read meanwhile; the keys of the step behind that are
+// read before this step's product with the values.  Tiles come to LDS straight from memory, one barrier a tile.  Two workgroups
+// share a CU, two waves a SIMD.
+template <int DP, bool kFull>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kernel(const PrefillArgs a) {
+  using Geo = Geometry<true, DP>;
+  constexpr int kTokens = Geo::kTokens, kColTiles = DP / 32, kFetch = Geo::kFetch;
+  constexpr int kSteps = kTokens / 32;               // of a tile
+  constexpr int kPieces = DP / 16;                   // of a query row, a lane
+  constexpr bool kEarly = DP <= 128;                 // registers are there for reads from LDS ahead of their use
+  constexpr int kPassRows = kThreads / Geo::kPieces; // rows of a tile that the workgroup brings at a time,
+  constexpr int kWaveLoadRows = kPassRows / kWaves;  // and a wave of it
+  constexpr int kKeyTiles = kEarly ? 2 : 3;
+  __shared__ char lds_k[kKeyTiles][Geo::kTileBytes], lds_v[2][Geo::kTileBytes];
+
+  int id = blockIdx.x;
+  const int split = id % a.splits;
+  id /= a.splits;
+  const int hk = id % a.d.Hk;
+  const Unit unit = find_unit<kTokens>(a, a.units - 1 - id / a.d.Hk);  // (the last units see the most tokens)
+  if (unit.rows == 0 || split >= unit.splits) return;
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 31, h = lane / 32;
+  const int bytes = kFull ? DP * 2 : a.d.D * 2;
+  const uint32_t page_bytes = static_cast<uint32_t>(a.d.Hk * bytes) << a.d.lg_page;
+  const int page_mask = (1 << a.d.lg_page) - 1;
+  const int32_t *table = a.table + static_cast<int64_t>(unit.seq) * a.d.max_pages;
+
+  // this lane's row
+  const int local = wave * 32 + n;
+  const bool mine = local < unit.rows;
+  const int row = unit.first_row + min(local, unit.rows - 1), token = quotient(row, a.d.G, a.inv_group);
+  const int pos = unit.pos0 + token, seen_from = a.d.window > 0 ? pos - a.d.window + 1 : 0;
+  const int64_t out_row = static_cast<int64_t>(unit.begin + token) * a.d.H + hk * a.d.G + (row - token * a.d.G);
+  u32x4 query[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int byte = 32 * i + 16 * h;
+    query[i] = u32x4{0u, 0u, 0u, 0u};
+    if (mine && byte < bytes) query[i] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q) + out_row * bytes + byte);
+  }
+  // of the wave: every row sees [all_from, all_to], none sees beyond any_to
+  const int all_to = __builtin_amdgcn_readfirstlane(pos), any_to = __builtin_amdgcn_readlane(pos, 31);
+  const int all_from = __builtin_amdgcn_readlane(seen_from, 31);
+  const bool idle = wave * 32 >= unit.rows;
+
+  const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * split / unit.splits);
+  const int tile1 = static_cast<int>(static_cast<int64_t>(unit.tiles) * (split + 1) / unit.splits);
+  const int end = unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1;  // tokens seen by any row
+
+  // ---- bringing tiles: memory to LDS, a piece a lane; lane t of a wave knows the page of the tile's token t ----
+  const int my_row = threadIdx.x / Geo::kPieces, my_slot = threadIdx.x % Geo::kPieces;
+  const char *const kh = static_cast<const char *>(a.k) + (static_cast<int64_t>(hk) << a.d.lg_page) * bytes;
+  const char *const vh = static_cast<const char *>(a.v) + (static_cast<int64_t>(hk) << a.d.lg_page) * bytes;
+  if (!kFull) {  // the pieces that no row has
+    for (int i = threadIdx.x; i < kKeyTiles * Geo::kTileBytes / 16; i += kThreads) reinterpret_cast<u32x4 *>(lds_k[0])[i] = u32x4{0u, 0u, 0u, 0u};
+    for (int i = threadIdx.x; i < 2 * Geo::kTileBytes / 16; i += kThreads) reinterpret_cast<u32x4 *>(lds_v[0])[i] = u32x4{0u, 0u, 0u, 0u};
+    __syncthreads();
+  }
+  // (for a token behind the last one that is seen: the page of that one)
+  auto page_of = [&](int tile) { return table[min(unit.base + tile * kTokens + lane, end - 1) >> a.d.lg_page]; };
+  // where a wave's loads of a tile begin in either cache, if they are on one page each
+  struct Where {
+    uint64_t at[kFetch];
+  };
+  auto where_of = [&](int tile, int page) {
+    Where w;
+    const int tile_first = unit.base + tile * kTokens;
+    const int there = static_cast<unsigned>(page) < static_cast<unsigned>(a.d.npages) ? page : 0;
+#pragma unroll
+    for (int i = 0; i < kFetch; ++i) {
+      const int at = wave * kWaveLoadRows + i * kPassRows;
+      w.at[i] = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(there, at))) * page_bytes +
+                static_cast<uint32_t>(((tile_first + at) & page_mask) * bytes);
+    }
+    return w;
+  };
+  const bool one_page = page_mask >= kWaveLoadRows - 1;
+  auto bring = [&](char *to, const char *head, const Where &w, int tile, int page, bool keys) {
+    const uint32_t to_wave = __builtin_amdgcn_readfirstlane(lds_address(to)) + wave * 1024;
+    if (one_page) {
+#pragma unroll
+      for (int i = 0; i < kFetch; ++i) {
+        const int row = my_row + (kPassRows % 16 == 0 ? 0 : i * kPassRows);
+        const int piece = keys ? Geo::key_piece(row, my_slot) : Geo::value_piece(row, my_slot);
+        if (kFull || 16 * piece < bytes)
+          load_to_lds(head + w.at[i], static_cast<uint32_t>((lane / Geo::kPieces) * bytes + 16 * piece), to_wave + i * kThreads * 16);
+      }
+      return;
+    }
+    const int there = static_cast<unsigned>(page) < static_cast<unsigned>(a.d.npages) ? page : 0;
+#pragma unroll
+    for (int i = 0; i < kFetch; ++i) {
+      const uint32_t where = __shfl(there, my_row + i * kPassRows);
+      const int row = my_row + i * kPassRows, piece = keys ? Geo::key_piece(row, my_slot) : Geo::value_piece(row, my_slot);
+      const uint32_t in_page = ((unit.base + tile * kTokens + row) & page_mask) * bytes + 16 * piece;
+      if (kFull || 16 * piece < bytes) load_to_lds(head + (static_cast<uint64_t>(where) * page_bytes + in_page), to_wave + i * kThreads * 16);
+    }
+  };
+  // tokens of a tile that are seen by no row: behind the last one, or of a page that is not in the cache
+  auto gone_of = [&](int tile, int page) {
+    const int first = unit.base + tile * kTokens;
+    return __ballot(static_cast<unsigned>(page) >= static_cast<unsigned>(a.d.npages) || first + lane >= end);
+  };
+  // (their probability is zero, and so must be its product: once the values are there, zeros take their place)
+  auto arrived = [&](char *values, uint64_t gone) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (gone != 0) {
+#pragma unroll
+      for (int i = 0; i < kFetch; ++i)
+        if ((gone >> (my_row + i * kPassRows)) & 1) *reinterpret_cast<u32x4 *>(values + 16 * threadIdx.x + i * kThreads * 16) = u32x4{0u, 0u, 0u, 0u};
+    }
+    __syncthreads();
+  };
+
+  f32x16 o[kColTiles];
+  float m = kNone, l = 0.f;
+#pragma unroll
+  for (int c = 0; c < kColTiles; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[c][r] = 0.f;
+  // addresses in a tile
+  const int k_row = n * Geo::kRowBytes;
+  const int v_row = (lane & 15) / 4, v_byte = 32 * ((lane >> 4) & 1) + 8 * (lane & 3);  // (8 bytes of a 64-byte column tile)
+  u32x4 keys[kPieces];  // of the step whose scores come next
+  auto read_keys = [&](const char *tile, int step) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      keys[i] = *reinterpret_cast<const u32x4 *>(tile + 32 * step * Geo::kRowBytes + k_row + 16 * Geo::key_piece(n, 2 * i + h));
+  };
+  auto scores = [&](const char *tile, int step) {
+    f32x16 to;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) to[r] = 0.f;
+    if (!kEarly) read_keys(tile, step);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) to = mfma_bf16(keys[i], query[i], to);
+    return to;
+  };
+
+  // The keys of a step are read two steps ahead, those of the tile in work with the one before it: in LDS are, of the tile in
+  // work, its values, and of the next one the keys.
+  uint64_t gone[3] = {0, 0, 0};       // of the tile in work and the next two
+  int page_k = 0;                     // of the tile whose keys are asked for next
+  Where where_v = {};                 // of the tile whose values are asked for next
+  if (tile0 < tile1) {
+    const int p0 = page_of(tile0), p1 = page_of(tile0 + 1);
+    page_k = page_of(tile0 + 2);
+    gone[0] = gone_of(tile0, p0);
+    gone[1] = gone_of(tile0 + 1, p1);
+    const Where w0 = where_of(tile0, p0);
+    where_v = where_of(tile0 + 1, p1);
+    bring(lds_k[0], kh, w0, tile0, p0, true);
+    bring(lds_v[0], vh, w0, tile0, p0, false);
+    bring(lds_k[1], kh, where_v, tile0 + 1, p1, true);
+  }
+  int page_v = page_of(tile0 + 1);
+  arrived(lds_v[0], gone[0]);
+  if (kEarly) read_keys(lds_k[0], 0);
+  f32x16 s = scores(lds_k[0], 0);
+  if (kEarly) read_keys(lds_k[0], 1);
+  __syncthreads();
+  int at_k = 0;
+  const auto wrap = [](int i) { return i >= kKeyTiles ? i - kKeyTiles : i; };
+  for (int tile = tile0; tile < tile1; ++tile) {
+    const int first = unit.base + tile * kTokens, odd = (tile - tile0) & 1;
+    char *const kt = lds_k[at_k], *const kt1 = lds_k[wrap(at_k + 1)], *const kt2 = lds_k[wrap(at_k + 2)];
+    char *const vt = lds_v[odd], *const vt1 = lds_v[odd ^ 1];
+    // (tiles behind the last one repeat its last token: they are brought and not used)
+    const Where where_k = where_of(tile + 2, page_k);
+    bring(vt1, vh, where_v, tile + 1, page_v, false);
+    bring(kt2, kh, where_k, tile + 2, page_k, true);
+    gone[2] = gone_of(tile + 2, page_k);
+    where_v = where_k;
+    page_v = page_k;
+    page_k = page_of(tile + 3);
+    if (!idle && first <= any_to) {
+#pragma unroll
+      for (int step = 0; step < kSteps; ++step) {
+        if (first + 32 * step + 31 > all_to || first + 32 * step < all_from || gone[0] != 0) {
+          asm volatile("" ::: "memory");  // (nothing of this is computed where the branch isn't taken)
+          const uint32_t out = static_cast<uint32_t>(gone[0] >> (32 * step)) >> (4 * h);
+          const int to = pos - (first + 32 * step + 4 * h), from = seen_from - (first + 32 * step + 4 * h);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int t = 8 * (r / 4) + r % 4;
+            if (t > to || t < from || (out & (1u << t))) s[r] = -INFINITY;
+          }
+        }
+        u32x4 p[2];
+        float sum;
+        auto exponentials = [&] {
+          sum = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[r + 1], a.scale_log2, -m));
+            sum += x;
+            sum += y;
+            p[r / 8][r / 2 % 4] = pack2(x, y);
+          }
+        };
+        // the values of the step, by groups of 16 tokens and 32 columns
+        const char *const v_lane = vt + (32 * step + 4 * h + v_row) * Geo::kRowBytes;
+        auto read_values = [&](int g, int c) {
+          const char *const v_at = v_lane + 16 * g * Geo::kRowBytes + 16 * Geo::value_piece(v_row, 4 * c + v_byte / 16) + v_byte % 16;
+          const u32x2 lo = lds_transposed(v_at), hi = lds_transposed(v_at + 8 * Geo::kRowBytes);
+          return u32x4{lo[0], lo[1], hi[0], hi[1]};
+        };
+        u32x4 values[2][kEarly ? kColTiles : 1];
+        if (kEarly)
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int c = 0; c < kColTiles; ++c) values[g][kEarly ? c : 0] = read_values(g, c);
+        __builtin_amdgcn_s_setprio(1);
+        const f32x16 next = scores(step + 1 < kSteps ? kt : kt1, step + 1 < kSteps ? step + 1 : 0);
+        exponentials();
+        __builtin_amdgcn_s_setprio(0);
+        if (__any(!(sum <= kMost))) {
+          asm volatile("" ::: "memory");
+          float top = s[0];
+#pragma unroll
+          for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+          const float larger = fmaxf(m, both_halves_max(top) * a.scale_log2), keep = __builtin_amdgcn_exp2f(m - larger);
+          m = larger;
+          l *= keep;
+#pragma unroll
+          for (int c = 0; c < kColTiles; ++c)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[c][r] *= keep;
+          exponentials();
+        }
+        l += sum;
+        if (kEarly) read_keys(kt1, step);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int c = 0; c < kColTiles; ++c) o[c] = mfma_bf16(kEarly ? values[g][kEarly ? c : 0] : read_values(g, c), p[g], o[c]);
+        s = next;
+      }
+    }
+    gone[0] = gone[1];
+    gone[1] = gone[2];
+    at_k = wrap(at_k + 1);
+    arrived(vt1, gone[0]);
+  }
+  l += __shfl_xor(l, 32);
+  if (mine) finish<true, DP>(a, unit, local, kUnitRows, out_row, h, o, m, l);
+}
+
+// The kernel of fp32: the matrix pipe's rate there is 16 times less, and nothing else is near it.
+template <int DP>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_f32_kernel(const PrefillArgs a) {
+  using Geo = Geometry<false, DP>;
+  constexpr int kTokens = Geo::kTokens, kColTiles = DP / 32;
   constexpr int kQueryPieces = DP * Geo::kSize / 32;  // of 16 bytes, a lane
   __shared__ char lds[2][2][Geo::kTileBytes];         // two tiles of K and V
 
@@ -166,7 +474,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_kernel(co
     const int t = min(first + (lane & (kTokens - 1)), end - 1);
     int page = table[t >> a.d.lg_page];
     const bool bad = static_cast<unsigned>(page) >= static_cast<unsigned>(a.d.npages);
-    gone_next = __ballot(bad) & (kTokens == 64 ? ~0ull : (1ull << kTokens) - 1);
+    gone_next = __ballot(bad) & ((1ull << kTokens) - 1);
     if (bad) page = -1;
 #pragma unroll
     for (int i = 0; i < Geo::kFetch; ++i) {
@@ -203,38 +511,29 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_kernel(co
     const uint64_t gone_now = gone;
     if (tile + 1 < tile1) fetch(tile + 1);
     if (!idle && first <= any_to) {
-      f32x16 s[kHalves];
+      f32x16 s;
 #pragma unroll
-      for (int t = 0; t < kHalves; ++t) {
+      for (int r = 0; r < 16; ++r) s[r] = 0.f;
+      const char *krow = kt + n * Geo::kRowBytes;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
-        const char *krow = kt + (32 * t + n) * Geo::kRowBytes;
+      for (int i = 0; i < kQueryPieces; ++i) {
+        const u32x4 k = *reinterpret_cast<const u32x4 *>(krow + 16 * Geo::key_piece(n, 2 * i + h));
 #pragma unroll
-        for (int i = 0; i < kQueryPieces; ++i) {
-          const u32x4 k = *reinterpret_cast<const u32x4 *>(krow + 16 * Geo::key_piece(n, 2 * i + h));
-          if constexpr (kBf16) {
-            s[t] = mfma_bf16(k, query[i], s[t]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[t] = mfma_f32(__uint_as_float(k[e]), __uint_as_float(query[i][e]), s[t]);
-          }
-        }
+        for (int e = 0; e < 4; ++e) s = mfma_f32(__uint_as_float(k[e]), __uint_as_float(query[i][e]), s);
       }
       if (first + kTokens - 1 > all_to || first < all_from || gone_now != 0) {
+        const uint32_t out = static_cast<uint32_t>(gone_now) >> (4 * h);
+        const int to = pos - (first + 4 * h), from = seen_from - (first + 4 * h);
 #pragma unroll
-        for (int t = 0; t < kHalves; ++t)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int in_tile = 32 * t + 8 * (r / 4) + 4 * h + r % 4, at = first + in_tile;
-            if (at > pos || at < seen_from || ((gone_now >> in_tile) & 1)) s[t][r] = -INFINITY;
-          }
+        for (int r = 0; r < 16; ++r) {
+          const int t = 8 * (r / 4) + r % 4;
+          if (t > to || t < from || (out & (1u << t))) s[r] = -INFINITY;
+        }
       }
-      float top = s[0][0];
+      float top = s[0];
 #pragma unroll
-      for (int t = 0; t < kHalves; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-      top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+      top = both_halves_max(top) * a.scale_log2;
       if (__any(top > m + kSlack)) {
         const float next = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(m - next);
         m = next;
@@ -245,35 +544,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_kernel(co
           for (int r = 0; r < 16; ++r) o[c][r] *= keep;
       }
 #pragma unroll
-      for (int t = 0; t < kHalves; ++t)
+      for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -m));
+        l += s[r];
+      }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], a.scale_log2, -m));
-          l += s[t][r];
-        }
-      if constexpr (kBf16) {
-        const char *vlane = vt + (4 * h + (lane & 15) / 4) * Geo::kRowBytes;
-        const int byte = 32 * ((lane >> 4) & 1) + 8 * (lane & 3), vrow = (lane & 15) / 4;  // (4 h and multiples of 8 rows leave row & 3)
+      for (int r = 0; r < 16; ++r) {
+        const float *vrow = reinterpret_cast<const float *>(vt + (8 * (r / 4) + 4 * h + r % 4) * Geo::kRowBytes);
 #pragma unroll
-        for (int g = 0; g < 2 * kHalves; ++g) {  // 16 tokens
-          u32x4 p;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = pack2(s[g / 2][8 * (g % 2) + 2 * i], s[g / 2][8 * (g % 2) + 2 * i + 1]);
-#pragma unroll
-          for (int c = 0; c < kColTiles; ++c) {
-            const int piece = Geo::value_piece(vrow, 4 * c + byte / 16);
-            const u32x2 lo = lds_transposed(vlane + 16 * g * Geo::kRowBytes + 16 * piece + byte % 16);
-            const u32x2 hi = lds_transposed(vlane + (16 * g + 8) * Geo::kRowBytes + 16 * piece + byte % 16);
-            o[c] = mfma_bf16(u32x4{lo[0], lo[1], hi[0], hi[1]}, p, o[c]);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float *vrow = reinterpret_cast<const float *>(vt + (8 * (r / 4) + 4 * h + r % 4) * Geo::kRowBytes);
-#pragma unroll
-          for (int c = 0; c < kColTiles; ++c) o[c] = mfma_f32(vrow[32 * c + n], s[0][r], o[c]);
-        }
+        for (int c = 0; c < kColTiles; ++c) o[c] = mfma_f32(vrow[32 * c + n], s[r], o[c]);
       }
     }
     if (tile + 1 < tile1) stage(buffer ^ 1);
@@ -281,37 +560,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_kernel(co
   }
 
   l += __shfl_xor(l, 32);
-  if (!mine) return;
-  if (unit.splits == 1) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int c = 0; c < kColTiles; ++c)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const int col = 32 * c + 2 * r + 4 * h;
-        if (col >= a.d.D) continue;
-        if constexpr (kBf16) {
-          const u32x2 q = {pack2(o[c][r] * inv, o[c][r + 1] * inv), pack2(o[c][r + 2] * inv, o[c][r + 3] * inv)};
-          *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + out_row * a.d.D + col) = q;
-        } else {
-          const f32x4 q = {o[c][r] * inv, o[c][r + 1] * inv, o[c][r + 2] * inv, o[c][r + 3] * inv};
-          *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + out_row * a.d.D + col) = q;
-        }
-      }
-  } else {
-    float *part = a.part + (static_cast<int64_t>(blockIdx.x) * kUnitRows + local) * (a.d.D + 4);
-#pragma unroll
-    for (int c = 0; c < kColTiles; ++c)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const int col = 32 * c + 2 * r + 4 * h;
-        if (col < a.d.D) *reinterpret_cast<f32x4 *>(part + col) = f32x4{o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
-      }
-    if (h == 0) {
-      part[a.d.D] = m;
-      part[a.d.D + 1] = l;
-    }
-  }
+  if (mine) finish<false, DP>(a, unit, local, kUnitRows, out_row, h, o, m, l);
 }
 
 // Joins the splits of a unit: one workgroup for kJoinRows of its rows.
@@ -368,17 +617,37 @@ Plan plan_of(const AttnDims &d) {
   return p;
 }
 
-template <bool kBf16>
+template <int DP>
+void launch_bf16(const PrefillArgs &a, dim3 grid, hipStream_t stream) {
+  if (a.d.D == DP)
+    hipLaunchKernelGGL((prefill_bf16_kernel<DP, true>), grid, dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((prefill_bf16_kernel<DP, false>), grid, dim3(kThreads), 0, stream, a);
+}
+
 hipError_t launch(const PrefillArgs &a, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(a.units) * a.d.Hk * a.splits), threads(kThreads);
-  if (a.d.D <= 64)
-    hipLaunchKernelGGL((prefill_kernel<kBf16, 64>), grid, threads, 0, stream, a);
-  else if (a.d.D <= 128)
-    hipLaunchKernelGGL((prefill_kernel<kBf16, 128>), grid, threads, 0, stream, a);
-  else
-    hipLaunchKernelGGL((prefill_kernel<kBf16, 256>), grid, threads, 0, stream, a);
+  if (a.d.bf16) {
+    if (a.d.D > 128)
+      launch_bf16<256>(a, grid, stream);
+    else if (a.d.D > 64)
+      launch_bf16<128>(a, grid, stream);
+    else
+      launch_bf16<64>(a, grid, stream);
+  } else {
+    if (a.d.D > 128)
+      hipLaunchKernelGGL(prefill_f32_kernel<256>, grid, threads, 0, stream, a);
+    else if (a.d.D > 64)
+      hipLaunchKernelGGL(prefill_f32_kernel<128>, grid, threads, 0, stream, a);
+    else
+      hipLaunchKernelGGL(prefill_f32_kernel<64>, grid, threads, 0, stream, a);
+  }
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-  hipLaunchKernelGGL(prefill_join_kernel<kBf16>, dim3(static_cast<unsigned>(a.units) * a.d.Hk * (kUnitRows / kJoinRows)), threads, 0, stream, a);
+  const dim3 joins(static_cast<unsigned>(a.units) * a.d.Hk * (kUnitRows / kJoinRows));
+  if (a.d.bf16)
+    hipLaunchKernelGGL(prefill_join_kernel<true>, joins, threads, 0, stream, a);
+  else
+    hipLaunchKernelGGL(prefill_join_kernel<false>, joins, threads, 0, stream, a);
   return hipGetLastError();
 }
 
@@ -408,7 +677,7 @@ hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32
   a.units = p.units;
   a.splits = p.splits;
   a.scale_log2 = scale * 1.44269504f;
-  return d.bf16 ? launch<true>(a, stream) : launch<false>(a, stream);
+  return launch(a, stream);
 }
 
 }  // namespace ssd

@@ -46,6 +46,8 @@ ssd_status make_dims(const ssd_attn_shape *s, bool packed, AttnDims *out) {
   if (static_cast<long double>(d.npages) * d.Hk * s->page_size * d.D > 1.0e15L || d.T > (1 << 30) || d.B > (1 << 30) ||
       static_cast<long double>(d.T) * d.H > 2147483647.0L || static_cast<long double>(d.B) * d.H > 2147483647.0L)
     return SSD_ERR_SHAPE;
+  // a page of the cache is addressed with 32 bits
+  if (static_cast<long double>(d.Hk) * s->page_size * d.D * (d.bf16 ? 2 : 4) > 2147483647.0L) return SSD_ERR_UNSUPPORTED;
   *out = d;
   return SSD_OK;
 }
