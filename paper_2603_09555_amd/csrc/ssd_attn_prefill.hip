@@ -12,6 +12,9 @@
 // operand of V^T P^T, whose first operand comes from LDS with the same order of tokens (bf16: by transposing reads).
 //
 // Where there are few units, several workgroups share one's tokens and leave (m, l, O) in the workspace for a second launch.
+#include <algorithm>
+#include <cmath>
+
 #include "ssd_attn.hpp"
 
 namespace ssd {
@@ -20,8 +23,11 @@ namespace {
 using namespace block;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kWaveRows = 32, kUnitRows = kWaves * kWaveRows;
-constexpr int kSplitTiles = 8;     // tiles a workgroup has at least when a unit is shared
-constexpr int kWantedUnits = 512;  // workgroups that fill the GPU
+constexpr int kSplitTokens = 512; // a unit is shared by no more workgroups than it has times that
+constexpr int kWorkgroups = 256;  // of eight waves, which fill the GPU
+constexpr int kManyUnits = 768;   // units that four waves each take,
+constexpr int kManyTiles = 16;    // unless they have fewer tiles
+constexpr int kMostSplits = 64;   // of a unit
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
 // The running maximum follows a larger one only when that is 2^kSlack times more: until then probabilities are up to 2^kSlack,
 // which costs no accuracy, and O need not be scaled again.
@@ -34,11 +40,12 @@ struct PrefillArgs {
   const int32_t *cu, *lens, *table;
   const void *q, *k, *v;
   void *y;
-  float *part;       // per unit and split: kUnitRows x (D + 4): O, m, l
+  void *part;        // for each unit and split
   AttnDims d;
   uint32_t inv_group;
   int units;         // at most, of a key head
   int splits;        // at most, of a unit
+  int groups;        // of waves, a workgroup
   float scale_log2;  // scale * log2(e)
 };
 
@@ -76,7 +83,7 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int u) {
   const int highest = r.pos0 + quotient(r.first_row + r.rows - 1, a.d.G, a.inv_group);
   r.base = (a.d.window > 0 ? max(0, lowest + 1 - a.d.window) : 0) & ~(kTokens - 1);
   r.tiles = highest < 0 ? 0 : (highest + 1 - r.base + kTokens - 1) / kTokens;
-  r.splits = max(1, min(a.splits, r.tiles / kSplitTiles));
+  r.splits = max(1, min(a.splits, (r.tiles * kTokens + kSplitTokens - 1) / kSplitTokens));
   return r;
 }
 
@@ -106,10 +113,11 @@ __device__ __forceinline__ void load_to_lds(const void *wave_from, uint32_t offs
 
 // Geometry of a tile in LDS for head vectors of up to DP values (D are there, the others are zeros): rows of kPieces pieces of 16
 // bytes, in an order that depends on the row so that the reads of either product go to all banks.
+constexpr int tokens_of_tile(bool bf16) { return bf16 ? 64 : 32; }
 template <bool kBf16, int DP>
 struct Geometry {
   static constexpr int kSize = kBf16 ? 2 : 4;
-  static constexpr int kTokens = kBf16 ? 64 : 32;
+  static constexpr int kTokens = tokens_of_tile(kBf16);
   static constexpr int kRowBytes = DP * kSize, kPieces = kRowBytes / 16;
   static constexpr int kTileBytes = kTokens * kRowBytes;
   static constexpr int kFetch = kTokens * kPieces / kThreads;  // pieces of a tile a thread brings
@@ -121,40 +129,72 @@ struct Geometry {
   }
 };
 
-// A row's end: to y, or as a split's part to the workspace.  o: columns 32 c + 8 (r / 4) + 4 h + r % 4 of the row
+// A part of a unit as its four waves hold it, lane by lane: the pieces of O^T, four columns of the lane's row each, then m and l.
+template <int DP>
+struct Part {
+  static constexpr int kPieces = DP / 8;
+  f32x4 o[kWaves][kPieces][64];
+  float m[kWaves][64], l[kWaves][64];
+};
+
+// Four columns of a row, of O / l, to y.
+template <bool kBf16>
+__device__ __forceinline__ void write_row(const PrefillArgs &a, int64_t out_row, int col, f32x4 o, float inv) {
+  if (col >= a.d.D) return;
+  if constexpr (kBf16) {
+    const u32x2 q = {pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
+    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + out_row * a.d.D + col) = q;
+  } else {
+    const f32x4 q = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + out_row * a.d.D + col) = q;
+  }
+}
+// Piece i of a lane: columns 8 i + 4 h on of its row (o: columns 32 c + 8 (r / 4) + 4 h + r % 4).
+__device__ __forceinline__ int piece_column(int i, int h) { return 8 * i + 4 * h; }
+
+// A wave's rows' end: to y, or as a part to the workspace.
 template <bool kBf16, int DP>
-__device__ __forceinline__ void finish(const PrefillArgs &a, const Unit &unit, int local, int unit_rows, int64_t out_row, int h,
-                                       const f32x16 (&o)[DP / 32], float m, float l) {
-  if (unit.splits == 1) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+__device__ __forceinline__ void finish(const PrefillArgs &a, bool whole, int slot, bool mine, int wave, int64_t out_row, const f32x16 (&o)[DP / 32],
+                                       float m, float l) {
+  const int lane = threadIdx.x & 63, h = lane / 32;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  Part<DP> *const part = static_cast<Part<DP> *>(a.part) + slot;
 #pragma unroll
-    for (int c = 0; c < DP / 32; ++c)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const int col = 32 * c + 2 * r + 4 * h;
-        if (col >= a.d.D) continue;
-        if constexpr (kBf16) {
-          const u32x2 q = {pack2(o[c][r] * inv, o[c][r + 1] * inv), pack2(o[c][r + 2] * inv, o[c][r + 3] * inv)};
-          *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + out_row * a.d.D + col) = q;
-        } else {
-          const f32x4 q = {o[c][r] * inv, o[c][r + 1] * inv, o[c][r + 2] * inv, o[c][r + 3] * inv};
-          *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + out_row * a.d.D + col) = q;
-        }
-      }
-    return;
+  for (int i = 0; i < Part<DP>::kPieces; ++i) {
+    const f32x4 q = {o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+    if (!whole) part->o[wave][i][lane] = q;
+    else if (mine) write_row<kBf16>(a, out_row, piece_column(i, h), q, inv);
   }
-  float *part = a.part + (static_cast<int64_t>(blockIdx.x) * unit_rows + local) * (a.d.D + 4);
-#pragma unroll
-  for (int c = 0; c < DP / 32; ++c)
-#pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      const int col = 32 * c + 2 * r + 4 * h;
-      if (col < a.d.D) *reinterpret_cast<f32x4 *>(part + col) = f32x4{o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
-    }
-  if (h == 0) {
-    part[a.d.D] = m;
-    part[a.d.D + 1] = l;
+  if (!whole) {
+    part->m[wave][lane] = m;
+    part->l[wave][lane] = l;
   }
+}
+
+// A workgroup may have two groups of four waves, each with every second tile of a unit.  Joins the second one's results to the
+// first one's; false for the second group, which is done then.
+template <int DP>
+__device__ __forceinline__ bool join_groups(Part<DP> &part, int group, int wave, f32x16 (&o)[DP / 32], float &m, float &l) {
+  const int lane = threadIdx.x & 63;
+  if (group == 1) {
+#pragma unroll
+    for (int i = 0; i < Part<DP>::kPieces; ++i)
+      part.o[wave][i][lane] = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+    part.m[wave][lane] = m;
+    part.l[wave][lane] = l;
+  }
+  __syncthreads();
+  if (group == 1) return false;
+  const float other = part.m[wave][lane], top = fmaxf(m, other), keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(other - top);
+  m = top;
+  l = fmaf(l, keep, part.l[wave][lane] * f);
+#pragma unroll
+  for (int i = 0; i < Part<DP>::kPieces; ++i) {
+    const f32x4 q = part.o[wave][i][lane];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[i / 4][4 * (i % 4) + r] = fmaf(o[i / 4][4 * (i % 4) + r], keep, q[r] * f);
+  }
+  return true;
 }
 
 // The larger of the two values that lanes l and l + 32 hold, in both.
@@ -167,8 +207,8 @@ __device__ __forceinline__ float both_halves_max(float v) {
 // the next step are computed beside the softmax of this one, and its values read meanwhile; the keys of the step behind that are
 // read before this step's product with the values.  Tiles come to LDS straight from memory, one barrier a tile.  Two workgroups
 // share a CU, two waves a SIMD.
-template <int DP, bool kFull>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kernel(const PrefillArgs a) {
+template <int DP, bool kFull, int kGroups>
+__global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill_bf16_kernel(const PrefillArgs a) {
   using Geo = Geometry<true, DP>;
   constexpr int kTokens = Geo::kTokens, kColTiles = DP / 32, kFetch = Geo::kFetch;
   constexpr int kSteps = kTokens / 32;               // of a tile
@@ -177,7 +217,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kern
   constexpr int kPassRows = kThreads / Geo::kPieces; // rows of a tile that the workgroup brings at a time,
   constexpr int kWaveLoadRows = kPassRows / kWaves;  // and a wave of it
   constexpr int kKeyTiles = kEarly ? 2 : 3;
-  __shared__ char lds_k[kKeyTiles][Geo::kTileBytes], lds_v[2][Geo::kTileBytes];
+  __shared__ __align__(16) char lds[kGroups][kKeyTiles + 2][Geo::kTileBytes];
+  static_assert(kGroups == 1 || sizeof(Part<DP>) <= sizeof(lds));
 
   int id = blockIdx.x;
   const int split = id % a.splits;
@@ -186,7 +227,10 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kern
   const Unit unit = find_unit<kTokens>(a, a.units - 1 - id / a.d.Hk);  // (the last units see the most tokens)
   if (unit.rows == 0 || split >= unit.splits) return;
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane & 31, h = lane / 32;
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % kWaves, group = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / kWaves;
+  const int thread = 64 * wave + lane;  // of the group
+  char (*const lds_k)[Geo::kTileBytes] = lds[group], (*const lds_v)[Geo::kTileBytes] = lds[group] + kKeyTiles;
   const int bytes = kFull ? DP * 2 : a.d.D * 2;
   const uint32_t page_bytes = static_cast<uint32_t>(a.d.Hk * bytes) << a.d.lg_page;
   const int page_mask = (1 << a.d.lg_page) - 1;
@@ -210,17 +254,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kern
   const int all_from = __builtin_amdgcn_readlane(seen_from, 31);
   const bool idle = wave * 32 >= unit.rows;
 
-  const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * split / unit.splits);
+  // the split's tiles, of which the group takes every kGroups-th
   const int tile1 = static_cast<int>(static_cast<int64_t>(unit.tiles) * (split + 1) / unit.splits);
+  const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * split / unit.splits) + group;
+  const int rounds = (tile1 - (tile0 - group) + kGroups - 1) / kGroups;
   const int end = unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1;  // tokens seen by any row
 
   // ---- bringing tiles: memory to LDS, a piece a lane; lane t of a wave knows the page of the tile's token t ----
-  const int my_row = threadIdx.x / Geo::kPieces, my_slot = threadIdx.x % Geo::kPieces;
+  const int my_row = thread / Geo::kPieces, my_slot = thread % Geo::kPieces;
   const char *const kh = static_cast<const char *>(a.k) + (static_cast<int64_t>(hk) << a.d.lg_page) * bytes;
   const char *const vh = static_cast<const char *>(a.v) + (static_cast<int64_t>(hk) << a.d.lg_page) * bytes;
   if (!kFull) {  // the pieces that no row has
-    for (int i = threadIdx.x; i < kKeyTiles * Geo::kTileBytes / 16; i += kThreads) reinterpret_cast<u32x4 *>(lds_k[0])[i] = u32x4{0u, 0u, 0u, 0u};
-    for (int i = threadIdx.x; i < 2 * Geo::kTileBytes / 16; i += kThreads) reinterpret_cast<u32x4 *>(lds_v[0])[i] = u32x4{0u, 0u, 0u, 0u};
+    for (int i = thread; i < (kKeyTiles + 2) * Geo::kTileBytes / 16; i += kThreads) reinterpret_cast<u32x4 *>(lds[group])[i] = u32x4{0u, 0u, 0u, 0u};
     __syncthreads();
   }
   // (for a token behind the last one that is seen: the page of that one)
@@ -266,7 +311,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kern
   // tokens of a tile that are seen by no row: behind the last one, or of a page that is not in the cache
   auto gone_of = [&](int tile, int page) {
     const int first = unit.base + tile * kTokens;
-    return __ballot(static_cast<unsigned>(page) >= static_cast<unsigned>(a.d.npages) || first + lane >= end);
+    return __ballot(lane < kTokens && (static_cast<unsigned>(page) >= static_cast<unsigned>(a.d.npages) || first + lane >= end));
   };
   // (their probability is zero, and so must be its product: once the values are there, zeros take their place)
   auto arrived = [&](char *values, uint64_t gone) {
@@ -274,7 +319,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kern
     if (gone != 0) {
 #pragma unroll
       for (int i = 0; i < kFetch; ++i)
-        if ((gone >> (my_row + i * kPassRows)) & 1) *reinterpret_cast<u32x4 *>(values + 16 * threadIdx.x + i * kThreads * 16) = u32x4{0u, 0u, 0u, 0u};
+        if ((gone >> (my_row + i * kPassRows)) & 1) *reinterpret_cast<u32x4 *>(values + 16 * thread + i * kThreads * 16) = u32x4{0u, 0u, 0u, 0u};
     }
     __syncthreads();
   };
@@ -309,18 +354,19 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kern
   uint64_t gone[3] = {0, 0, 0};       // of the tile in work and the next two
   int page_k = 0;                     // of the tile whose keys are asked for next
   Where where_v = {};                 // of the tile whose values are asked for next
-  if (tile0 < tile1) {
-    const int p0 = page_of(tile0), p1 = page_of(tile0 + 1);
-    page_k = page_of(tile0 + 2);
+  int page_v = 0;
+  if (rounds > 0) {
+    const int p0 = page_of(tile0), p1 = page_of(tile0 + kGroups);
+    page_v = p1;
+    page_k = page_of(tile0 + 2 * kGroups);
     gone[0] = gone_of(tile0, p0);
-    gone[1] = gone_of(tile0 + 1, p1);
+    gone[1] = gone_of(tile0 + kGroups, p1);
     const Where w0 = where_of(tile0, p0);
-    where_v = where_of(tile0 + 1, p1);
+    where_v = where_of(tile0 + kGroups, p1);
     bring(lds_k[0], kh, w0, tile0, p0, true);
     bring(lds_v[0], vh, w0, tile0, p0, false);
-    bring(lds_k[1], kh, where_v, tile0 + 1, p1, true);
+    bring(lds_k[1], kh, where_v, tile0 + kGroups, p1, true);
   }
-  int page_v = page_of(tile0 + 1);
   arrived(lds_v[0], gone[0]);
   if (kEarly) read_keys(lds_k[0], 0);
   f32x16 s = scores(lds_k[0], 0);
@@ -328,19 +374,20 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kern
   __syncthreads();
   int at_k = 0;
   const auto wrap = [](int i) { return i >= kKeyTiles ? i - kKeyTiles : i; };
-  for (int tile = tile0; tile < tile1; ++tile) {
-    const int first = unit.base + tile * kTokens, odd = (tile - tile0) & 1;
+  for (int round = 0; round < rounds; ++round) {
+    const int tile = tile0 + kGroups * round;
+    const int first = unit.base + tile * kTokens, odd = round & 1;
     char *const kt = lds_k[at_k], *const kt1 = lds_k[wrap(at_k + 1)], *const kt2 = lds_k[wrap(at_k + 2)];
     char *const vt = lds_v[odd], *const vt1 = lds_v[odd ^ 1];
     // (tiles behind the last one repeat its last token: they are brought and not used)
-    const Where where_k = where_of(tile + 2, page_k);
-    bring(vt1, vh, where_v, tile + 1, page_v, false);
-    bring(kt2, kh, where_k, tile + 2, page_k, true);
-    gone[2] = gone_of(tile + 2, page_k);
+    const Where where_k = where_of(tile + 2 * kGroups, page_k);
+    bring(vt1, vh, where_v, tile + kGroups, page_v, false);
+    bring(kt2, kh, where_k, tile + 2 * kGroups, page_k, true);
+    gone[2] = gone_of(tile + 2 * kGroups, page_k);
     where_v = where_k;
     page_v = page_k;
-    page_k = page_of(tile + 3);
-    if (!idle && first <= any_to) {
+    page_k = page_of(tile + 3 * kGroups);
+    if (!idle && tile < tile1 && first <= any_to) {
 #pragma unroll
       for (int step = 0; step < kSteps; ++step) {
         if (first + 32 * step + 31 > all_to || first + 32 * step < all_from || gone[0] != 0) {
@@ -411,16 +458,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_bf16_kern
     arrived(vt1, gone[0]);
   }
   l += __shfl_xor(l, 32);
-  if (mine) finish<true, DP>(a, unit, local, kUnitRows, out_row, h, o, m, l);
+  if (kGroups == 2 && !join_groups<DP>(*reinterpret_cast<Part<DP> *>(lds), group, wave, o, m, l)) return;
+  finish<true, DP>(a, unit.splits == 1, blockIdx.x, mine, wave, out_row, o, m, l);
 }
 
 // The kernel of fp32: the matrix pipe's rate there is 16 times less, and nothing else is near it.
-template <int DP>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_f32_kernel(const PrefillArgs a) {
+template <int DP, int kGroups>
+__global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill_f32_kernel(const PrefillArgs a) {
   using Geo = Geometry<false, DP>;
   constexpr int kTokens = Geo::kTokens, kColTiles = DP / 32;
   constexpr int kQueryPieces = DP * Geo::kSize / 32;  // of 16 bytes, a lane
-  __shared__ char lds[2][2][Geo::kTileBytes];         // two tiles of K and V
+  __shared__ __align__(16) char all_lds[kGroups][2][2][Geo::kTileBytes];  // two tiles of K and V
+  static_assert(kGroups == 1 || sizeof(Part<DP>) <= sizeof(all_lds));
 
   int id = blockIdx.x;
   const int split = id % a.splits;
@@ -429,7 +478,10 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_f32_kerne
   const Unit unit = find_unit<kTokens>(a, a.units - 1 - id / a.d.Hk);  // (the last units see the most tokens)
   if (unit.rows == 0 || split >= unit.splits) return;
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, n = lane & 31, h = lane / 32;
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % kWaves, group = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / kWaves;
+  const int thread = 64 * wave + lane;  // of the group
+  char (*const lds)[2][Geo::kTileBytes] = all_lds[group];
   const int bytes = a.d.D * Geo::kSize;
   const int64_t page_bytes = (static_cast<int64_t>(a.d.Hk) << a.d.lg_page) * bytes;
   const int page_mask = (1 << a.d.lg_page) - 1;
@@ -463,8 +515,10 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_f32_kerne
     for (int r = 0; r < 16; ++r) o[c][r] = 0.f;
   float m = kNone, l = 0.f;
 
-  const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * split / unit.splits);
+  // the split's tiles, of which the group takes every kGroups-th
   const int tile1 = static_cast<int>(static_cast<int64_t>(unit.tiles) * (split + 1) / unit.splits);
+  const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * split / unit.splits) + group;
+  const int rounds = (tile1 - (tile0 - group) + kGroups - 1) / kGroups;
   const int end = unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1;  // tokens seen by any row
 
   u32x4 fetched[2][Geo::kFetch];
@@ -478,7 +532,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_f32_kerne
     if (bad) page = -1;
 #pragma unroll
     for (int i = 0; i < Geo::kFetch; ++i) {
-      const int piece = threadIdx.x + i * kThreads, r = piece / Geo::kPieces, c = piece % Geo::kPieces;
+      const int piece = thread + i * kThreads, r = piece / Geo::kPieces, c = piece % Geo::kPieces;
       const int where = __shfl(page, r);
       const int at = min(first + r, end - 1) & page_mask;
       fetched[0][i] = fetched[1][i] = u32x4{0u, 0u, 0u, 0u};
@@ -493,24 +547,24 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_f32_kerne
   auto stage = [&](int buffer) {
 #pragma unroll
     for (int i = 0; i < Geo::kFetch; ++i) {
-      const int piece = threadIdx.x + i * kThreads, r = piece / Geo::kPieces, c = piece % Geo::kPieces;
+      const int piece = thread + i * kThreads, r = piece / Geo::kPieces, c = piece % Geo::kPieces;
       *reinterpret_cast<u32x4 *>(&lds[buffer][0][r * Geo::kRowBytes + 16 * Geo::key_piece(r, c)]) = fetched[0][i];
       *reinterpret_cast<u32x4 *>(&lds[buffer][1][r * Geo::kRowBytes + 16 * Geo::value_piece(r, c)]) = fetched[1][i];
     }
     gone = gone_next;
   };
 
-  if (tile0 < tile1) {
+  if (rounds > 0) {
     fetch(tile0);
     stage(0);
   }
   __syncthreads();
-  for (int tile = tile0; tile < tile1; ++tile) {
-    const int buffer = (tile - tile0) & 1, first = unit.base + tile * kTokens;
+  for (int round = 0; round < rounds; ++round) {
+    const int tile = tile0 + kGroups * round, buffer = round & 1, first = unit.base + tile * kTokens;
     const char *kt = lds[buffer][0], *vt = lds[buffer][1];
     const uint64_t gone_now = gone;
-    if (tile + 1 < tile1) fetch(tile + 1);
-    if (!idle && first <= any_to) {
+    if (round + 1 < rounds) fetch(tile + kGroups);
+    if (!idle && tile < tile1 && first <= any_to) {
       f32x16 s;
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = 0.f;
@@ -555,100 +609,119 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void prefill_f32_kerne
         for (int c = 0; c < kColTiles; ++c) o[c] = mfma_f32(vrow[32 * c + n], s[r], o[c]);
       }
     }
-    if (tile + 1 < tile1) stage(buffer ^ 1);
+    if (round + 1 < rounds) stage(buffer ^ 1);
     __syncthreads();
   }
 
   l += __shfl_xor(l, 32);
-  if (mine) finish<false, DP>(a, unit, local, kUnitRows, out_row, h, o, m, l);
+  if (kGroups == 2 && !join_groups<DP>(*reinterpret_cast<Part<DP> *>(all_lds), group, wave, o, m, l)) return;
+  finish<false, DP>(a, unit.splits == 1, blockIdx.x, mine, wave, out_row, o, m, l);
 }
 
-// Joins the splits of a unit: one workgroup for kJoinRows of its rows.
-constexpr int kJoinRows = 16;
-template <bool kBf16>
+// Joins the parts of a unit, 32 of its columns a workgroup.
+template <bool kBf16, int DP>
 __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillArgs a) {
+  constexpr int kTokens = tokens_of_tile(kBf16);
   int id = blockIdx.x;
-  const int cut = id % (kUnitRows / kJoinRows);
-  id /= kUnitRows / kJoinRows;
+  const int cut = id % (DP / 32);
+  id /= DP / 32;
   const int hk = id % a.d.Hk;
-  const Unit unit = find_unit<kBf16 ? 64 : 32>(a, a.units - 1 - id / a.d.Hk);
-  if (unit.rows <= cut * kJoinRows || unit.splits == 1) return;
-  const int cols = a.d.D / 4;
-  for (int e = threadIdx.x; e < kJoinRows * cols; e += kThreads) {
-    const int local = cut * kJoinRows + e / cols, col = 4 * (e % cols);
-    if (local >= unit.rows) break;
-    const float *part = a.part + (static_cast<int64_t>(id) * a.splits * kUnitRows + local) * (a.d.D + 4);
-    const int64_t step = static_cast<int64_t>(kUnitRows) * (a.d.D + 4);
-    float top = kNone, sum = 0.f;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < unit.splits; ++s, part += step) {
-      const float m = part[a.d.D], l = part[a.d.D + 1];
-      const f32x4 o = *reinterpret_cast<const f32x4 *>(part + col);
-      const float next = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(top - next), f = __builtin_amdgcn_exp2f(m - next);
-      top = next;
-      sum = fmaf(sum, keep, l * f);
+  const Unit unit = find_unit<kTokens>(a, a.units - 1 - id / a.d.Hk);
+  if (unit.rows == 0 || unit.splits == 1) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, local = 32 * wave + (lane & 31), h = lane / 32;
+  float top = kNone, sum = 0.f;
+  f32x4 o[4] = {};
+#pragma unroll 2
+  for (int split = 0; split < unit.splits; ++split) {
+    const Part<DP> &part = static_cast<const Part<DP> *>(a.part)[static_cast<int64_t>(id) * a.splits + split];
+    const float m = part.m[wave][lane], l = part.l[wave][lane];
+    const float next = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(top - next), f = __builtin_amdgcn_exp2f(m - next);
+    top = next;
+    sum = fmaf(sum, keep, l * f);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = fmaf(v[r], keep, o[r] * f);
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int row = unit.first_row + local, token = quotient(row, a.d.G, a.inv_group);
-    const int64_t at = (static_cast<int64_t>(unit.begin + token) * a.d.H + hk * a.d.G + (row - token * a.d.G)) * a.d.D + col;
-    if constexpr (kBf16) {
-      const u32x2 q = {pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
-      *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + at) = q;
-    } else {
-      *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + at) = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 q = part.o[wave][4 * cut + i][lane];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[i][r] = fmaf(o[i][r], keep, q[r] * f);
     }
   }
+  if (local >= unit.rows) return;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int row = unit.first_row + local, token = quotient(row, a.d.G, a.inv_group);
+  const int64_t out_row = static_cast<int64_t>(unit.begin + token) * a.d.H + hk * a.d.G + (row - token * a.d.G);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) write_row<kBf16>(a, out_row, piece_column(4 * cut + i, h), o[i], inv);
 }
 
 struct Plan {
-  int units, splits;
+  int units, splits, groups;
 };
+// Two groups of waves share a unit where that leaves every CU a workgroup or few more: 2048 tokens, 32 heads over 8 of 128, 520
+// units: 52 us, with a group each 56; 4096 tokens, 1032 units: 170 and 155.  Units of few tiles are not worth it: four times 512
+// tokens, 8 tiles: 31 and 25; 1024 tokens, 16 tiles: 24 and 27.  fp32, bound by its products alone, always: 2048 tokens, 16 heads
+// over 4 of 128, twice: 327 and 535; 8192 tokens, heads of 64: 1186 and 1268.
+//
+// A unit's tiles are shared by several workgroups where that shortens the longest row of units a CU works on by more than the
+// parts' way through memory and the second launch take.  The host knows the rows of all sequences together, not of each, and the
+// most tokens that the page table holds.
 Plan plan_of(const AttnDims &d) {
   Plan p;
-  p.units = static_cast<int>(static_cast<int64_t>(d.T) * d.G / kUnitRows + d.B);
+  const int64_t rows = static_cast<int64_t>(d.T) * d.G;
+  p.units = static_cast<int>(rows / kUnitRows + d.B);
   const int64_t all = static_cast<int64_t>(p.units) * d.Hk;
-  const int64_t tiles = d.capacity() / (d.bf16 ? 64 : 32);
-  const int64_t wanted = (kWantedUnits + all - 1) / all, most = tiles / kSplitTiles;
-  p.splits = static_cast<int>(wanted < most ? wanted : most);
-  if (p.splits < 1) p.splits = 1;
+  const int64_t most_seen = d.window > 0 ? std::min<int64_t>(d.capacity(), static_cast<int64_t>(d.window) + kUnitRows / d.G) : d.capacity();
+  const int64_t tiles = (most_seen + tokens_of_tile(d.bf16) - 1) / tokens_of_tile(d.bf16);
+  p.groups = d.D <= 128 && (!d.bf16 || (all < kManyUnits && tiles >= kManyTiles)) ? 2 : 1;
+  p.splits = 1;
+  if (all >= kManyUnits) return p;
+  // in us: a tile on a CU (bf16 at 1 PFLOP/s, fp32 at 150 TFLOP/s); a part written and read
+  const double tile = (d.bf16 ? 1.0 : 3.5) * d.D / 128, part = 0.04 * d.D / 128, launch = 5.0;
+  const double units = (std::ceil(static_cast<double>(rows) / kUnitRows) + 0.5 * (d.B - 1)) * d.Hk;
+  // whole prompts, whose units see from no tile to all: the longest first fills the CUs evenly; pieces behind a long cache see much
+  // the same each, and the last CU to begin one decides
+  const bool prompts = most_seen <= 2 * static_cast<int64_t>(d.T / d.B);
+  double best = 0.0;
+  for (int s = 1; s == 1 || (s <= kMostSplits && (s - 1) * kSplitTokens < most_seen); ++s) {
+    const double longest = static_cast<double>(tiles) / s;
+    const double row = prompts ? std::max(longest, units * tiles / 2 / kWorkgroups) + longest / 4 : std::ceil(units * s / kWorkgroups) * longest;
+    const double cost = row * tile + (s > 1 ? launch + part * units * s : 0.0);
+    if (s == 1 || cost < best) {
+      best = cost;
+      p.splits = s;
+    }
+  }
   return p;
 }
 
-template <int DP>
-void launch_bf16(const PrefillArgs &a, dim3 grid, hipStream_t stream) {
-  if (a.d.D == DP)
-    hipLaunchKernelGGL((prefill_bf16_kernel<DP, true>), grid, dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((prefill_bf16_kernel<DP, false>), grid, dim3(kThreads), 0, stream, a);
-}
-
+template <bool kBf16, int DP>
 hipError_t launch(const PrefillArgs &a, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(a.units) * a.d.Hk * a.splits), threads(kThreads);
-  if (a.d.bf16) {
-    if (a.d.D > 128)
-      launch_bf16<256>(a, grid, stream);
-    else if (a.d.D > 64)
-      launch_bf16<128>(a, grid, stream);
+  const dim3 grid(static_cast<unsigned>(a.units) * a.d.Hk * a.splits);
+  constexpr int kTwo = DP <= 128 ? 2 : 1;  // (heads of 256 values leave registers for one wave a SIMD)
+  const bool two = kTwo == 2 && a.groups == 2;
+  const dim3 threads(two ? 2 * kThreads : kThreads);
+  if constexpr (!kBf16) {
+    if (two)
+      hipLaunchKernelGGL((prefill_f32_kernel<DP, kTwo>), grid, threads, 0, stream, a);
     else
-      launch_bf16<64>(a, grid, stream);
+      hipLaunchKernelGGL((prefill_f32_kernel<DP, 1>), grid, threads, 0, stream, a);
+  } else if (a.d.D == DP) {
+    if (two)
+      hipLaunchKernelGGL((prefill_bf16_kernel<DP, true, kTwo>), grid, threads, 0, stream, a);
+    else
+      hipLaunchKernelGGL((prefill_bf16_kernel<DP, true, 1>), grid, threads, 0, stream, a);
   } else {
-    if (a.d.D > 128)
-      hipLaunchKernelGGL(prefill_f32_kernel<256>, grid, threads, 0, stream, a);
-    else if (a.d.D > 64)
-      hipLaunchKernelGGL(prefill_f32_kernel<128>, grid, threads, 0, stream, a);
+    if (two)
+      hipLaunchKernelGGL((prefill_bf16_kernel<DP, false, kTwo>), grid, threads, 0, stream, a);
     else
-      hipLaunchKernelGGL(prefill_f32_kernel<64>, grid, threads, 0, stream, a);
+      hipLaunchKernelGGL((prefill_bf16_kernel<DP, false, 1>), grid, threads, 0, stream, a);
   }
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-  const dim3 joins(static_cast<unsigned>(a.units) * a.d.Hk * (kUnitRows / kJoinRows));
-  if (a.d.bf16)
-    hipLaunchKernelGGL(prefill_join_kernel<true>, joins, threads, 0, stream, a);
-  else
-    hipLaunchKernelGGL(prefill_join_kernel<false>, joins, threads, 0, stream, a);
+  hipLaunchKernelGGL((prefill_join_kernel<kBf16, DP>), dim3(static_cast<unsigned>(a.units) * a.d.Hk * (DP / 32)), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
+}
+template <bool kBf16>
+hipError_t launch(const PrefillArgs &a, hipStream_t stream) {
+  return a.d.D <= 64 ? launch<kBf16, 64>(a, stream) : a.d.D <= 128 ? launch<kBf16, 128>(a, stream) : launch<kBf16, 256>(a, stream);
 }
 
 }  // namespace
@@ -656,7 +729,7 @@ hipError_t launch(const PrefillArgs &a, hipStream_t stream) {
 size_t attn_prefill_workspace_bytes(const AttnDims &d) {
   const Plan p = plan_of(d);
   if (p.splits == 1) return 256;
-  return (static_cast<size_t>(p.units) * d.Hk * p.splits * kUnitRows * (d.D + 4) * 4 + 255) / 256 * 256;
+  return static_cast<size_t>(p.units) * d.Hk * p.splits * (d.D <= 64 ? sizeof(Part<64>) : d.D <= 128 ? sizeof(Part<128>) : sizeof(Part<256>));
 }
 
 hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32_t *lens, const int32_t *table, const void *q,
@@ -671,13 +744,14 @@ hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32
   a.k = k_cache;
   a.v = v_cache;
   a.y = y;
-  a.part = static_cast<float *>(workspace);
+  a.part = workspace;
   a.d = d;
   a.inv_group = inverse_of(d.G);
   a.units = p.units;
   a.splits = p.splits;
+  a.groups = p.groups;
   a.scale_log2 = scale * 1.44269504f;
-  return launch(a, stream);
+  return d.bf16 ? launch<true>(a, stream) : launch<false>(a, stream);
 }
 
 }  // namespace ssd

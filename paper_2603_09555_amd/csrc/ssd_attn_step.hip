@@ -23,7 +23,7 @@ namespace {
 
 using namespace block;
 
-constexpr int kThreads = 256, kWaves = 4, kTile = 32, kBlock = kWaves * kTile, kRows = 16;
+constexpr int kThreads = kDealers, kWaves = 4, kTile = 32, kBlock = kWaves * kTile, kRows = 16;
 constexpr int kWorkgroups = 1024;  // a power of two
 constexpr int kLgWorkgroups = 10;
 constexpr unsigned kFewUnits = 256;
@@ -52,27 +52,8 @@ __device__ __forceinline__ Span span_of(const StepArgs &a, int b) {
   return s;
 }
 
-// Blocks (of one unit each) of the sequences in front of each thread's share of them; [kThreads]: of all.
-struct Prefix {
-  int64_t at[kThreads + 1];
-  int64_t wave[kWaves];
-};
 __device__ __forceinline__ void count_blocks(const StepArgs &a, Prefix &s) {
-  const int t = threadIdx.x, lane = t & 63, share = (a.d.B + kThreads - 1) / kThreads;
-  int64_t mine = 0;
-  for (int b = t * share; b < min((t + 1) * share, a.d.B); ++b) mine += span_of(a, b).blocks;
-  int64_t sum = mine;
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const int64_t o = __shfl_up(sum, k);
-    if (lane >= k) sum += o;
-  }
-  if (lane == 63) s.wave[t / 64] = sum;
-  __syncthreads();
-  for (int w = 0; w < t / 64; ++w) sum += s.wave[w];
-  s.at[t + 1] = sum;
-  if (t == 0) s.at[0] = 0;
-  __syncthreads();
+  count_blocks(s, a.d.B, [&](int b) { return span_of(a, b).blocks; });
 }
 
 // Exchanges halves: the low (or high) 16 bits of two registers.
@@ -189,17 +170,14 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void step_kernel(const
 
   // the run of this workgroup, and where it begins
   count_blocks(a, lds.prefix);
-  const int64_t total = lds.prefix.at[kThreads] * a.units;
+  const int64_t total = uniform(lds.prefix.at[kDealers]) * a.units;
   const int64_t run = (total + kWorkgroups - 1) >> kLgWorkgroups;
   int64_t at = blockIdx.x * run;
   const int64_t end = min(total, at + run);
   if (at >= end) return;
-  int share = 0;
-#pragma unroll
-  for (int s = kThreads / 2; s > 0; s >>= 1)
-    if (lds.prefix.at[share + s] * a.units <= at) share += s;
-  int b = share * ((a.d.B + kThreads - 1) / kThreads);
-  int64_t left = at - lds.prefix.at[share] * a.units;
+  const int dealer = dealer_of(lds.prefix, at, a.units);
+  int b = dealer * share_of(a.d.B);
+  int64_t left = uniform(at - lds.prefix.at[dealer] * a.units);
   Span sp = span_of(a, b);
   while (left >= static_cast<int64_t>(sp.blocks) * a.units) {
     left -= static_cast<int64_t>(sp.blocks) * a.units;
@@ -383,8 +361,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int ro
   id /= static_cast<unsigned>(col_cuts * row_cuts);
   const int b = static_cast<int>(id / static_cast<unsigned>(a.units)), unit = static_cast<int>(id) - b * a.units;
   count_blocks(a, prefix);
-  const int64_t total = prefix.at[kThreads] * a.units, run = (total + kWorkgroups - 1) >> kLgWorkgroups;
-  const int share = (a.d.B + kThreads - 1) / kThreads;
+  const int64_t total = prefix.at[kDealers] * a.units, run = (total + kWorkgroups - 1) >> kLgWorkgroups;
+  const int share = share_of(a.d.B);
   int64_t before = prefix.at[b / share];
   for (int i = b / share * share; i < b; ++i) before += span_of(a, i).blocks;
   const Span sp = span_of(a, b);
