@@ -11,27 +11,23 @@ namespace ssd {
 __device__ __forceinline__ int cut_length(const AttnDims &d, int len) { return min(max(len, 0), d.capacity()); }
 
 struct Token {
-  int seq, pos;  // pos < 0: in front of its sequence's beginning
-  bool found;    // in a sequence
+  int seq, pos;  // pos < 0: in no sequence, or in front of its beginning
 };
 
-// The sequence and position of a packed new token (cu == nullptr: one for each sequence).  All lanes of a wave ask for the
-// same token: 64 boundaries are compared at a time.
+// The sequence and position of a packed new token (cu == nullptr: one for each sequence).
 __device__ __forceinline__ Token find_token(const AttnDims &d, const int32_t *cu, const int32_t *lens, int token) {
-  Token t = {token, -1, cu == nullptr};
+  Token t = {token, -1};
   int end = token + 1;
   if (cu != nullptr) {
-    int last = -1;  // the last sequence that begins at or in front of the token (and, being last, is not empty)
-    for (int b0 = 0; b0 < d.B; b0 += 64) {
-      const int b = b0 + (threadIdx.x & 63);
-      const uint64_t m = __ballot(b < d.B && cu[b] <= token);
-      if (m != 0) last = b0 + 63 - __builtin_clzll(m);
+    int last = 0, behind = d.B;  // the last sequence that begins at or in front of the token (and, being last, is not empty)
+    while (behind - last > 1) {
+      const int b = (last + behind) / 2;
+      if (cu[b] <= token) last = b;
+      else behind = b;
     }
-    if (last < 0) return t;
-    t.seq = last;
     end = min(cu[last + 1], d.T);
-    if (token >= end) return t;
-    t.found = true;
+    if (cu[last] > token || token >= end) return t;
+    t.seq = last;
   }
   t.pos = cut_length(d, lens[t.seq]) - (end - token);
   return t;

@@ -4,14 +4,21 @@
 //   pair (a, c) of head values:             (a cos - c sin, c cos + a sin),  cos, sin = rope[p][pair]
 //   key, value  ->  page table[b][p / page_size], slot p % page_size
 //
-// A copy in effect: each value is read and written once.  A thread writes one piece of 16 bytes of one head of one token
-// (and reads the piece that holds the other halves of its pairs, which a neighbour reads too, from the first-level cache).
+// A copy in effect: each value is read and written once, bound by memory, or by the chain of memory latencies for few tokens
+// (boundaries, length, page, then the values).  A workgroup finds the places of a few neighbouring tokens once; its threads then
+// take their pieces of 16 bytes in turn.  A piece that holds one half of its pairs brings the other halves' piece with it, which
+// its neighbour brings too, from the first-level cache.
+#include <algorithm>
+
 #include "ssd_attn.hpp"
 
 namespace ssd {
 namespace {
 
 using namespace block;
+
+constexpr int kMostTokens = 16;        // a workgroup
+constexpr int kManyItems = 256 * 2048;  // pieces that are a workgroup of one each for 2048
 
 struct AppendArgs {
   const void *src[3];      // q, k, v
@@ -23,73 +30,123 @@ struct AppendArgs {
   int head_pieces;         // pieces of a head
   uint32_t inv_head_pieces;
   int row_pieces;          // pieces of a token: queries (if any), keys, values
+  uint32_t inv_row_pieces;
   int q_heads;             // 0: no queries
+  int run;                 // tokens a workgroup
 };
 
-template <typename E>
-__device__ __forceinline__ float value(E v);
-template <>
-__device__ __forceinline__ float value<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ float value<uint16_t>(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+struct Place {
+  int pos;       // < 0: none
+  int64_t slot;  // cache row of key head 0, or -1
+};
 
 template <bool kBf16>
-__global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
-  using E = typename std::conditional<kBf16, uint16_t, float>::type;
-  constexpr int W = 16 / sizeof(E);
-  const int token = blockIdx.x;
-  const int idx = blockIdx.y * 256 + threadIdx.x;
-  const Token at = find_token(a.d, a.cu, a.lens, token);
-  if (!at.found || at.pos < 0 || idx >= a.row_pieces) return;
-  int head = quotient(idx, a.head_pieces, a.inv_head_pieces);
-  const int first = (idx - head * a.head_pieces) * W;
-  // which of q, k, v
-  int what = 0;
-  if (head >= a.q_heads) {
-    head -= a.q_heads;
-    what = 1;
-    if (head >= a.d.Hk) {
-      head -= a.d.Hk;
-      what = 2;
+using Element = typename std::conditional<kBf16, uint16_t, float>::type;
+__device__ __forceinline__ float value(float v) { return v; }
+__device__ __forceinline__ float value(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+template <bool kBf16, int W>
+__device__ __forceinline__ void unpack(const u32x4 &q, float (&v)[W]) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = !kBf16 ? __uint_as_float(q[i % 4]) : i % 2 == 0 ? bf_lo(q[i / 2]) : bf_hi(q[i / 2]);
+}
+// N neighbouring values at an address of any multiple of 4
+template <int N>
+__device__ __forceinline__ void load_rope(const float *p, float *v) {
+  typedef f32x4 __attribute__((aligned(4))) vec4;
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef f32x2 __attribute__((aligned(4))) vec2;
+  if constexpr (N == 2) {
+    const f32x2 a = *reinterpret_cast<const vec2 *>(p);
+    v[0] = a[0];
+    v[1] = a[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const f32x4 a = *reinterpret_cast<const vec4 *>(p + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[i + k] = a[k];
     }
   }
-  E *dst;
-  if (what == 0) {
-    dst = static_cast<E *>(a.q_out) + (static_cast<int64_t>(token) * a.d.H + head) * a.d.D + first;
-  } else {
-    const int64_t slot = slot_of(a.d, a.table, at.seq, at.pos, head);
-    if (slot < 0) return;
-    dst = static_cast<E *>(a.cache[what - 1]) + slot * a.d.D + first;
+}
+
+// kWhole: pieces lie in one half of the pairs (interleaved pairs: in the rotated part) or outside it.
+template <bool kBf16, bool kWhole>
+__global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
+  using E = Element<kBf16>;
+  constexpr int W = 16 / sizeof(E);
+  __shared__ Place place[kMostTokens];
+  const int first_token = blockIdx.x * a.run, tokens = min(a.run, a.d.T - first_token), items = tokens * a.row_pieces;
+  if (static_cast<int>(threadIdx.x) < tokens) {
+    const Token t = find_token(a.d, a.cu, a.lens, first_token + threadIdx.x);
+    place[threadIdx.x] = {t.pos, t.pos < 0 ? -1 : slot_of(a.d, a.table, t.seq, t.pos, 0)};
   }
-  const E *src = static_cast<const E *>(a.src[what]) + token * a.stride[what] + static_cast<int64_t>(head) * a.d.D;
-  u32x4 q = *reinterpret_cast<const u32x4 *>(src + first);
+  __syncthreads();
   const int half = a.rope.half;
-  if (what < 2 && first < 2 * half) {
-    const float *cs = a.rope.cos + static_cast<int64_t>(at.pos) * half, *sn = a.rope.sin + static_cast<int64_t>(at.pos) * half;
-    E e[W];
-    __builtin_memcpy(e, &q, 16);
-    float r[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      const int c = first + i;
-      r[i] = value(e[i]);
-      if (c < 2 * half) {
-        const bool second = a.rope.interleaved ? (c & 1) : c >= half;
-        const int pair = a.rope.interleaved ? c >> 1 : second ? c - half : c;
-        const int other = a.rope.interleaved ? c ^ 1 : second ? c - half : c + half;
-        const float o = value(src[other]);
-        r[i] = fmaf(r[i], cs[pair], second ? o * sn[pair] : -o * sn[pair]);
+  for (int item = blockIdx.y * 256 + threadIdx.x; item < items; item += gridDim.y * 256) {
+    const int local = quotient(item, a.row_pieces, a.inv_row_pieces), idx = item - local * a.row_pieces, token = first_token + local;
+    const Place at = place[local];
+    int head = quotient(idx, a.head_pieces, a.inv_head_pieces);
+    const int first = (idx - head * a.head_pieces) * W;
+    // which of q, k, v
+    int what = 0;
+    if (head >= a.q_heads) {
+      head -= a.q_heads;
+      what = 1;
+      if (head >= a.d.Hk) {
+        head -= a.d.Hk;
+        what = 2;
       }
     }
-    if (kBf16) {
+    if (at.pos < 0 || (what > 0 && at.slot < 0)) continue;
+    E *const dst = what == 0 ? static_cast<E *>(a.q_out) + (static_cast<int64_t>(token) * a.d.H + head) * a.d.D + first
+                             : static_cast<E *>(a.cache[what - 1]) + (at.slot + (static_cast<int64_t>(head) << a.d.lg_page)) * a.d.D + first;
+    const E *const src = static_cast<const E *>(a.src[what]) + token * a.stride[what] + static_cast<int64_t>(head) * a.d.D;
+    u32x4 q = *reinterpret_cast<const u32x4 *>(src + first);
+    if (what < 2 && first < 2 * half) {
+      const float *const cs = a.rope.cos + static_cast<int64_t>(at.pos) * half, *const sn = a.rope.sin + static_cast<int64_t>(at.pos) * half;
+      float v[W], r[W];
+      unpack<kBf16>(q, v);
+      if (kWhole && !a.rope.interleaved) {
+        const bool second = first >= half;
+        const int pair = second ? first - half : first;
+        float o[W], c[W], s[W];
+        unpack<kBf16>(*reinterpret_cast<const u32x4 *>(src + (second ? first - half : first + half)), o);
+        load_rope<W>(cs + pair, c);
+        load_rope<W>(sn + pair, s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) q[i] = pack2(r[(2 * i) % W], r[(2 * i + 1) % W]);
-    } else {
+        for (int i = 0; i < W; ++i) r[i] = fmaf(v[i], c[i], second ? o[i] * s[i] : -o[i] * s[i]);
+      } else if (kWhole) {
+        float c[W / 2], s[W / 2];
+        load_rope<W / 2>(cs + first / 2, c);
+        load_rope<W / 2>(sn + first / 2, s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) q[i] = __float_as_uint(r[i]);
+        for (int i = 0; i < W; i += 2) {
+          r[i] = fmaf(v[i], c[i / 2], -v[i + 1] * s[i / 2]);
+          r[i + 1] = fmaf(v[i + 1], c[i / 2], v[i] * s[i / 2]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const int c = first + i;
+          r[i] = v[i];
+          if (c < 2 * half) {
+            const bool second = a.rope.interleaved ? (c & 1) : c >= half;
+            const int pair = a.rope.interleaved ? c >> 1 : second ? c - half : c;
+            const float o = value(src[a.rope.interleaved ? c ^ 1 : second ? c - half : c + half]);
+            r[i] = fmaf(v[i], cs[pair], second ? o * sn[pair] : -o * sn[pair]);
+          }
+        }
+      }
+      if constexpr (kBf16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = pack2(r[2 * i], r[2 * i + 1]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = __float_as_uint(r[i]);
+      }
     }
+    *reinterpret_cast<u32x4 *>(dst) = q;
   }
-  *reinterpret_cast<u32x4 *>(dst) = q;
 }
 
 }  // namespace
@@ -116,11 +173,21 @@ hipError_t launch_attn_append(const AttnDims &d, const Rope &rope, const int32_t
   a.head_pieces = d.D / (d.bf16 ? 8 : 4);
   a.inv_head_pieces = inverse_of(a.head_pieces);
   a.row_pieces = (a.q_heads + 2 * d.Hk) * a.head_pieces;
-  const dim3 grid(d.T, (a.row_pieces + 255) / 256);
-  if (d.bf16)
-    hipLaunchKernelGGL(append_kernel<true>, grid, dim3(256), 0, stream, a);
+  a.inv_row_pieces = inverse_of(a.row_pieces);
+  // a few tokens a workgroup where there are workgroups enough, and one item a thread where there are not
+  const int64_t items = static_cast<int64_t>(d.T) * a.row_pieces;
+  a.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMostTokens, items / kManyItems)));
+  const dim3 grid((d.T + a.run - 1) / a.run, a.run > 1 ? 1 : (a.row_pieces + 255) / 256);
+  const int width = rope.interleaved ? 2 * rope.half : rope.half;
+  const bool whole = width % (d.bf16 ? 8 : 4) == 0;
+  if (d.bf16 && whole)
+    hipLaunchKernelGGL((append_kernel<true, true>), grid, dim3(256), 0, stream, a);
+  else if (d.bf16)
+    hipLaunchKernelGGL((append_kernel<true, false>), grid, dim3(256), 0, stream, a);
+  else if (whole)
+    hipLaunchKernelGGL((append_kernel<false, true>), grid, dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL(append_kernel<false>, grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((append_kernel<false, false>), grid, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

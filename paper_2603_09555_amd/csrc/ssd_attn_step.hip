@@ -12,10 +12,16 @@
 //   * the first operand is then eight values of one column of V, from eight tokens.  A lane reads its eight tokens' rows, some
 //     neighbouring columns of each, and makes the columns' operands by exchanging halves of registers (bf16; fp32 needs none).
 //
+// The waves of a workgroup take every kWaves-th tile of a unit (a sequence and key head) and are joined through LDS at its end.
+// What hides the latency of memory is other waves' requests; where a SIMD has no more than two waves, the next tile's keys are asked
+// for before this one is worked on, and its page numbers a tile earlier.
+//
 // Work is dealt by length: the visible tokens of all sequences and key heads, in blocks of 128, make one long list of which every
-// workgroup takes an equal run, whatever the lengths are; the four waves of a workgroup take every fourth tile of a block's 32
-// tokens and are joined through LDS at the end of a unit (a sequence and key head).  A unit within one workgroup is finished
-// there; the others leave (m, l, O) in the workspace, which a second launch joins.
+// workgroup takes an equal run, whatever the lengths are.  A unit within one workgroup is finished there; the others leave
+// (m, l, O) in the workspace, which a second launch joins.  Where no sequence can be long, a workgroup of eight waves takes a unit
+// and there is no second launch.
+#include <algorithm>
+
 #include "ssd_attn.hpp"
 
 namespace ssd {
@@ -23,9 +29,10 @@ namespace {
 
 using namespace block;
 
-constexpr int kThreads = kDealers, kWaves = 4, kTile = 32, kBlock = kWaves * kTile, kRows = 16;
-constexpr int kWorkgroups = 1024;  // a power of two
-constexpr int kLgWorkgroups = 10;
+constexpr int kThreads = kDealers, kTile = 32, kBlock = kThreads / 64 * kTile, kRows = 16;
+// Workgroups that work is dealt to: as many as are in work at a time, four to one a CU as their registers allow.
+constexpr int workgroups_of(bool bf16, int dp) { return 256 * (dp == 256 ? 1 : bf16 ? (dp == 64 ? 4 : 3) : dp == 64 ? 3 : 2); }
+constexpr int kMostWorkgroups = 1024;
 constexpr unsigned kFewUnits = 256;
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
 
@@ -37,8 +44,12 @@ struct StepArgs {
   AttnDims d;
   int row_tiles;     // of 16 heads, of a key head's heads
   int units;         // of a sequence
+  int workgroups;    // that work is dealt to
   float scale_log2;  // scale * log2(e)
 };
+
+inline int row_tiles_of(const AttnDims &d) { return (d.G + kRows - 1) / kRows; }  // of 16 heads, of a key head's heads
+inline int units_of(const AttnDims &d) { return d.Hk * row_tiles_of(d); }         // of a sequence
 
 struct Span {
   int lo, len, base, blocks;  // tokens seen: [lo, len), in blocks of 128 from base on
@@ -76,7 +87,9 @@ struct Tile {
   static constexpr int kValuePieces = kCols * kSize / 16 > 0 ? kCols * kSize / 16 : 1;  // of 16 bytes (one of 8 if that is less)
   static constexpr bool kHalfPiece = kCols * kSize == 8;
 
-  u32x4 key[2][kKeyPieces];
+  struct Keys {
+    u32x4 of[2][kKeyPieces];
+  };
   u32x4 val[8][kValuePieces];
 
   // Byte of a row where the lane's piece p of V begins.
@@ -84,13 +97,13 @@ struct Tile {
   // Column of V that element c of the lane n's operands stands for.
   static __device__ __forceinline__ int column(int c, int n) { return kBf16 ? n * kCols + c : 64 * (c / 4) + 4 * n + c % 4; }
 
-  __device__ __forceinline__ void load_key(int half, const char *row, int j, int bytes) {
+  static __device__ __forceinline__ void load_key(Keys &keys, int half, const char *row, int j, int bytes) {
 #pragma unroll
     for (int i = 0; i < kKeyPieces; ++i) {
       const int at = 64 * i + 16 * j;
       u32x4 q = {0u, 0u, 0u, 0u};
       if (at < bytes) q = *reinterpret_cast<const u32x4 *>(row + at);
-      key[half][i] = q;
+      keys.of[half][i] = q;
     }
   }
   __device__ __forceinline__ void load_value(int i, const char *row, int n, int bytes) {
@@ -115,15 +128,15 @@ struct Tile {
     for (int p = 0; p < kValuePieces; ++p) val[i][p] = u32x4{0u, 0u, 0u, 0u};
   }
 
-  __device__ __forceinline__ f32x4 scores(int half, const u32x4 (&query)[kKeyPieces]) const {
+  static __device__ __forceinline__ f32x4 scores(const Keys &keys, int half, const u32x4 (&query)[kKeyPieces]) {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kKeyPieces; ++i) {
       if (kBf16) {
-        s = mfma_bf16(key[half][i], query[i], s);
+        s = mfma_bf16(keys.of[half][i], query[i], s);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = mfma_f32(__uint_as_float(key[half][i][e]), __uint_as_float(query[i][e]), s);
+        for (int e = 0; e < 4; ++e) s = mfma_f32(__uint_as_float(keys.of[half][i][e]), __uint_as_float(query[i][e]), s);
       }
     }
     return s;
@@ -153,9 +166,18 @@ struct Tile {
   }
 };
 
-template <bool kBf16, int DP>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void step_kernel(const StepArgs a) {
+constexpr int waves_a_simd(bool bf16, int dp) { return dp == 256 ? 1 : 2; }
+
+// a / b of which one, as a rule, does not need 64 bits.
+__device__ __forceinline__ int64_t quotient64(int64_t n, int64_t d) {
+  return (n | d) >> 32 == 0 ? static_cast<int64_t>(static_cast<uint32_t>(n) / static_cast<uint32_t>(d)) : n / d;
+}
+__device__ __forceinline__ int64_t run_of(const StepArgs &a, int64_t total) { return quotient64(total + a.workgroups - 1, a.workgroups); }
+
+template <bool kBf16, int DP, int kWaves, bool kDealt>
+__global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_kernel(const StepArgs a) {
   using T = Tile<kBf16, DP>;
+  constexpr bool kAhead = kDealt ? kBf16 && DP == 256 : kBf16 || DP == 64;
   __shared__ union {
     Prefix prefix;
     struct {
@@ -169,26 +191,35 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void step_kernel(const
   const int page_mask = (1 << a.d.lg_page) - 1;
 
   // the run of this workgroup, and where it begins
-  count_blocks(a, lds.prefix);
-  const int64_t total = uniform(lds.prefix.at[kDealers]) * a.units;
-  const int64_t run = (total + kWorkgroups - 1) >> kLgWorkgroups;
-  int64_t at = blockIdx.x * run;
-  const int64_t end = min(total, at + run);
-  if (at >= end) return;
-  const int dealer = dealer_of(lds.prefix, at, a.units);
-  int b = dealer * share_of(a.d.B);
-  int64_t left = uniform(at - lds.prefix.at[dealer] * a.units);
-  Span sp = span_of(a, b);
-  while (left >= static_cast<int64_t>(sp.blocks) * a.units) {
-    left -= static_cast<int64_t>(sp.blocks) * a.units;
-    sp = span_of(a, ++b);
+  int64_t at = 0, end = 0;
+  int b, unit, block = 0;
+  Span sp;
+  if (kDealt) {
+    count_blocks(a, lds.prefix);
+    const int64_t total = uniform(lds.prefix.at[kDealers]) * a.units, run = run_of(a, total);
+    at = blockIdx.x * run;
+    end = min(total, at + run);
+    if (at >= end) return;
+    const int dealer = dealer_of(lds.prefix, at, a.units);
+    b = dealer * share_of(a.d.B);
+    int64_t left = uniform(at - lds.prefix.at[dealer] * a.units);
+    sp = span_of(a, b);
+    while (left >= static_cast<int64_t>(sp.blocks) * a.units) {
+      left -= static_cast<int64_t>(sp.blocks) * a.units;
+      sp = span_of(a, ++b);
+    }
+    unit = static_cast<int>(quotient64(left, sp.blocks));
+    block = static_cast<int>(left - static_cast<int64_t>(unit) * sp.blocks);
+    __syncthreads();
+  } else {
+    b = static_cast<int>(blockIdx.x / static_cast<unsigned>(a.units));
+    unit = static_cast<int>(blockIdx.x) - b * a.units;
+    sp = span_of(a, b);
   }
-  int unit = static_cast<int>(left / sp.blocks), block = static_cast<int>(left - static_cast<int64_t>(unit) * sp.blocks);
   bool continued = block > 0;
-  __syncthreads();
 
   while (true) {
-    const int blocks = static_cast<int>(min(static_cast<int64_t>(sp.blocks - block), end - at));
+    const int blocks = kDealt ? static_cast<int>(min(static_cast<int64_t>(sp.blocks - block), end - at)) : sp.blocks;
     const int hk = unit / a.row_tiles, first_row = (unit - hk * a.row_tiles) * kRows;
     const int rows = min(kRows, rows_of_heads - first_row);
     const int64_t row0 = static_cast<int64_t>(b) * a.d.H + hk * a.d.G + first_row;  // of q and y
@@ -209,30 +240,56 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void step_kernel(const
     for (int c = 0; c < T::kCols; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = kNone, l = 0.f;
 
-    for (int first = sp.base + block * kBlock + wave * kTile; first < min(sp.len, sp.base + (block + blocks) * kBlock); first += kBlock) {
-      T t;
-      // pages of tokens n and 16 + n of the tile (tokens that aren't seen: of the nearest one that is)
-      int page[2];
-      uint32_t seen = 0xffffffffu;
-      {
-        uint32_t gone = 0;
+    // pages of tokens n and 16 + n of a tile (tokens that aren't seen: of the nearest one that is)
+    struct Pages {
+      int of[2];
+    };
+    auto pages_of = [&](int first) {
+      Pages p;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int token = min(max(first + 16 * h + n, sp.lo), sp.len - 1);
-          page[h] = table[token >> a.d.lg_page];
-          const bool bad = static_cast<unsigned>(page[h]) >= static_cast<unsigned>(a.d.npages);
-          gone |= static_cast<uint32_t>(__ballot(bad) & 0xffffu) << (16 * h);
-          if (bad) page[h] = 0;
-          t.load_key(h, kh + page[h] * page_bytes + (token & page_mask) * bytes, j, bytes);
-        }
-        if (first < sp.lo) seen &= 0xffffffffu << (sp.lo - first);
-        if (first + kTile > sp.len) seen &= 0xffffffffu >> (first + kTile - sp.len);
-        seen &= ~gone;
+      for (int h = 0; h < 2; ++h) p.of[h] = table[min(max(first + 16 * h + n, sp.lo), sp.len - 1) >> a.d.lg_page];
+      return p;
+    };
+    auto there = [&](int page) { return static_cast<unsigned>(page) < static_cast<unsigned>(a.d.npages); };
+    auto load_keys = [&](typename T::Keys &keys, int first, const Pages &p) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int token = min(max(first + 16 * h + n, sp.lo), sp.len - 1);
+        T::load_key(keys, h, kh + (there(p.of[h]) ? p.of[h] : 0) * page_bytes + (token & page_mask) * bytes, j, bytes);
+      }
+    };
+    int first = sp.base + block * kBlock + wave * kTile;
+    const int last = min(sp.len, sp.base + (block + blocks) * kBlock);
+    typename T::Keys keys_ahead;
+    Pages pages_ahead, pages_next;
+    if (kAhead && first < last) {
+      pages_ahead = pages_of(first);
+      load_keys(keys_ahead, first, pages_ahead);
+      pages_next = pages_of(first + kWaves * kTile);
+    }
+    for (; first < last; first += kWaves * kTile) {
+      T t;
+      typename T::Keys keys;
+      Pages pages;
+      if (kAhead) {
+        keys = keys_ahead;
+        pages = pages_ahead;
+      } else {
+        pages = pages_of(first);
+        load_keys(keys, first, pages);
+      }
+      uint32_t seen = 0xffffffffu;
+      if (first < sp.lo) seen &= 0xffffffffu << (sp.lo - first);
+      if (first + kTile > sp.len) seen &= 0xffffffffu >> (first + kTile - sp.len);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        seen &= ~(static_cast<uint32_t>(__ballot(!there(pages.of[h])) & 0xffffu) << (16 * h));
+        if (!there(pages.of[h])) pages.of[h] = 0;
       }
       if (a.d.lg_page >= 2) {  // four neighbouring tokens of an aligned tile are on one page
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int64_t where = __shfl(page[h], 4 * j) * page_bytes;
+          const int64_t where = __shfl(pages.of[h], 4 * j) * page_bytes;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int token = min(max(first + 16 * h + 4 * j + r, sp.lo), sp.len - 1);
@@ -246,13 +303,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void step_kernel(const
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int token = min(max(first + 16 * h + 4 * j + r, sp.lo), sp.len - 1);
-            t.load_value(4 * h + r, vh + __shfl(page[h], 4 * j + r) * page_bytes + (token & page_mask) * bytes, n, bytes);
+            t.load_value(4 * h + r, vh + __shfl(pages.of[h], 4 * j + r) * page_bytes + (token & page_mask) * bytes, n, bytes);
           }
+      }
+      if (kAhead) {  // (behind the last tile: the last token's, not used)
+        load_keys(keys_ahead, first + kWaves * kTile, pages_next);
+        pages_ahead = pages_next;
+        pages_next = pages_of(first + 2 * kWaves * kTile);
       }
       f32x4 s[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        s[h] = t.scores(h, query);
+        s[h] = T::scores(keys, h, query);
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[h][r] *= a.scale_log2;
       }
@@ -302,9 +364,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void step_kernel(const
         *reinterpret_cast<f32x4 *>(&lds.join.o[wave][n][T::column(c, 4 * j + r)]) = q;
       }
     __syncthreads();
-    const bool whole = blocks == sp.blocks;
+    const bool whole = !kDealt || blocks == sp.blocks;
     const int slot_row = (2 * static_cast<int>(blockIdx.x) + (continued ? 0 : 1)) * kRows;
-    for (int e = threadIdx.x; e < rows * (DP / 4); e += kThreads) {
+    for (int e = threadIdx.x; e < rows * (DP / 4); e += 64 * kWaves) {
       const int row = e / (DP / 4), col = (e % (DP / 4)) * 4;
       if (col >= a.d.D) continue;
       float top = kNone, f[kWaves], sum = 0.f;
@@ -338,7 +400,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void step_kernel(const
       }
     }
     at += blocks;
-    if (at >= end) break;
+    if (!kDealt || at >= end) break;
     __syncthreads();
     block = 0;
     continued = false;
@@ -361,7 +423,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int ro
   id /= static_cast<unsigned>(col_cuts * row_cuts);
   const int b = static_cast<int>(id / static_cast<unsigned>(a.units)), unit = static_cast<int>(id) - b * a.units;
   count_blocks(a, prefix);
-  const int64_t total = prefix.at[kDealers] * a.units, run = (total + kWorkgroups - 1) >> kLgWorkgroups;
+  const int64_t total = uniform(prefix.at[kDealers]) * a.units, run = run_of(a, total);
   const int share = share_of(a.d.B);
   int64_t before = prefix.at[b / share];
   for (int i = b / share * share; i < b; ++i) before += span_of(a, i).blocks;
@@ -373,8 +435,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int ro
   int64_t begin = 0;
   if (sp.blocks > 0) {
     begin = before * a.units + static_cast<int64_t>(unit) * sp.blocks;
-    first = static_cast<int>(begin / run);
-    last = static_cast<int>((begin + sp.blocks - 1) / run);
+    first = static_cast<int>(quotient64(begin, run));
+    last = static_cast<int>(quotient64(begin + sp.blocks - 1, run));
     if (first == last) return;  // finished where it was computed
   }
   const int items = rows * cols, abreast = max(1, kThreads / items);
@@ -428,30 +490,46 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int ro
   }
 }
 
+// Whether work is dealt, from the most tokens that a sequence can have: half of them are reckoned with.  In us, with 32 heads over
+// 8 of 128, bf16: a unit to a workgroup takes 4 and its bytes at 52 GB/s, or all units' at 6 TB/s; dealing takes 12 and all units'
+// bytes at 5.2 TB/s.  One sequence of 518 tokens: 9.1 and 12.6 dealt; of 2000: 22 and 13; 16 of 2000: 24 and 36.  A sequence of
+// more than a MiB a key head, 20 us for a workgroup, may be the only one that long: then work is dealt.
+bool dealt(const AttnDims &d) {
+  const double longest = 2.0 * d.capacity() * d.D * (d.bf16 ? 2 : 4), all = 0.5 * longest * d.B * units_of(d);
+  if (longest > 1048576.0) return true;
+  return 4.0 + std::max(longest / 52.0e3, all / 6.0e6) > 12.0 + all / 5.2e6;
+}
+
+template <bool kBf16, int DP>
+void launch_step(const StepArgs &a, hipStream_t stream) {
+  constexpr int kWide = DP <= 128 ? 8 : 4;  // waves: two a SIMD, where registers allow
+  if (dealt(a.d))
+    hipLaunchKernelGGL((step_kernel<kBf16, DP, kThreads / 64, true>), dim3(a.workgroups), dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((step_kernel<kBf16, DP, kWide, false>), dim3(static_cast<unsigned>(a.units) * a.d.B), dim3(64 * kWide), 0, stream, a);
+}
+
 template <bool kBf16>
 hipError_t launch(const StepArgs &a, hipStream_t stream) {
-  const dim3 grid(kWorkgroups), threads(kThreads);
-  if (a.d.D <= 64)
-    hipLaunchKernelGGL((step_kernel<kBf16, 64>), grid, threads, 0, stream, a);
-  else if (a.d.D <= 128)
-    hipLaunchKernelGGL((step_kernel<kBf16, 128>), grid, threads, 0, stream, a);
-  else
-    hipLaunchKernelGGL((step_kernel<kBf16, 256>), grid, threads, 0, stream, a);
-  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (a.d.D <= 64) launch_step<kBf16, 64>(a, stream);
+  else if (a.d.D <= 128) launch_step<kBf16, 128>(a, stream);
+  else launch_step<kBf16, 256>(a, stream);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess || !dealt(a.d)) return e;
   // Few units have many parts each, up to one of every workgroup: a workgroup for 32 values of a head.
   const unsigned units = static_cast<unsigned>(a.units) * a.d.B;
   const int tile_rows = a.d.G < kRows ? a.d.G : kRows, all_cols = a.d.D / 4;
   const bool few = units < kFewUnits;
   const int rows = few ? 1 : tile_rows, cols = few && all_cols > 8 ? 8 : all_cols;
   const int row_cuts = (tile_rows + rows - 1) / rows, col_cuts = (all_cols + cols - 1) / cols;
-  hipLaunchKernelGGL(join_kernel<kBf16>, dim3(units * row_cuts * col_cuts), threads, 0, stream, a, rows, cols, row_cuts, col_cuts);
+  hipLaunchKernelGGL(join_kernel<kBf16>, dim3(units * row_cuts * col_cuts), dim3(kThreads), 0, stream, a, rows, cols, row_cuts, col_cuts);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t attn_step_workspace_bytes(const AttnDims &d) {
-  return (static_cast<size_t>(2 * kWorkgroups * kRows) * (d.D + 4) * 4 + 255) / 256 * 256;
+  if (!dealt(d)) return 256;
+  return (static_cast<size_t>(2 * kMostWorkgroups * kRows) * (d.D + 4) * 4 + 255) / 256 * 256;
 }
 
 hipError_t launch_attn_step(const AttnDims &d, const int32_t *lens, const int32_t *table, const void *q, const void *k_cache,
@@ -465,8 +543,9 @@ hipError_t launch_attn_step(const AttnDims &d, const int32_t *lens, const int32_
   a.y = y;
   a.part = static_cast<float *>(workspace);
   a.d = d;
-  a.row_tiles = (d.G + kRows - 1) / kRows;
-  a.units = d.Hk * a.row_tiles;
+  a.row_tiles = row_tiles_of(d);
+  a.units = units_of(d);
+  a.workgroups = workgroups_of(d.bf16, d.D <= 64 ? 64 : d.D <= 128 ? 128 : 256);
   a.scale_log2 = scale * 1.44269504f;
   return d.bf16 ? launch<true>(a, stream) : launch<false>(a, stream);
 }

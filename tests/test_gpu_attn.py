@@ -77,10 +77,11 @@ LENGTHS = [[1], [0], [2, 0, 31], [32, 33, 63, 64, 65], [127, 128, 129, 500], [10
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("heads", HEADS, ids=lambda h: "x".join(map(str, h)))
 def test_step_matches_oracle(ssd, heads, io):
-    for i, lengths in enumerate(LENGTHS):
-        s = make(lengths, *heads, io, seed=i)
+    for i, lengths in enumerate(LENGTHS + LENGTHS):
+        # (a wide page table: sequences might be long, and work is dealt to the workgroups by length)
+        s = make(lengths, *heads, io, seed=i, more_pages=0 if i < len(LENGTHS) else -(-600000 // heads[2] // heads[3]))
         for window in (0, 1, 40):
-            print("step", heads, io, lengths, window, flush=True)
+            print("step", heads, io, lengths, window, s["table"].shape[1], flush=True)
             y = run_step(ssd, s, window=window)
             assert_close(y, block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], window=window), TOL[io], "step")
 
@@ -120,7 +121,10 @@ def test_many_sequences(ssd):
     """More sequences than a wave, and than a workgroup, has lanes; most are short, some are empty."""
     lengths = [(i * 7) % 90 for i in range(700)]
     s = make(lengths, 2, 1, 64, 16, "bf16", seed=32)
-    assert_close(run_step(ssd, s), block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"]), TOL["bf16"], "step")
+    ref = block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"])
+    assert_close(run_step(ssd, s), ref, TOL["bf16"], "step")
+    s["table"] = torch.cat((s["table"], torch.full((700, 1000), -1, dtype=torch.int32)), dim=1)
+    assert_close(run_step(ssd, s), ref, TOL["bf16"], "step, dealt")
     new = [min(n, (i * 5) % 4) for i, n in enumerate(lengths)]
     s = make(lengths, 2, 1, 64, 16, "bf16", new=new, seed=33)
     ref = block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], s["cu"])
