@@ -17,8 +17,9 @@ namespace {
 
 using namespace block;
 
-constexpr int kMostTokens = 16;        // a workgroup
-constexpr int kManyItems = 256 * 2048;  // pieces that are a workgroup of one each for 2048
+constexpr int kBatch = 2;        // tokens whose pieces a thread has on their way at a time
+constexpr int kMostTokens = 4;   // a workgroup
+constexpr int kFewWorkgroups = 2048;  // more take several tokens each
 
 struct AppendArgs {
   const void *src[3];      // q, k, v
@@ -30,7 +31,6 @@ struct AppendArgs {
   int head_pieces;         // pieces of a head
   uint32_t inv_head_pieces;
   int row_pieces;          // pieces of a token: queries (if any), keys, values
-  uint32_t inv_row_pieces;
   int q_heads;             // 0: no queries
   int run;                 // tokens a workgroup
 };
@@ -75,77 +75,97 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
   using E = Element<kBf16>;
   constexpr int W = 16 / sizeof(E);
   __shared__ Place place[kMostTokens];
-  const int first_token = blockIdx.x * a.run, tokens = min(a.run, a.d.T - first_token), items = tokens * a.row_pieces;
+  const int first_token = blockIdx.x * a.run, tokens = min(a.run, a.d.T - first_token);
   if (static_cast<int>(threadIdx.x) < tokens) {
     const Token t = find_token(a.d, a.cu, a.lens, first_token + threadIdx.x);
     place[threadIdx.x] = {t.pos, t.pos < 0 ? -1 : slot_of(a.d, a.table, t.seq, t.pos, 0)};
   }
   __syncthreads();
-  const int half = a.rope.half;
-  for (int item = blockIdx.y * 256 + threadIdx.x; item < items; item += gridDim.y * 256) {
-    const int local = quotient(item, a.row_pieces, a.inv_row_pieces), idx = item - local * a.row_pieces, token = first_token + local;
-    const Place at = place[local];
-    int head = quotient(idx, a.head_pieces, a.inv_head_pieces);
-    const int first = (idx - head * a.head_pieces) * W;
-    // which of q, k, v
-    int what = 0;
-    if (head >= a.q_heads) {
-      head -= a.q_heads;
-      what = 1;
-      if (head >= a.d.Hk) {
-        head -= a.d.Hk;
-        what = 2;
-      }
+  // this thread's piece of a token: which of q, k, v, its head and first value
+  const int idx = blockIdx.y * 256 + threadIdx.x;
+  if (idx >= a.row_pieces) return;
+  int head = quotient(idx, a.head_pieces, a.inv_head_pieces), what = 0;
+  const int first = (idx - head * a.head_pieces) * W;
+  if (head >= a.q_heads) {
+    head -= a.q_heads;
+    what = 1;
+    if (head >= a.d.Hk) {
+      head -= a.d.Hk;
+      what = 2;
     }
-    if (at.pos < 0 || (what > 0 && at.slot < 0)) continue;
-    E *const dst = what == 0 ? static_cast<E *>(a.q_out) + (static_cast<int64_t>(token) * a.d.H + head) * a.d.D + first
-                             : static_cast<E *>(a.cache[what - 1]) + (at.slot + (static_cast<int64_t>(head) << a.d.lg_page)) * a.d.D + first;
-    const E *const src = static_cast<const E *>(a.src[what]) + token * a.stride[what] + static_cast<int64_t>(head) * a.d.D;
-    u32x4 q = *reinterpret_cast<const u32x4 *>(src + first);
-    if (what < 2 && first < 2 * half) {
-      const float *const cs = a.rope.cos + static_cast<int64_t>(at.pos) * half, *const sn = a.rope.sin + static_cast<int64_t>(at.pos) * half;
-      float v[W], r[W];
-      unpack<kBf16>(q, v);
-      if (kWhole && !a.rope.interleaved) {
-        const bool second = first >= half;
-        const int pair = second ? first - half : first;
-        float o[W], c[W], s[W];
-        unpack<kBf16>(*reinterpret_cast<const u32x4 *>(src + (second ? first - half : first + half)), o);
-        load_rope<W>(cs + pair, c);
-        load_rope<W>(sn + pair, s);
+  }
+  const int64_t stride = a.stride[what];
+  const E *const src = static_cast<const E *>(a.src[what]) + first_token * stride + static_cast<int64_t>(head) * a.d.D;
+  E *const out = what == 0 ? static_cast<E *>(a.q_out) + (static_cast<int64_t>(first_token) * a.d.H + head) * a.d.D + first
+                           : static_cast<E *>(a.cache[what - 1]) + (static_cast<int64_t>(head) << a.d.lg_page) * a.d.D + first;
+  const int64_t out_stride = static_cast<int64_t>(a.d.H) * a.d.D;
+  const int half = a.rope.half;
+  const bool rotated = what < 2 && first < 2 * half, second = !a.rope.interleaved && first >= half;
+  const int partner = second ? first - half : first + half, pair = a.rope.interleaved ? first / 2 : second ? first - half : first;
+  // kBatch tokens at a time: asked for together, then written
+  for (int token0 = 0; token0 < tokens; token0 += kBatch) {
+    u32x4 q[kBatch], other[kBatch];
+    Place at[kBatch];
 #pragma unroll
-        for (int i = 0; i < W; ++i) r[i] = fmaf(v[i], c[i], second ? o[i] * s[i] : -o[i] * s[i]);
-      } else if (kWhole) {
-        float c[W / 2], s[W / 2];
-        load_rope<W / 2>(cs + first / 2, c);
-        load_rope<W / 2>(sn + first / 2, s);
+    for (int k = 0; k < kBatch; ++k) {
+      at[k].pos = -1;
+      if (token0 + k >= tokens) continue;
+      at[k] = place[token0 + k];
+      if (at[k].pos < 0 || (what > 0 && at[k].slot < 0)) {
+        at[k].pos = -1;
+        continue;
+      }
+      const E *const row = src + (token0 + k) * stride;
+      q[k] = *reinterpret_cast<const u32x4 *>(row + first);
+      if (kWhole && rotated && !a.rope.interleaved) other[k] = *reinterpret_cast<const u32x4 *>(row + partner);
+    }
 #pragma unroll
-        for (int i = 0; i < W; i += 2) {
-          r[i] = fmaf(v[i], c[i / 2], -v[i + 1] * s[i / 2]);
-          r[i + 1] = fmaf(v[i + 1], c[i / 2], v[i] * s[i / 2]);
-        }
-      } else {
+    for (int k = 0; k < kBatch; ++k) {
+      if (at[k].pos < 0) continue;
+      if (rotated) {
+        const float *const cs = a.rope.cos + static_cast<int64_t>(at[k].pos) * half, *const sn = a.rope.sin + static_cast<int64_t>(at[k].pos) * half;
+        float v[W], r[W];
+        unpack<kBf16>(q[k], v);
+        if (kWhole && !a.rope.interleaved) {
+          float o[W], c[W], s[W];
+          unpack<kBf16>(other[k], o);
+          load_rope<W>(cs + pair, c);
+          load_rope<W>(sn + pair, s);
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const int c = first + i;
-          r[i] = v[i];
-          if (c < 2 * half) {
-            const bool second = a.rope.interleaved ? (c & 1) : c >= half;
-            const int pair = a.rope.interleaved ? c >> 1 : second ? c - half : c;
-            const float o = value(src[a.rope.interleaved ? c ^ 1 : second ? c - half : c + half]);
-            r[i] = fmaf(v[i], cs[pair], second ? o * sn[pair] : -o * sn[pair]);
+          for (int i = 0; i < W; ++i) r[i] = fmaf(v[i], c[i], second ? o[i] * s[i] : -o[i] * s[i]);
+        } else if (kWhole) {
+          float c[W / 2], s[W / 2];
+          load_rope<W / 2>(cs + pair, c);
+          load_rope<W / 2>(sn + pair, s);
+#pragma unroll
+          for (int i = 0; i < W; i += 2) {
+            r[i] = fmaf(v[i], c[i / 2], -v[i + 1] * s[i / 2]);
+            r[i + 1] = fmaf(v[i + 1], c[i / 2], v[i] * s[i / 2]);
+          }
+        } else {
+          const E *const row = src + (token0 + k) * stride;
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            const int c = first + i;
+            r[i] = v[i];
+            if (c < 2 * half) {
+              const bool b = a.rope.interleaved ? (c & 1) : c >= half;  // the second of its pair
+              const int p = a.rope.interleaved ? c >> 1 : b ? c - half : c;
+              const float o = value(row[a.rope.interleaved ? c ^ 1 : b ? c - half : c + half]);
+              r[i] = fmaf(v[i], cs[p], b ? o * sn[p] : -o * sn[p]);
+            }
           }
         }
-      }
-      if constexpr (kBf16) {
+        if constexpr (kBf16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = pack2(r[2 * i], r[2 * i + 1]);
-      } else {
+          for (int i = 0; i < 4; ++i) q[k][i] = pack2(r[2 * i], r[2 * i + 1]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = __float_as_uint(r[i]);
+          for (int i = 0; i < 4; ++i) q[k][i] = __float_as_uint(r[i]);
+        }
       }
+      *reinterpret_cast<u32x4 *>(out + (what == 0 ? (token0 + k) * out_stride : at[k].slot * a.d.D)) = q[k];
     }
-    *reinterpret_cast<u32x4 *>(dst) = q;
   }
 }
 
@@ -173,11 +193,9 @@ hipError_t launch_attn_append(const AttnDims &d, const Rope &rope, const int32_t
   a.head_pieces = d.D / (d.bf16 ? 8 : 4);
   a.inv_head_pieces = inverse_of(a.head_pieces);
   a.row_pieces = (a.q_heads + 2 * d.Hk) * a.head_pieces;
-  a.inv_row_pieces = inverse_of(a.row_pieces);
-  // a few tokens a workgroup where there are workgroups enough, and one item a thread where there are not
-  const int64_t items = static_cast<int64_t>(d.T) * a.row_pieces;
-  a.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMostTokens, items / kManyItems)));
-  const dim3 grid((d.T + a.run - 1) / a.run, a.run > 1 ? 1 : (a.row_pieces + 255) / 256);
+  const int parts = (a.row_pieces + 255) / 256;
+  a.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMostTokens, static_cast<int64_t>(d.T) * parts / kFewWorkgroups)));
+  const dim3 grid((d.T + a.run - 1) / a.run, parts);
   const int width = rope.interleaved ? 2 * rope.half : rope.half;
   const bool whole = width % (d.bf16 ? 8 : 4) == 0;
   if (d.bf16 && whole)

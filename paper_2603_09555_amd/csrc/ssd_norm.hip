@@ -46,13 +46,13 @@ __device__ __forceinline__ void combine(float v[kPiece], float s[kPiece], float 
 }
 
 // kThreads threads a unit, kHold pieces a thread in registers (0: units too wide for that are read a second time, from the
-// caches).  Units of one wave share a workgroup of four.
+// caches).  Units of a wave or less share a workgroup of four waves.
 template <typename Io, typename Side, int kMode, int kThreads, int kHold>
 __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(const NormArgs a) {
-  constexpr int kBlock = kThreads < 256 ? 256 : kThreads, kUnits = kBlock / kThreads, kWaves = kThreads / 64;
+  constexpr int kBlock = kThreads < 256 ? 256 : kThreads, kUnits = kBlock / kThreads, kWaves = kThreads < 64 ? 1 : kThreads / 64;
   const int t = threadIdx.x % kThreads;
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * kUnits + threadIdx.x / kThreads;
-  if (unit >= a.units) return;  // (a whole wave; workgroups of several waves a unit have one unit)
+  if (unit >= a.units) return;  // (all threads of a unit; workgroups of several waves a unit have one unit)
   int64_t row = unit;
   int first = 0;
   if (a.groups > 1) {
@@ -103,7 +103,8 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(c
       for (int i = 0; i < kPiece; ++i) sum = fmaf(v[0][i], v[0][i], sum);
     }
   }
-  sum = wave_sum(sum);
+#pragma unroll
+  for (int d = (kThreads < 64 ? kThreads : 64) / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   if (kWaves > 1) {
     __shared__ float part[kWaves];
     if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = sum;
@@ -137,19 +138,28 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(c
   }
 }
 
+template <typename Io, typename Side, int kMode, int kThreads, int kHold>
+hipError_t launch_shape(const NormArgs &a, hipStream_t stream) {
+  constexpr int kBlock = kThreads < 256 ? 256 : kThreads, kUnits = kBlock / kThreads;
+  hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, kThreads, kHold>), dim3(static_cast<unsigned>((a.units + kUnits - 1) / kUnits)), dim3(kBlock), 0,
+                     stream, a);
+  return hipGetLastError();
+}
+
+// Threads and pieces a thread by the unit's width: no more registers than the pieces need, which leave room for other units'
+// requests (16384 rows of 5120 bf16 values: 132 us with four pieces a thread, of which two and a half are there, 100 with three),
+// and no wave with nothing to do.
 template <typename Io, typename Side, int kMode>
 hipError_t launch_mode(const NormArgs &a, hipStream_t stream) {
   const int pieces = (a.n + kPiece - 1) / kPiece;
-  const dim3 one(static_cast<unsigned>(a.units)), four(static_cast<unsigned>((a.units + 3) / 4));
-  if (pieces <= 64)
-    hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, 64, 1>), four, dim3(256), 0, stream, a);
-  else if (pieces <= 256)
-    hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, 256, 1>), one, dim3(256), 0, stream, a);
-  else if (pieces <= 1024)
-    hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, 256, 4>), one, dim3(256), 0, stream, a);
-  else
-    hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, 1024, 0>), one, dim3(1024), 0, stream, a);
-  return hipGetLastError();
+  if (pieces <= 16) return launch_shape<Io, Side, kMode, 16, 1>(a, stream);
+  if (pieces <= 64) return launch_shape<Io, Side, kMode, 64, 1>(a, stream);
+  if (pieces <= 256) return launch_shape<Io, Side, kMode, 256, 1>(a, stream);
+  if (pieces <= 512) return launch_shape<Io, Side, kMode, 256, 2>(a, stream);
+  if (pieces <= 768) return launch_shape<Io, Side, kMode, 256, 3>(a, stream);
+  if (pieces <= 1024) return launch_shape<Io, Side, kMode, 512, 2>(a, stream);
+  if (pieces <= 2048) return launch_shape<Io, Side, kMode, 512, 4>(a, stream);
+  return launch_shape<Io, Side, kMode, 1024, 0>(a, stream);
 }
 
 }  // namespace
