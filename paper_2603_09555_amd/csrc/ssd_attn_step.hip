@@ -36,11 +36,17 @@ constexpr int kMostWorkgroups = 1024;
 constexpr unsigned kFewUnits = 256;
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
 
+// The workgroups that have blocks of a unit.  They write it down, so that the joining launch need not deal again.
+struct Spread {
+  int first, last;
+};
+
 struct StepArgs {
   const int32_t *lens, *table;
   const void *q, *k, *v;
   void *y;
   float *part;       // per workgroup two slots of kRows x (D + 2): O, m, l of a unit that began before its run, and of its last one
+  Spread *spread;    // of each sequence's units
   AttnDims d;
   int row_tiles;     // of 16 heads, of a key head's heads
   int units;         // of a sequence
@@ -61,10 +67,6 @@ __device__ __forceinline__ Span span_of(const StepArgs &a, int b) {
   s.base = s.lo & ~(kTile - 1);
   s.blocks = (s.len - s.base + kBlock - 1) / kBlock;
   return s;
-}
-
-__device__ __forceinline__ void count_blocks(const StepArgs &a, Prefix &s) {
-  count_blocks(s, a.d.B, [&](int b) { return span_of(a, b).blocks; });
 }
 
 // Exchanges halves: the low (or high) 16 bits of two registers.
@@ -191,26 +193,43 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
   const int page_mask = (1 << a.d.lg_page) - 1;
 
   // the run of this workgroup, and where it begins
-  int64_t at = 0, end = 0;
+  int64_t left_of_run = 0;
   int b, unit, block = 0;
   Span sp;
   if (kDealt) {
-    count_blocks(a, lds.prefix);
-    const int64_t total = uniform(lds.prefix.at[kDealers]) * a.units, run = run_of(a, total);
-    at = blockIdx.x * run;
-    end = min(total, at + run);
-    if (at >= end) return;
-    const int dealer = dealer_of(lds.prefix, at, a.units);
-    b = dealer * share_of(a.d.B);
-    int64_t left = uniform(at - lds.prefix.at[dealer] * a.units);
-    sp = span_of(a, b);
-    while (left >= static_cast<int64_t>(sp.blocks) * a.units) {
-      left -= static_cast<int64_t>(sp.blocks) * a.units;
-      sp = span_of(a, ++b);
+    int64_t left;
+    if (a.d.B <= 64) {  // a wave has them all
+      int blocks = lane < a.d.B ? span_of(a, lane).blocks : 0, sum = blocks;  // (2^24 each at most)
+#pragma unroll
+      for (int k = 1; k < 64; k <<= 1) {
+        const int o = __shfl_up(sum, k);
+        if (lane >= k) sum += o;
+      }
+      const int64_t total = static_cast<int64_t>(__builtin_amdgcn_readlane(sum, 63)) * a.units;
+      const int64_t run = run_of(a, total), at = blockIdx.x * run;
+      left_of_run = min(run, total - at);
+      if (left_of_run <= 0) return;
+      b = __builtin_popcountll(__ballot(static_cast<int64_t>(sum) * a.units <= at));
+      left = at - static_cast<int64_t>(__builtin_amdgcn_readlane(sum - blocks, b)) * a.units;
+      sp = span_of(a, b);
+    } else {
+      count_blocks(lds.prefix, a.d.B, [&](int i) { return span_of(a, i).blocks; });
+      const int64_t total = uniform(lds.prefix.at[kDealers]) * a.units;
+      const int64_t run = run_of(a, total), at = blockIdx.x * run;
+      left_of_run = min(run, total - at);
+      if (left_of_run <= 0) return;
+      const int dealer = dealer_of(lds.prefix, at, a.units);
+      b = dealer * share_of(a.d.B);
+      left = uniform(at - lds.prefix.at[dealer] * a.units);
+      sp = span_of(a, b);
+      while (left >= static_cast<int64_t>(sp.blocks) * a.units) {
+        left -= static_cast<int64_t>(sp.blocks) * a.units;
+        sp = span_of(a, ++b);
+      }
+      __syncthreads();
     }
     unit = static_cast<int>(quotient64(left, sp.blocks));
     block = static_cast<int>(left - static_cast<int64_t>(unit) * sp.blocks);
-    __syncthreads();
   } else {
     b = static_cast<int>(blockIdx.x / static_cast<unsigned>(a.units));
     unit = static_cast<int>(blockIdx.x) - b * a.units;
@@ -219,7 +238,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
   bool continued = block > 0;
 
   while (true) {
-    const int blocks = kDealt ? static_cast<int>(min(static_cast<int64_t>(sp.blocks - block), end - at)) : sp.blocks;
+    const int blocks = kDealt ? static_cast<int>(min(static_cast<int64_t>(sp.blocks - block), left_of_run)) : sp.blocks;
     const int hk = unit / a.row_tiles, first_row = (unit - hk * a.row_tiles) * kRows;
     const int rows = min(kRows, rows_of_heads - first_row);
     const int64_t row0 = static_cast<int64_t>(b) * a.d.H + hk * a.d.G + first_row;  // of q and y
@@ -365,6 +384,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
       }
     __syncthreads();
     const bool whole = !kDealt || blocks == sp.blocks;
+    if (kDealt && threadIdx.x == 0) {
+      Spread &spread = a.spread[static_cast<int64_t>(b) * a.units + unit];
+      if (!continued) spread.first = static_cast<int>(blockIdx.x);
+      if (block + blocks == sp.blocks) spread.last = static_cast<int>(blockIdx.x);
+    }
     const int slot_row = (2 * static_cast<int>(blockIdx.x) + (continued ? 0 : 1)) * kRows;
     for (int e = threadIdx.x; e < rows * (DP / 4); e += 64 * kWaves) {
       const int row = e / (DP / 4), col = (e % (DP / 4)) * 4;
@@ -399,8 +423,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
         }
       }
     }
-    at += blocks;
-    if (!kDealt || at >= end) break;
+    left_of_run -= blocks;
+    if (!kDealt || left_of_run <= 0) break;
     __syncthreads();
     block = 0;
     continued = false;
@@ -416,27 +440,19 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
 // them where there are many units), and as many of the parts at a time as it has threads for.
 template <bool kBf16>
 __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int rows, int cols, int row_cuts, int col_cuts) {
-  __shared__ Prefix prefix;
   __shared__ float got[kThreads][6];
   unsigned id = blockIdx.x;
   const int col_cut = static_cast<int>(id % col_cuts), row_cut = static_cast<int>(id / col_cuts % row_cuts);
   id /= static_cast<unsigned>(col_cuts * row_cuts);
   const int b = static_cast<int>(id / static_cast<unsigned>(a.units)), unit = static_cast<int>(id) - b * a.units;
-  count_blocks(a, prefix);
-  const int64_t total = uniform(prefix.at[kDealers]) * a.units, run = run_of(a, total);
-  const int share = share_of(a.d.B);
-  int64_t before = prefix.at[b / share];
-  for (int i = b / share * share; i < b; ++i) before += span_of(a, i).blocks;
-  const Span sp = span_of(a, b);
+  const Spread spread = a.spread[id];
   const int hk = unit / a.row_tiles, first_row = (unit - hk * a.row_tiles) * kRows;
   const int64_t row0 = static_cast<int64_t>(b) * a.d.H + hk * a.d.G + first_row;
   const int row_end = min(min(kRows, a.d.G - first_row), (row_cut + 1) * rows), col_end = min(a.d.D / 4, (col_cut + 1) * cols);
   int first = 0, last = -1;
-  int64_t begin = 0;
-  if (sp.blocks > 0) {
-    begin = before * a.units + static_cast<int64_t>(unit) * sp.blocks;
-    first = static_cast<int>(quotient64(begin, run));
-    last = static_cast<int>(quotient64(begin + sp.blocks - 1, run));
+  if (span_of(a, b).blocks > 0) {  // (otherwise nobody has been there)
+    first = spread.first;
+    last = spread.last;
     if (first == last) return;  // finished where it was computed
   }
   const int items = rows * cols, abreast = max(1, kThreads / items);
@@ -449,7 +465,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int ro
     if (mine) {
 #pragma unroll 4
       for (int w = first + lane; w <= last; w += abreast) {
-        const int slot_row = (2 * w + (begin >= w * run ? 1 : 0)) * kRows + row;
+        const int slot_row = (2 * w + (w == first ? 1 : 0)) * kRows + row;
         const float *part = a.part + static_cast<int64_t>(slot_row) * (a.d.D + 4);
         const float m = part[a.d.D], l = part[a.d.D + 1];
         const f32x4 o = *reinterpret_cast<const f32x4 *>(part + col);
@@ -491,9 +507,10 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int ro
 }
 
 // Whether work is dealt, from the most tokens that a sequence can have: half of them are reckoned with.  In us, with 32 heads over
-// 8 of 128, bf16: a unit to a workgroup takes 4 and its bytes at 52 GB/s, or all units' at 6 TB/s; dealing takes 12 and all units'
-// bytes at 5.2 TB/s.  One sequence of 518 tokens: 9.1 and 12.6 dealt; of 2000: 22 and 13; 16 of 2000: 24 and 36.  A sequence of
-// more than a MiB a key head, 20 us for a workgroup, may be the only one that long: then work is dealt.
+// 8 of 128, bf16: a unit to a workgroup takes 4 and its bytes at 52 GB/s, or all units' at 6 TB/s; dealing takes 10 and all units'
+// bytes at 5.2 TB/s, and is charged 2 more, for lengths that are alike lose more by it than uneven ones win.  One sequence of 518
+// tokens: 8.8 and 10.9 dealt; of 2000: 22 and 11; 16 of 2000: 23 and 31.  A sequence of more than a MiB a key head, 20 us for a
+// workgroup, may be the only one that long: then work is dealt.
 bool dealt(const AttnDims &d) {
   const double longest = 2.0 * d.capacity() * d.D * (d.bf16 ? 2 : 4), all = 0.5 * longest * d.B * units_of(d);
   if (longest > 1048576.0) return true;
@@ -525,11 +542,13 @@ hipError_t launch(const StepArgs &a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+size_t part_bytes(const AttnDims &d) { return (static_cast<size_t>(2 * kMostWorkgroups * kRows) * (d.D + 4) * 4 + 255) / 256 * 256; }
+
 }  // namespace
 
 size_t attn_step_workspace_bytes(const AttnDims &d) {
   if (!dealt(d)) return 256;
-  return (static_cast<size_t>(2 * kMostWorkgroups * kRows) * (d.D + 4) * 4 + 255) / 256 * 256;
+  return part_bytes(d) + (static_cast<size_t>(d.B) * units_of(d) * sizeof(Spread) + 255) / 256 * 256;
 }
 
 hipError_t launch_attn_step(const AttnDims &d, const int32_t *lens, const int32_t *table, const void *q, const void *k_cache,
@@ -542,6 +561,7 @@ hipError_t launch_attn_step(const AttnDims &d, const int32_t *lens, const int32_
   a.v = v_cache;
   a.y = y;
   a.part = static_cast<float *>(workspace);
+  a.spread = reinterpret_cast<Spread *>(static_cast<char *>(workspace) + part_bytes(d));
   a.d = d;
   a.row_tiles = row_tiles_of(d);
   a.units = units_of(d);

@@ -86,6 +86,19 @@ def test_step_matches_oracle(ssd, heads, io):
             assert_close(y, block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], window=window), TOL[io], "step")
 
 
+@pytest.mark.parametrize("batch", [64, 65, 257, 700])
+def test_step_many_sequences_dealt(ssd, batch):
+    """More sequences than a wave, or a workgroup, has lanes, many of them empty; the table is wide, so that work is dealt."""
+    lengths = np.random.default_rng(batch).integers(0, 300, batch)
+    lengths[::3] = 0
+    lengths[-1] = 0
+    s = make([int(n) for n in lengths], 6, 2, 64, 16, "bf16", seed=batch, more_pages=700)
+    for window in (0, 100):
+        print("step", batch, window, flush=True)
+        y = run_step(ssd, s, window=window)
+        assert_close(y, block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], window=window), TOL["bf16"], "step")
+
+
 PIECES = [  # new tokens, cached tokens
     ([1], [0]), ([5], [0]), ([0, 3, 0, 0, 70, 1], [9, 0, 0, 5, 130, 64]), ([64, 65, 63], [0, 64, 1]), ([260], [0]), ([7, 129], [1000, 513]),
 ]
