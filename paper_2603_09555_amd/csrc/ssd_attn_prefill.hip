@@ -23,12 +23,15 @@ namespace {
 using namespace block;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kWaveRows = 32, kUnitRows = kWaves * kWaveRows;
-constexpr int kSplitTokens = 512; // a unit is shared by no more workgroups than it has times that
 constexpr int kWorkgroups = 256;  // of eight waves, which fill the GPU
 constexpr int kManyUnits = 768;   // units that four waves each take,
 constexpr int kManyTiles = 16;    // unless they have fewer tiles
 constexpr int kMostSplits = 64;   // of a unit
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
+constexpr int tokens_of_tile(bool bf16) { return bf16 ? 64 : 32; }
+// Tiles that a workgroup at least takes where several share a unit: 1.0 us of work in bf16 a tile and CU with heads of 128 values,
+// 3.5 in fp32.  (12 heads over 4 of 64 in fp32: 512 tokens 42 us with 16 of them, 21 with 4; 1023 tokens 47 and 42.)
+constexpr int least_tiles(int tokens) { return tokens == tokens_of_tile(true) ? 8 : 4; }
 // The running maximum follows a larger one only when that is 2^kSlack times more: until then probabilities are up to 2^kSlack,
 // which costs no accuracy, and O need not be scaled again.
 constexpr float kSlack = 8.f;
@@ -83,7 +86,7 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int u) {
   const int highest = r.pos0 + quotient(r.first_row + r.rows - 1, a.d.G, a.inv_group);
   r.base = (a.d.window > 0 ? max(0, lowest + 1 - a.d.window) : 0) & ~(kTokens - 1);
   r.tiles = highest < 0 ? 0 : (highest + 1 - r.base + kTokens - 1) / kTokens;
-  r.splits = max(1, min(a.splits, (r.tiles * kTokens + kSplitTokens - 1) / kSplitTokens));
+  r.splits = max(1, min(a.splits, (r.tiles + least_tiles(kTokens) - 1) / least_tiles(kTokens)));
   return r;
 }
 
@@ -113,7 +116,6 @@ __device__ __forceinline__ void load_to_lds(const void *wave_from, uint32_t offs
 
 // Geometry of a tile in LDS for head vectors of up to DP values (D are there, the others are zeros): rows of kPieces pieces of 16
 // bytes, in an order that depends on the row so that the reads of either product go to all banks.
-constexpr int tokens_of_tile(bool bf16) { return bf16 ? 64 : 32; }
 template <bool kBf16, int DP>
 struct Geometry {
   static constexpr int kSize = kBf16 ? 2 : 4;
@@ -681,7 +683,7 @@ Plan plan_of(const AttnDims &d) {
   // the same each, and the last CU to begin one decides
   const bool prompts = most_seen <= 2 * static_cast<int64_t>(d.T / d.B);
   double best = 0.0;
-  for (int s = 1; s == 1 || (s <= kMostSplits && (s - 1) * kSplitTokens < most_seen); ++s) {
+  for (int s = 1; s == 1 || (s <= kMostSplits && (s - 1) * least_tiles(tokens_of_tile(d.bf16)) < tiles); ++s) {
     const double longest = static_cast<double>(tiles) / s;
     const double row = prompts ? std::max(longest, units * tiles / 2 / kWorkgroups) + longest / 4 : std::ceil(units * s / kWorkgroups) * longest;
     const double cost = row * tile + (s > 1 ? launch + part * units * s : 0.0);
