@@ -389,7 +389,11 @@ SSD_API ssd_status ssd_norm_residual(int64_t rows, int32_t width, int32_t io_dty
  * appended and not seen.  A new token in front of its sequence's beginning
  * (seq_lens[b] smaller than the number of its new tokens) is not appended and
  * sees nothing.  A token that sees nothing gets y = 0.  What lies in a page
- * behind a sequence's end is never used, whatever its value.
+ * behind a sequence's end is never used, whatever its value, nor are keys that a
+ * token does not see.  Values that it does not see are not used by ssd_attn_step;
+ * in ssd_attn_prefill, where rows share a tile of tokens, those of its own
+ * sequence are multiplied by a probability of zero if they are less than 64
+ * tokens from what it sees, and have to be finite.
  */
 typedef struct {
   int32_t batch;     /* sequences */
@@ -444,7 +448,9 @@ SSD_API ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *
  *   workspace         at least ssd_attn_step_workspace_bytes() bytes, 256-byte
  *                     aligned; its size depends on the shape alone
  * Work is dealt to the workgroups by the lengths as the device holds them, so a
- * captured call follows seq_lens as they grow.
+ * captured call follows seq_lens as they grow.  A call repeats bit for bit; where
+ * a sequence's sum is divided, and with it the last bits of its result, depends
+ * on the lengths of the whole batch.
  * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _WORKSPACE, _HIP.
  */
 SSD_API size_t ssd_attn_step_workspace_bytes(const ssd_attn_shape *shape);
