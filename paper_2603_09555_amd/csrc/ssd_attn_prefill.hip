@@ -7,15 +7,20 @@
 //
 //   S^T (tokens x rows) = K Q^T,   p = 2^(S - m),   O^T (values x rows) += V^T P^T
 //
-// Tiles of K and V (64 tokens; fp32: 32) go through LDS, the next one being on its way while one is worked on.  The first
+// Tiles of K and V (64 tokens; fp32: 32) go through LDS, the next one being on its way while one is worked on.  fp32 is taken apart
+// into three values of bf16 each, and six products stand for one.  The first
 // product leaves a lane with tokens 8i + 4h .. 8i + 4h + 3 (h = lane / 32) of its row; these are what it supplies as the second
-// operand of V^T P^T, whose first operand comes from LDS with the same order of tokens (bf16: by transposing reads).
+// operand of V^T P^T, whose first operand comes from LDS by transposing reads, with the same order of tokens.
 //
 // Where there are few units, several workgroups share one's tokens and leave (m, l, O) in the workspace for a second launch.
+//
+// 32 heads over 8 of 128, bf16: 16384 tokens 2.05 ms, 1070 TFLOP/s of the causal products (the library's large product: 1316); 4096
+// tokens 147 us, 1024 tokens 24 us; 64 tokens behind 32000 51 us.  fp32: see its kernel.
 #include <algorithm>
 #include <cmath>
 
 #include "ssd_attn.hpp"
+#include "ssd_split_bf16.hpp"
 
 namespace ssd {
 namespace {
@@ -30,13 +35,10 @@ constexpr int kMostSplits = 64;   // of a unit
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
 constexpr int tokens_of_tile(bool bf16) { return bf16 ? 64 : 32; }
 // Tiles that a workgroup at least takes where several share a unit: 1.0 us of work in bf16 a tile and CU with heads of 128 values,
-// 3.5 in fp32.  (12 heads over 4 of 64 in fp32: 512 tokens 42 us with 16 of them, 21 with 4; 1023 tokens 47 and 42.)
+// 2.0 in fp32.
 constexpr int least_tiles(int tokens) { return tokens == tokens_of_tile(true) ? 8 : 4; }
-// The running maximum follows a larger one only when that is 2^kSlack times more: until then probabilities are up to 2^kSlack,
-// which costs no accuracy, and O need not be scaled again.
-constexpr float kSlack = 8.f;
-// bf16 does without looking for the largest score of a step: the sum of a lane's probabilities, which is needed anyway, says
-// whether one is too large for the running maximum.
+// There is no search for the largest score of a step: the sum of a lane's probabilities, which is needed anyway, says whether one is
+// too large for the running maximum.  Until then probabilities are up to this, which costs no accuracy, and O need not be scaled again.
 constexpr float kMost = 65536.f;
 
 struct PrefillArgs {
@@ -48,7 +50,7 @@ struct PrefillArgs {
   uint32_t inv_group;
   int units;         // at most, of a key head
   int splits;        // at most, of a unit
-  int groups;        // of waves, a workgroup
+  int groups;        // of waves, a workgroup (bf16)
   float scale_log2;  // scale * log2(e)
 };
 
@@ -93,7 +95,6 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int u) {
 __device__ __forceinline__ f32x16 mfma_bf16(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
 // Transposed LDS read (ds_read_b64_tr_b16): in each group of 16 lanes, lane i names four neighbouring 16-bit values, of row i / 4
 // and columns 4 (i % 4) on, and receives column i of the four rows.
@@ -101,6 +102,14 @@ __device__ __forceinline__ u32x2 lds_transposed(const char *p) {
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uint32_t)(uintptr_t)p));
+}
+
+// The same from a constant offset behind the lane's address.
+__device__ __forceinline__ u32x2 lds_transposed(uint32_t lane_at, int offset) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  typedef __attribute__((address_space(3))) char lds_char;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)lane_at + offset)));
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)); }
@@ -114,21 +123,18 @@ __device__ __forceinline__ void load_to_lds(const void *wave_from, uint32_t offs
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(wave_from), "s"(to) : "m0", "memory");
 }
 
-// Geometry of a tile in LDS for head vectors of up to DP values (D are there, the others are zeros): rows of kPieces pieces of 16
-// bytes, in an order that depends on the row so that the reads of either product go to all banks.
-template <bool kBf16, int DP>
+// Geometry of a bf16 tile in LDS for head vectors of up to DP values (D are there, the others are zeros): rows of kPieces pieces of
+// 16 bytes, in an order that depends on the row so that the reads of either product go to all banks.
+template <int DP>
 struct Geometry {
-  static constexpr int kSize = kBf16 ? 2 : 4;
-  static constexpr int kTokens = tokens_of_tile(kBf16);
-  static constexpr int kRowBytes = DP * kSize, kPieces = kRowBytes / 16;
+  static constexpr int kTokens = tokens_of_tile(true);
+  static constexpr int kRowBytes = 2 * DP, kPieces = kRowBytes / 16;
   static constexpr int kTileBytes = kTokens * kRowBytes;
   static constexpr int kFetch = kTokens * kPieces / kThreads;  // pieces of a tile a thread brings
   // 16 lanes read the same piece of neighbouring rows
   static __device__ __forceinline__ int key_piece(int row, int c) { return c ^ (row & (kPieces < 16 ? kPieces - 1 : 15)); }
-  // bf16: 32 lanes read 64 bytes of four neighbouring rows; fp32: 128 of one
-  static __device__ __forceinline__ int value_piece(int row, int c) {
-    return !kBf16 ? c : DP == 64 ? c ^ ((row & 2) << 1) : c ^ ((row & 3) << 2);
-  }
+  // 32 lanes read 64 bytes of four neighbouring rows
+  static __device__ __forceinline__ int value_piece(int row, int c) { return DP == 64 ? c ^ ((row & 2) << 1) : c ^ ((row & 3) << 2); }
 };
 
 // A part of a unit as its four waves hold it, lane by lane: the pieces of O^T, four columns of the lane's row each, then m and l.
@@ -211,7 +217,7 @@ __device__ __forceinline__ float both_halves_max(float v) {
 // share a CU, two waves a SIMD.
 template <int DP, bool kFull, int kGroups>
 __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill_bf16_kernel(const PrefillArgs a) {
-  using Geo = Geometry<true, DP>;
+  using Geo = Geometry<DP>;
   constexpr int kTokens = Geo::kTokens, kColTiles = DP / 32, kFetch = Geo::kFetch;
   constexpr int kSteps = kTokens / 32;               // of a tile
   constexpr int kPieces = DP / 16;                   // of a query row, a lane
@@ -464,13 +470,26 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
   finish<true, DP>(a, unit.splits == 1, blockIdx.x, mine, wave, out_row, o, m, l);
 }
 
-// The kernel of fp32: the matrix pipe's rate there is 16 times less, and nothing else is near it.
-template <int DP, int kGroups>
-__global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill_f32_kernel(const PrefillArgs a) {
-  using Geo = Geometry<false, DP>;
-  constexpr int kTokens = Geo::kTokens, kColTiles = DP / 32;
-  constexpr int kQueryPieces = DP * Geo::kSize / 32;  // of 16 bytes, a lane
-  __shared__ __align__(16) char all_lds[kGroups][2][2][Geo::kTileBytes];  // two tiles of K and V
+// Groups of waves of a workgroup.  Heads of up to 64 values: three workgroups share a CU, and what each does on the vector ALU is
+// beside the others' products (8192 tokens, 16 heads: 745 us, with two groups 760; 1023 tokens, 12 heads: 27 and 31).  Up to 128:
+// two waves a SIMD is what registers allow, and two groups finish a unit sooner than one (2048 tokens, 16 heads, twice: 206 and 301).
+constexpr int f32_groups(int dp) { return dp == 128 ? 2 : 1; }
+// The kernel of fp32, on bf16 products too: a value is the sum of three of bf16, and six products of parts stand for one (what is
+// left out is 2^-24 of it, an fp32 product's rounding), at 16 times the rate of fp32's own.  A tile is taken apart once, on its way
+// to LDS; the next one waits in registers meanwhile.  Probabilities are taken apart as they are made.  Against fp32's own
+// instruction: 1023 tokens, 12 heads over 4 of 64: 27 us and 41; 8192 tokens, 16 over 4 of 64: 745 and 1180; 2048 tokens, 16 over 4 of
+// 128, twice: 206 and 327; of 256, once: 311 and 424.
+template <int DP>
+__global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void prefill_f32_kernel(const PrefillArgs a) {
+  using split::Op;
+  constexpr bool kEarly = DP <= 64;  // registers are there for the next tile during the keys' product
+  constexpr int kTokens = tokens_of_tile(false), kColTiles = DP / 32, kGroups = f32_groups(DP);
+  constexpr int kSteps = DP / 16;                        // of a product with a key
+  constexpr int kFetch = kTokens * DP / 8 / kThreads;    // pieces of 8 values of a tile that a thread brings
+  // Rows of a part in LDS, so far apart that a read's go to all banks: 16 bytes of neighbouring rows (K), 64 of four (V)
+  constexpr int kKeyRow = 2 * DP + 16, kValueRow = 2 * DP + 64, kPieces = DP / 8;
+  constexpr int kKeyPart = kTokens * kKeyRow, kValuePart = kTokens * kValueRow;
+  __shared__ __align__(16) char all_lds[kGroups][3 * kKeyPart + 3 * kValuePart];
   static_assert(kGroups == 1 || sizeof(Part<DP>) <= sizeof(all_lds));
 
   int id = blockIdx.x;
@@ -483,8 +502,8 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % kWaves, group = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / kWaves;
   const int thread = 64 * wave + lane;  // of the group
-  char (*const lds)[2][Geo::kTileBytes] = all_lds[group];
-  const int bytes = a.d.D * Geo::kSize;
+  char *const lds_k = all_lds[group], *const lds_v = lds_k + 3 * kKeyPart;
+  const int bytes = a.d.D * 4;
   const int64_t page_bytes = (static_cast<int64_t>(a.d.Hk) << a.d.lg_page) * bytes;
   const int page_mask = (1 << a.d.lg_page) - 1;
   const char *kh = static_cast<const char *>(a.k) + (static_cast<int64_t>(hk) << a.d.lg_page) * bytes;
@@ -503,12 +522,23 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
   const int all_from = __builtin_amdgcn_readlane(seen_from, 31);
   const bool idle = wave * kWaveRows >= unit.rows;
 
-  u32x4 query[kQueryPieces];
+  auto take_apart = [](const u32x4 (&q)[2], Op (&o)[3]) {
+    float v[8];
 #pragma unroll
-  for (int i = 0; i < kQueryPieces; ++i) {
-    const int byte = 32 * i + 16 * h;
-    query[i] = u32x4{0u, 0u, 0u, 0u};
-    if (mine && byte < bytes) query[i] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q) + out_row * bytes + byte);
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(q[e / 4][e % 4]);
+    split::split3_even(v, o);
+  };
+  Op query[kSteps][3];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int byte = 64 * i + 32 * h;
+    u32x4 q[2] = {u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}};
+    if (mine && byte < bytes) {
+      const u32x4 *from = reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q) + out_row * bytes + byte);
+      q[0] = from[0];
+      q[1] = from[1];
+    }
+    take_apart(q, query[i]);
   }
   f32x16 o[kColTiles];
 #pragma unroll
@@ -523,61 +553,78 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
   const int rounds = (tile1 - (tile0 - group) + kGroups - 1) / kGroups;
   const int end = unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1;  // tokens seen by any row
 
-  u32x4 fetched[2][Geo::kFetch];
+  u32x4 fetched[2][kFetch][2];
   uint64_t gone = 0, gone_next = 0;  // tokens of the tile whose page is not in the cache
-  auto fetch = [&](int tile) {
+  auto page_of = [&](int tile) { return table[min(unit.base + tile * kTokens + (lane & (kTokens - 1)), end - 1) >> a.d.lg_page]; };
+  auto fetch = [&](int tile, int page) {
     const int first = unit.base + tile * kTokens;
-    const int t = min(first + (lane & (kTokens - 1)), end - 1);
-    int page = table[t >> a.d.lg_page];
     const bool bad = static_cast<unsigned>(page) >= static_cast<unsigned>(a.d.npages);
     gone_next = __ballot(bad) & ((1ull << kTokens) - 1);
     if (bad) page = -1;
 #pragma unroll
-    for (int i = 0; i < Geo::kFetch; ++i) {
-      const int piece = thread + i * kThreads, r = piece / Geo::kPieces, c = piece % Geo::kPieces;
+    for (int i = 0; i < kFetch; ++i) {
+      const int piece = thread + i * kThreads, r = piece / kPieces, c = piece % kPieces;
       const int where = __shfl(page, r);
       const int at = min(first + r, end - 1) & page_mask;
-      fetched[0][i] = fetched[1][i] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) fetched[0][i][e] = fetched[1][i][e] = u32x4{0u, 0u, 0u, 0u};
       // (a token behind the last one that is seen is brought as zeros: its probability is zero, and so must be the product)
-      if (where >= 0 && 16 * c < bytes && first + r < end) {
-        const int64_t byte = where * page_bytes + static_cast<int64_t>(at) * bytes + 16 * c;
-        fetched[0][i] = *reinterpret_cast<const u32x4 *>(kh + byte);
-        fetched[1][i] = *reinterpret_cast<const u32x4 *>(vh + byte);
+      if (where >= 0 && 32 * c < bytes && first + r < end) {
+        const int64_t byte = where * page_bytes + static_cast<int64_t>(at) * bytes + 32 * c;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          fetched[0][i][e] = *reinterpret_cast<const u32x4 *>(kh + byte + 16 * e);
+          fetched[1][i][e] = *reinterpret_cast<const u32x4 *>(vh + byte + 16 * e);
+        }
       }
     }
   };
-  auto stage = [&](int buffer) {
+  auto stage = [&] {
 #pragma unroll
-    for (int i = 0; i < Geo::kFetch; ++i) {
-      const int piece = thread + i * kThreads, r = piece / Geo::kPieces, c = piece % Geo::kPieces;
-      *reinterpret_cast<u32x4 *>(&lds[buffer][0][r * Geo::kRowBytes + 16 * Geo::key_piece(r, c)]) = fetched[0][i];
-      *reinterpret_cast<u32x4 *>(&lds[buffer][1][r * Geo::kRowBytes + 16 * Geo::value_piece(r, c)]) = fetched[1][i];
+    for (int i = 0; i < kFetch; ++i) {
+      const int piece = thread + i * kThreads, r = piece / kPieces, c = piece % kPieces;
+      Op parts[3];
+      take_apart(fetched[0][i], parts);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4 *>(lds_k + p * kKeyPart + r * kKeyRow + 16 * c) = parts[p].q;
+      take_apart(fetched[1][i], parts);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4 *>(lds_v + p * kValuePart + r * kValueRow + 16 * c) = parts[p].q;
     }
     gone = gone_next;
   };
+  const char *const k_lane = lds_k + n * kKeyRow + 16 * h;
+  const uint32_t v_lane = lds_address(lds_v + (4 * h + (lane & 15) / 4) * kValueRow + 32 * ((lane >> 4) & 1) + 8 * (lane & 3));
 
   if (rounds > 0) {
-    fetch(tile0);
-    stage(0);
+    fetch(tile0, page_of(tile0));
+    stage();
   }
   __syncthreads();
   for (int round = 0; round < rounds; ++round) {
-    const int tile = tile0 + kGroups * round, buffer = round & 1, first = unit.base + tile * kTokens;
-    const char *kt = lds[buffer][0], *vt = lds[buffer][1];
+    const int tile = tile0 + kGroups * round, first = unit.base + tile * kTokens;
     const uint64_t gone_now = gone;
-    if (round + 1 < rounds) fetch(tile + kGroups);
-    if (!idle && tile < tile1 && first <= any_to) {
-      f32x16 s;
+    const bool busy = !idle && tile < tile1 && first <= any_to;
+    const int page_next = page_of(tile + kGroups);
+    if (kEarly && round + 1 < rounds) fetch(tile + kGroups, page_next);
+    f32x16 s;
+    if (busy) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = 0.f;
-      const char *krow = kt + n * Geo::kRowBytes;
+      Op k[2][3];
+      auto read_keys = [&](int i) {
 #pragma unroll
-      for (int i = 0; i < kQueryPieces; ++i) {
-        const u32x4 k = *reinterpret_cast<const u32x4 *>(krow + 16 * Geo::key_piece(n, 2 * i + h));
+        for (int p = 0; p < 3; ++p) k[i & 1][p].q = *reinterpret_cast<const u32x4 *>(k_lane + p * kKeyPart + 32 * i);
+      };
+      read_keys(0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = mfma_f32(__uint_as_float(k[e]), __uint_as_float(query[i][e]), s);
+      for (int i = 0; i < kSteps; ++i) {
+        if (i + 1 < kSteps) read_keys(i + 1);
+        s = split::mfma6(k[i & 1], query[i], s);
+        if (DP > 64) asm volatile("" ::: "memory");  // (no reads further ahead: there are no registers for them)
       }
       if (first + kTokens - 1 > all_to || first < all_from || gone_now != 0) {
+        asm volatile("" ::: "memory");  // (nothing of this is computed where the branch isn't taken)
         const uint32_t out = static_cast<uint32_t>(gone_now) >> (4 * h);
         const int to = pos - (first + 4 * h), from = seen_from - (first + 4 * h);
 #pragma unroll
@@ -586,32 +633,63 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
           if (t > to || t < from || (out & (1u << t))) s[r] = -INFINITY;
         }
       }
-      float top = s[0];
+      float e[16], sum;
+      auto exponentials = [&] {
+        sum = 0.f;
 #pragma unroll
-      for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
-      top = both_halves_max(top) * a.scale_log2;
-      if (__any(top > m + kSlack)) {
-        const float next = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(m - next);
-        m = next;
+        for (int r = 0; r < 16; ++r) {
+          e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -m));
+          sum += e[r];
+        }
+      };
+      exponentials();
+      if (__any(!(sum <= kMost))) {
+        asm volatile("" ::: "memory");
+        float top = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+        const float larger = fmaxf(m, both_halves_max(top) * a.scale_log2), keep = __builtin_amdgcn_exp2f(m - larger);
+        m = larger;
         l *= keep;
 #pragma unroll
         for (int c = 0; c < kColTiles; ++c)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[c][r] *= keep;
+        exponentials();
       }
+      l += sum;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -m));
-        l += s[r];
-      }
+      for (int r = 0; r < 16; ++r) s[r] = e[r];
+    }
+    if (!kEarly && round + 1 < rounds) fetch(tile + kGroups, page_next);
+    if (busy) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float *vrow = reinterpret_cast<const float *>(vt + (8 * (r / 4) + 4 * h + r % 4) * Geo::kRowBytes);
+      for (int g = 0; g < 2; ++g) {
+        float e[8];
 #pragma unroll
-        for (int c = 0; c < kColTiles; ++c) o[c] = mfma_f32(vrow[32 * c + n], s[r], o[c]);
+        for (int r = 0; r < 8; ++r) e[r] = s[8 * g + r];
+        Op p[3];
+        split::split3_even(e, p);
+        Op v[2][3];
+        auto read_values = [&](int c) {
+#pragma unroll
+          for (int part = 0; part < 3; ++part) {
+            const int at = part * kValuePart + 16 * g * kValueRow + 64 * c;
+            v[c & 1][part].h[0] = lds_transposed(v_lane, at);
+            v[c & 1][part].h[1] = lds_transposed(v_lane, at + 8 * kValueRow);
+          }
+        };
+        read_values(0);
+#pragma unroll
+        for (int c = 0; c < kColTiles; ++c) {
+          if (c + 1 < kColTiles) read_values(c + 1);
+          o[c] = split::mfma6(v[c & 1], p, o[c]);
+          if (DP > 64) asm volatile("" ::: "memory");
+        }
       }
     }
-    if (round + 1 < rounds) stage(buffer ^ 1);
+    __syncthreads();
+    if (round + 1 < rounds) stage();
     __syncthreads();
   }
 
@@ -658,10 +736,9 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillArg
 struct Plan {
   int units, splits, groups;
 };
-// Two groups of waves share a unit where that leaves every CU a workgroup or few more: 2048 tokens, 32 heads over 8 of 128, 520
+// bf16: two groups of waves share a unit where that leaves every CU a workgroup or few more: 2048 tokens, 32 heads over 8 of 128, 520
 // units: 52 us, with a group each 56; 4096 tokens, 1032 units: 170 and 155.  Units of few tiles are not worth it: four times 512
-// tokens, 8 tiles: 31 and 25; 1024 tokens, 16 tiles: 24 and 27.  fp32, bound by its products alone, always: 2048 tokens, 16 heads
-// over 4 of 128, twice: 327 and 535; 8192 tokens, heads of 64: 1186 and 1268.
+// tokens, 8 tiles: 31 and 25; 1024 tokens, 16 tiles: 24 and 27.
 //
 // A unit's tiles are shared by several workgroups where that shortens the longest row of units a CU works on by more than the
 // parts' way through memory and the second launch take.  The host knows the rows of all sequences together, not of each, and the
@@ -673,11 +750,11 @@ Plan plan_of(const AttnDims &d) {
   const int64_t all = static_cast<int64_t>(p.units) * d.Hk;
   const int64_t most_seen = d.window > 0 ? std::min<int64_t>(d.capacity(), static_cast<int64_t>(d.window) + kUnitRows / d.G) : d.capacity();
   const int64_t tiles = (most_seen + tokens_of_tile(d.bf16) - 1) / tokens_of_tile(d.bf16);
-  p.groups = d.D <= 128 && (!d.bf16 || (all < kManyUnits && tiles >= kManyTiles)) ? 2 : 1;
+  p.groups = d.bf16 && d.D <= 128 && all < kManyUnits && tiles >= kManyTiles ? 2 : 1;
   p.splits = 1;
   if (all >= kManyUnits) return p;
-  // in us: a tile on a CU (bf16 at 1 PFLOP/s, fp32 at 150 TFLOP/s); a part written and read
-  const double tile = (d.bf16 ? 1.0 : 3.5) * d.D / 128, part = 0.04 * d.D / 128, launch = 5.0;
+  // in us: a tile on a CU, a part written and read
+  const double tile = (d.bf16 ? 1.0 : 2.0) * d.D / 128, part = 0.04 * d.D / 128, launch = 5.0;
   const double units = (std::ceil(static_cast<double>(rows) / kUnitRows) + 0.5 * (d.B - 1)) * d.Hk;
   // whole prompts, whose units see from no tile to all: the longest first fills the CUs evenly; pieces behind a long cache see much
   // the same each, and the last CU to begin one decides
@@ -702,10 +779,7 @@ hipError_t launch(const PrefillArgs &a, hipStream_t stream) {
   const bool two = kTwo == 2 && a.groups == 2;
   const dim3 threads(two ? 2 * kThreads : kThreads);
   if constexpr (!kBf16) {
-    if (two)
-      hipLaunchKernelGGL((prefill_f32_kernel<DP, kTwo>), grid, threads, 0, stream, a);
-    else
-      hipLaunchKernelGGL((prefill_f32_kernel<DP, 1>), grid, threads, 0, stream, a);
+    hipLaunchKernelGGL(prefill_f32_kernel<DP>, grid, dim3(kThreads * f32_groups(DP)), 0, stream, a);
   } else if (a.d.D == DP) {
     if (two)
       hipLaunchKernelGGL((prefill_bf16_kernel<DP, true, kTwo>), grid, threads, 0, stream, a);

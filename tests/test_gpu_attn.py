@@ -116,6 +116,23 @@ def test_prefill_matches_oracle(ssd, heads, io):
             assert_close(y, ref, TOL[io], "prefill")
 
 
+@pytest.mark.parametrize("heads", [(6, 2, 64, 16), (4, 2, 128, 16), (2, 1, 256, 16)], ids=lambda h: "x".join(map(str, h)))
+def test_prefill_f32_is_exact_over_the_range(ssd, heads):
+    """The values' parts lose nothing: a power of two goes through to the results bit by bit.  What is infinite and seen shows."""
+    s = make([300, 70], *heads, "f32", new=[130, 70], seed=40)
+    y = run_prefill(ssd, s)
+    v = s["v"]
+    for power in (100, -60):
+        s["v"] = v * 2.0 ** power
+        assert torch.equal(run_prefill(ssd, s), y * 2.0 ** power), power
+    s["v"] = v.clone()
+    s["v"][s["table"][0, 0], 0, 0, 3] = float("inf")  # the first token of the first sequence, which all of its rows see
+    y = run_prefill(ssd, s)
+    groups = heads[0] // heads[1]
+    assert not torch.isfinite(y[:130, :groups, 3]).any()
+    assert torch.isfinite(y[130:]).all() and torch.isfinite(y[:130, groups:]).all() and torch.isfinite(y[:130, :, :3]).all()
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_long_step_and_prefill(ssd, io):
     """Enough work for every workgroup, split and joined: a long sequence among short ones, and a late piece of a prompt."""
