@@ -32,6 +32,10 @@ constexpr int kWorkgroups = 256;  // of eight waves, which fill the GPU
 constexpr int kManyUnits = 768;   // units that four waves each take,
 constexpr int kManyTiles = 16;    // unless they have fewer tiles
 constexpr int kMostSplits = 64;   // of a unit
+// Where units are shared, a workgroup is to have a little more than its part of all tiles.  A unit has less than twice its
+// sequence's average of them, so that there are at most 2 kWorkgroups / 1.125 workgroups more than units.
+constexpr float kShare = 1.125f / kWorkgroups;
+constexpr int kMostParts = 2 * kWorkgroups;
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
 constexpr int tokens_of_tile(bool bf16) { return bf16 ? 64 : 32; }
 // Tiles that a workgroup at least takes where several share a unit: 1.0 us of work in bf16 a tile and CU with heads of 128 values,
@@ -50,45 +54,125 @@ struct PrefillArgs {
   uint32_t inv_group;
   int units;         // at most, of a key head
   int splits;        // at most, of a unit
+  int parts;         // there is room for
   int groups;        // of waves, a workgroup (bf16)
   float scale_log2;  // scale * log2(e)
 };
 
-// A unit's rows and the tokens they see.
+// A unit's rows and the tokens they see; one of the workgroups that share it.
 struct Unit {
   int rows;        // 0: there is no such unit
   int first_row;   // of its sequence
   int seq, begin;  // the sequence and its first new token
   int pos0;        // that token's position
   int base, tiles, splits;
+  int split;       // this workgroup's
+  int part;        // place of its first workgroup among all (of a key head)
 };
 template <int kTokens>
-__device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int u) {
-  Unit r = {};
-  // Sequence b's units begin at cu[b] * group / rows + b: these are at least as far apart as its units are many.
-  const auto bound = [&](int b) { return min(max(a.cu[b], 0), a.d.T); };
-  const auto first_unit = [&](int b) { return static_cast<int64_t>(bound(b)) * a.d.G / kUnitRows + b; };
-  int last = -1;
-  for (int b0 = 0; b0 < a.d.B; b0 += 64) {
-    const int b = b0 + (threadIdx.x & 63);
-    const uint64_t m = __ballot(b < a.d.B && first_unit(b) <= u);
-    if (m != 0) last = b0 + 63 - __builtin_clzll(m);
-  }
-  if (last < 0) return r;
-  r.seq = last;
-  r.begin = bound(last);
-  const int count = bound(last + 1) - r.begin;
-  const int64_t first = (u - first_unit(last)) * kUnitRows, all = static_cast<int64_t>(count) * a.d.G;
-  if (first >= all) return r;
-  r.first_row = static_cast<int>(first);
-  r.rows = static_cast<int>(min(static_cast<int64_t>(kUnitRows), all - first));
-  const int len = cut_length(a.d, a.lens[last]);
-  r.pos0 = len - count;
+__device__ __forceinline__ void see(const PrefillArgs &a, Unit &r) {
   const int lowest = r.pos0 + quotient(r.first_row, a.d.G, a.inv_group);
   const int highest = r.pos0 + quotient(r.first_row + r.rows - 1, a.d.G, a.inv_group);
   r.base = (a.d.window > 0 ? max(0, lowest + 1 - a.d.window) : 0) & ~(kTokens - 1);
   r.tiles = highest < 0 ? 0 : (highest + 1 - r.base + kTokens - 1) / kTokens;
-  r.splits = max(1, min(a.splits, (r.tiles + least_tiles(kTokens) - 1) / least_tiles(kTokens)));
+}
+// A sequence's units.
+struct Line {
+  int begin, pos0, all;  // all: rows
+  int units, tiles;      // tiles of the last unit, which has the most
+  float work;            // tiles of all, about
+};
+template <int kTokens>
+__device__ __forceinline__ Line line_of(const PrefillArgs &a, int b) {
+  Line r = {};
+  if (b >= a.d.B) return r;
+  r.begin = min(max(a.cu[b], 0), a.d.T);
+  const int count = min(max(a.cu[b + 1], 0), a.d.T) - r.begin;
+  r.pos0 = cut_length(a.d, a.lens[b]) - count;
+  if (count <= 0) return r;
+  r.all = count * a.d.G;
+  r.units = (r.all - 1) / kUnitRows + 1;
+  Unit u = {};
+  u.pos0 = r.pos0;
+  u.rows = min(kUnitRows, r.all);
+  see<kTokens>(a, u);
+  const int first_tiles = u.tiles;
+  u.first_row = (r.units - 1) * kUnitRows;
+  u.rows = r.all - u.first_row;
+  see<kTokens>(a, u);
+  r.tiles = max(first_tiles, u.tiles);
+  r.work = 0.5f * static_cast<float>(r.units) * static_cast<float>(first_tiles + r.tiles);
+  return r;
+}
+__device__ __forceinline__ int64_t shuffle_up64(int64_t v, int k) {
+  const int lo = __shfl_up(static_cast<int>(v), k), hi = __shfl_up(static_cast<int>(v >> 32), k);
+  return static_cast<int64_t>(hi) << 32 | static_cast<uint32_t>(lo);
+}
+// Unit (kByUnit) or workgroup k of a key head, in the order in which they are begun: the sequences whose workgroups have the most
+// tiles first, of a sequence the last units first, which see the most tokens.  A long unit is shared by as many workgroups as give
+// each a little more than the average CU's load, which only the device knows.  They have neighbouring numbers, and there are no
+// gaps but where a prompt's first units need fewer: a workgroup without work that is between others leaves its CU idle for as long
+// as theirs take.  Every wave finds out by itself, a lane a sequence.  Ten pieces of 0 to 512 tokens behind up to 20000, 20 heads over
+// 4, window 4096: 63 us, with units in the order of the sequences and the same shares for all 71; eight prompts of 1 to 4096 tokens,
+// 16 heads over 4: 141 and 153.
+template <int kTokens, bool kByUnit>
+__device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
+  const int lane = threadIdx.x & 63, lanes = min(a.d.B, 64);
+  Unit r = {};
+  Line line = line_of<kTokens>(a, lane);
+  float share = 0.f;  // tiles that a workgroup is to have
+  if (a.splits > 1) {
+    float work = line.work;
+    for (int b0 = 64; b0 < a.d.B; b0 += 64) work += line_of<kTokens>(a, b0 + lane).work;
+    for (int d = 1; d < lanes; d <<= 1) work += __shfl_xor(work, d);
+    work = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(work)));
+    share = fmaxf(work * static_cast<float>(a.d.Hk) * kShare, static_cast<float>(least_tiles(kTokens)));
+  }
+  int done = 0, done_units = 0;  // of the sequences in front of these 64
+  for (int b0 = 0; b0 < a.d.B; b0 += 64) {
+    if (b0 > 0) line = line_of<kTokens>(a, b0 + lane);
+    const int splits = a.splits > 1 ? min(max(static_cast<int>(ceilf(static_cast<float>(line.tiles) / share)), 1), a.splits) : 1;
+    const int n = line.units * splits, per = line.tiles / splits;
+    int most = per;
+    for (int d = 1; d < lanes; d <<= 1) most = max(most, __shfl_xor(most, d));
+    const bool front = 2 * per > most;
+    // workgroups of those in front in the upper half, of the others in the lower one
+    const int64_t mine = front ? static_cast<int64_t>(n) << 32 : n, mine_units = front ? static_cast<int64_t>(line.units) << 32 : line.units;
+    int64_t sum = mine, units = mine_units;
+    for (int d = 1; d < lanes; d <<= 1) {
+      const int64_t o = shuffle_up64(sum, d);
+      if (lane >= d) sum += o;
+      if (kByUnit) {
+        const int64_t p = shuffle_up64(units, d);
+        if (lane >= d) units += p;
+      }
+    }
+    const auto before = [&](int64_t sum, int64_t mine, int done) {
+      const int fronts = __builtin_amdgcn_readlane(static_cast<int>(sum >> 32), lanes - 1);
+      return done + (front ? static_cast<int>((sum - mine) >> 32) : fronts + static_cast<int>(sum - mine));
+    };
+    const int first = before(sum, mine, done), first_unit = kByUnit ? before(units, mine_units, done_units) : 0;
+    const uint64_t here = kByUnit ? __ballot(k >= first_unit && k < first_unit + line.units) : __ballot(k >= first && k < first + n);
+    if (here != 0) {
+      const int l = __builtin_ctzll(here);
+      const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      r.seq = b0 + l;
+      r.begin = of(line.begin);
+      r.pos0 = of(line.pos0);
+      r.splits = of(splits);
+      const int place = k - of(kByUnit ? first_unit : first), u = kByUnit ? place : place / r.splits;
+      r.split = kByUnit ? 0 : place - u * r.splits;
+      r.part = of(first) + u * r.splits;
+      r.first_row = (of(line.units) - 1 - u) * kUnitRows;
+      r.rows = min(kUnitRows, of(line.all) - r.first_row);
+      see<kTokens>(a, r);
+      r.splits = max(1, min(r.splits, (r.tiles + least_tiles(kTokens) - 1) / least_tiles(kTokens)));
+      if (r.split >= r.splits) r.rows = 0;
+      return r;
+    }
+    done += __builtin_amdgcn_readlane(static_cast<int>(sum >> 32) + static_cast<int>(sum), lanes - 1);
+    if (kByUnit) done_units += __builtin_amdgcn_readlane(static_cast<int>(units >> 32) + static_cast<int>(units), lanes - 1);
+  }
   return r;
 }
 
@@ -228,12 +312,9 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
   __shared__ __align__(16) char lds[kGroups][kKeyTiles + 2][Geo::kTileBytes];
   static_assert(kGroups == 1 || sizeof(Part<DP>) <= sizeof(lds));
 
-  int id = blockIdx.x;
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int hk = id % a.d.Hk;
-  const Unit unit = find_unit<kTokens>(a, a.units - 1 - id / a.d.Hk);  // (the last units see the most tokens)
-  if (unit.rows == 0 || split >= unit.splits) return;
+  const int hk = static_cast<int>(blockIdx.x) % a.d.Hk;
+  const Unit unit = find_unit<kTokens, false>(a, static_cast<int>(blockIdx.x) / a.d.Hk);
+  if (unit.rows == 0) return;
 
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % kWaves, group = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / kWaves;
@@ -263,8 +344,8 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
   const bool idle = wave * 32 >= unit.rows;
 
   // the split's tiles, of which the group takes every kGroups-th
-  const int tile1 = static_cast<int>(static_cast<int64_t>(unit.tiles) * (split + 1) / unit.splits);
-  const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * split / unit.splits) + group;
+  const int tile1 = static_cast<int>(static_cast<int64_t>(unit.tiles) * (unit.split + 1) / unit.splits);
+  const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * unit.split / unit.splits) + group;
   const int rounds = (tile1 - (tile0 - group) + kGroups - 1) / kGroups;
   const int end = unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1;  // tokens seen by any row
 
@@ -492,12 +573,9 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
   __shared__ __align__(16) char all_lds[kGroups][3 * kKeyPart + 3 * kValuePart];
   static_assert(kGroups == 1 || sizeof(Part<DP>) <= sizeof(all_lds));
 
-  int id = blockIdx.x;
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int hk = id % a.d.Hk;
-  const Unit unit = find_unit<kTokens>(a, a.units - 1 - id / a.d.Hk);  // (the last units see the most tokens)
-  if (unit.rows == 0 || split >= unit.splits) return;
+  const int hk = static_cast<int>(blockIdx.x) % a.d.Hk;
+  const Unit unit = find_unit<kTokens, false>(a, static_cast<int>(blockIdx.x) / a.d.Hk);
+  if (unit.rows == 0) return;
 
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % kWaves, group = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / kWaves;
@@ -548,8 +626,8 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
   float m = kNone, l = 0.f;
 
   // the split's tiles, of which the group takes every kGroups-th
-  const int tile1 = static_cast<int>(static_cast<int64_t>(unit.tiles) * (split + 1) / unit.splits);
-  const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * split / unit.splits) + group;
+  const int tile1 = static_cast<int>(static_cast<int64_t>(unit.tiles) * (unit.split + 1) / unit.splits);
+  const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * unit.split / unit.splits) + group;
   const int rounds = (tile1 - (tile0 - group) + kGroups - 1) / kGroups;
   const int end = unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1;  // tokens seen by any row
 
@@ -706,14 +784,16 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillArg
   const int cut = id % (DP / 32);
   id /= DP / 32;
   const int hk = id % a.d.Hk;
-  const Unit unit = find_unit<kTokens>(a, a.units - 1 - id / a.d.Hk);
+  const Unit unit = find_unit<kTokens, true>(a, id / a.d.Hk);
   if (unit.rows == 0 || unit.splits == 1) return;
+  // (boundaries that make sequences overlap could have more parts than there is room for)
+  if (unit.part < 0 || static_cast<int64_t>(unit.part + unit.splits) * a.d.Hk > a.parts) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, local = 32 * wave + (lane & 31), h = lane / 32;
   float top = kNone, sum = 0.f;
   f32x4 o[4] = {};
 #pragma unroll 2
   for (int split = 0; split < unit.splits; ++split) {
-    const Part<DP> &part = static_cast<const Part<DP> *>(a.part)[static_cast<int64_t>(id) * a.splits + split];
+    const Part<DP> &part = static_cast<const Part<DP> *>(a.part)[static_cast<int64_t>(unit.part + split) * a.d.Hk + hk];
     const float m = part.m[wave][lane], l = part.l[wave][lane];
     const float next = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(top - next), f = __builtin_amdgcn_exp2f(m - next);
     top = next;
@@ -734,15 +814,16 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillArg
 }
 
 struct Plan {
-  int units, splits, groups;
+  int units, groups;
+  bool shared;
 };
 // bf16: two groups of waves share a unit where that leaves every CU a workgroup or few more: 2048 tokens, 32 heads over 8 of 128, 520
 // units: 52 us, with a group each 56; 4096 tokens, 1032 units: 170 and 155.  Units of few tiles are not worth it: four times 512
 // tokens, 8 tiles: 31 and 25; 1024 tokens, 16 tiles: 24 and 27.
 //
-// A unit's tiles are shared by several workgroups where that shortens the longest row of units a CU works on by more than the
-// parts' way through memory and the second launch take.  The host knows the rows of all sequences together, not of each, and the
-// most tokens that the page table holds.
+// A unit's tiles may be shared by several workgroups where that could shorten the longest row of units a CU works on by more than
+// the parts' way through memory and the second launch take.  The host knows the rows of all sequences together, not of each, and
+// the most tokens that the page table holds; by how many, the device finds (find_unit).
 Plan plan_of(const AttnDims &d) {
   Plan p;
   const int64_t rows = static_cast<int64_t>(d.T) * d.G;
@@ -751,7 +832,7 @@ Plan plan_of(const AttnDims &d) {
   const int64_t most_seen = d.window > 0 ? std::min<int64_t>(d.capacity(), static_cast<int64_t>(d.window) + kUnitRows / d.G) : d.capacity();
   const int64_t tiles = (most_seen + tokens_of_tile(d.bf16) - 1) / tokens_of_tile(d.bf16);
   p.groups = d.bf16 && d.D <= 128 && all < kManyUnits && tiles >= kManyTiles ? 2 : 1;
-  p.splits = 1;
+  p.shared = false;
   if (all >= kManyUnits) return p;
   // in us: a tile on a CU, a part written and read
   const double tile = (d.bf16 ? 1.0 : 2.0) * d.D / 128, part = 0.04 * d.D / 128, launch = 5.0;
@@ -759,22 +840,20 @@ Plan plan_of(const AttnDims &d) {
   // whole prompts, whose units see from no tile to all: the longest first fills the CUs evenly; pieces behind a long cache see much
   // the same each, and the last CU to begin one decides
   const bool prompts = most_seen <= 2 * static_cast<int64_t>(d.T / d.B);
-  double best = 0.0;
+  double whole = 0.0;
   for (int s = 1; s == 1 || (s <= kMostSplits && (s - 1) * least_tiles(tokens_of_tile(d.bf16)) < tiles); ++s) {
     const double longest = static_cast<double>(tiles) / s;
     const double row = prompts ? std::max(longest, units * tiles / 2 / kWorkgroups) + longest / 4 : std::ceil(units * s / kWorkgroups) * longest;
     const double cost = row * tile + (s > 1 ? launch + part * units * s : 0.0);
-    if (s == 1 || cost < best) {
-      best = cost;
-      p.splits = s;
-    }
+    if (s == 1) whole = cost;
+    else p.shared |= cost < whole;
   }
   return p;
 }
 
 template <bool kBf16, int DP>
 hipError_t launch(const PrefillArgs &a, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(a.units) * a.d.Hk * a.splits);
+  const dim3 grid(static_cast<unsigned>(a.units) * a.d.Hk + (a.splits > 1 ? kMostParts : 0));
   constexpr int kTwo = DP <= 128 ? 2 : 1;  // (heads of 256 values leave registers for one wave a SIMD)
   const bool two = kTwo == 2 && a.groups == 2;
   const dim3 threads(two ? 2 * kThreads : kThreads);
@@ -804,8 +883,8 @@ hipError_t launch(const PrefillArgs &a, hipStream_t stream) {
 
 size_t attn_prefill_workspace_bytes(const AttnDims &d) {
   const Plan p = plan_of(d);
-  if (p.splits == 1) return 256;
-  return static_cast<size_t>(p.units) * d.Hk * p.splits * (d.D <= 64 ? sizeof(Part<64>) : d.D <= 128 ? sizeof(Part<128>) : sizeof(Part<256>));
+  if (!p.shared) return 256;
+  return (static_cast<size_t>(p.units) * d.Hk + kMostParts) * (d.D <= 64 ? sizeof(Part<64>) : d.D <= 128 ? sizeof(Part<128>) : sizeof(Part<256>));
 }
 
 hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32_t *lens, const int32_t *table, const void *q,
@@ -824,7 +903,8 @@ hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32
   a.d = d;
   a.inv_group = inverse_of(d.G);
   a.units = p.units;
-  a.splits = p.splits;
+  a.splits = p.shared ? kMostSplits : 1;
+  a.parts = p.units * d.Hk + kMostParts;
   a.groups = p.groups;
   a.scale_log2 = scale * 1.44269504f;
   return d.bf16 ? launch<true>(a, stream) : launch<false>(a, stream);

@@ -134,6 +134,36 @@ def test_prefill_f32_is_exact_over_the_range(ssd, heads):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("batch", [2, 64, 65, 150])
+def test_prefill_many_sequences(ssd, batch, io):
+    """Pieces of few and of many tokens, some of them behind a long cache, whose units are shared, and some with nothing new."""
+    rng = np.random.default_rng(batch)
+    new, prior = rng.integers(0, 40, batch), rng.integers(0, 60, batch)
+    new[::3] = 0
+    new[-2], prior[-2] = 150, 2500
+    new[0], prior[0] = 3, 1700
+    s = make([int(n) for n in new + prior], 3, 1, 64, 16, io, new=[int(n) for n in new], seed=batch)
+    for window in (0, 700):
+        print("prefill", batch, io, window, flush=True)
+        y = run_prefill(ssd, s, window=window)
+        ref = block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], s["cu"], window=window)
+        assert_close(y, ref, TOL[io], "prefill")
+
+
+def test_prefill_overlapping_boundaries_stay_inside(ssd):
+    """Boundaries that count tokens many times over: results are anything, what surrounds y and the caches stays as it was."""
+    s = make([3000] * 40, 4, 1, 64, 16, "bf16", new=[20] * 40, seed=50)
+    s["cu"] = torch.tensor([0, 800] * 20 + [0], dtype=torch.int32)
+    d = dev(s)
+    k, v = d["k"].clone(), d["v"].clone()
+    room = torch.full((802, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    ssd.ssd_attn_prefill(d["q"], d["k"], d["v"], d["table"], d["lens"], d["cu"], y=room[1:801])
+    torch.cuda.synchronize()
+    assert bool((room[0] == 7).all()) and bool((room[801] == 7).all())
+    assert torch.equal(d["k"].view(torch.int16), k.view(torch.int16)) and torch.equal(d["v"].view(torch.int16), v.view(torch.int16))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_long_step_and_prefill(ssd, io):
     """Enough work for every workgroup, split and joined: a long sequence among short ones, and a late piece of a prompt."""
     s = make([20011, 17, 900], 10, 2, 128, 16, io, seed=30)
