@@ -7,7 +7,7 @@
 // A unit -- a row, or one group of a row -- is read once, kept in registers as fp32 while its squares are summed, and written
 // once.  A thread owns pieces of 8 neighbouring values (bf16: 16 bytes; fp32: 32).  Both are streams; with few rows they are a
 // chain of two memory latencies and a reduction, and the unit is spread over as many threads as it has pieces for.
-// 16384 rows of 5120, gated, bf16: 100 us, 5.0 TB/s (a copy: 4.9); 16383 of 768, residual, fp32: 40 us, 5.0 TB/s; one row: 4.4 us.
+// 16384 rows of 5120, gated, bf16: 100 us, 5.0 TB/s (a copy: 4.9); 16383 of 768, residual, fp32: 40 us, 5.0 TB/s; one row: 3.1 us, a launch.
 #include "ssd_block.hpp"
 
 namespace ssd {
@@ -16,6 +16,7 @@ namespace {
 using namespace block;
 
 constexpr int kPiece = 8;
+constexpr int kFewUnits = 512;
 
 enum Mode { kGateFirst = 0, kNormFirst = 1, kResidual = 2 };
 
@@ -149,13 +150,19 @@ hipError_t launch_shape(const NormArgs &a, hipStream_t stream) {
 
 // Threads and pieces a thread by the unit's width: no more registers than the pieces need, which leave room for other units'
 // requests (16384 rows of 5120 bf16 values: 132 us with four pieces a thread, of which two and a half are there, 100 with three),
-// and no wave with nothing to do.
+// and no wave with nothing to do.  Few units leave CUs idle, and each is a chain of latencies: a piece a thread, where that is
+// possible (5120 bf16 values: one row 3.1 us instead of 4.2, 512 rows 5.5 and 6.7, 1024 rows 8.5 and 8.4).
 template <typename Io, typename Side, int kMode>
 hipError_t launch_mode(const NormArgs &a, hipStream_t stream) {
   const int pieces = (a.n + kPiece - 1) / kPiece;
   if (pieces <= 16) return launch_shape<Io, Side, kMode, 16, 1>(a, stream);
   if (pieces <= 64) return launch_shape<Io, Side, kMode, 64, 1>(a, stream);
   if (pieces <= 256) return launch_shape<Io, Side, kMode, 256, 1>(a, stream);
+  if (a.units <= kFewUnits && pieces <= 2048) {
+    if (pieces <= 512) return launch_shape<Io, Side, kMode, 512, 1>(a, stream);
+    if (pieces <= 1024) return launch_shape<Io, Side, kMode, 1024, 1>(a, stream);
+    return launch_shape<Io, Side, kMode, 1024, 2>(a, stream);
+  }
   if (pieces <= 512) return launch_shape<Io, Side, kMode, 256, 2>(a, stream);
   if (pieces <= 768) return launch_shape<Io, Side, kMode, 256, 3>(a, stream);
   if (pieces <= 1024) return launch_shape<Io, Side, kMode, 512, 2>(a, stream);

@@ -67,6 +67,22 @@ def test_residual_norm_matches_oracle(ssd, width, io, stream):
         close(out, ref, "out", x.dtype)
 
 
+@pytest.mark.parametrize("rows", [512, 513])
+@pytest.mark.parametrize("width", [2050, 4096, 5117, 8192, 8200, 16384])
+def test_norms_of_more_rows(ssd, width, rows):
+    """Wide rows, on either side of the number from which a thread takes several pieces of them."""
+    x, side, w = draw(rows, width, "bf16", 20), draw(rows, width, "bf16", 21), draw(1, width, "f32", 22)[0]
+    print("norms", rows, width, flush=True)
+    gated = ssd.ssd_norm_gated(x.cuda(), side.cuda(), w.cuda(), norm_first=True)
+    out, r = ssd.ssd_norm_residual(side.cuda(), x.cuda(), w.cuda(), scale=0.5)
+    torch.cuda.synchronize()
+    some = slice(None, None, 37)
+    close(gated[some], block_oracle.norm_gated(x[some], side[some], w, 1e-5, 1, True), "gated", x.dtype)
+    ref, r_ref = block_oracle.norm_residual(side[some], x[some], w, 0.5, 1e-5)
+    close(r[some], r_ref, "stream", side.dtype)
+    close(out[some], ref, "out", x.dtype)
+
+
 @pytest.mark.parametrize("stream", ["f32", "bf16"])
 def test_first_block_has_no_residual(ssd, stream):
     x, w = draw(7, 300, "bf16", 7), draw(1, 300, "f32", 8)[0]
