@@ -21,7 +21,7 @@
 // (m, l, O) in the workspace, which a second launch joins.  Where no sequence can be long, a workgroup of eight waves takes a unit
 // and there is no second launch.
 //
-// 32 heads over 8 of 128, bf16: 64 sequences to 32768 tokens 165 us, 5.4 TB/s of K and V; one of 32000 29 us, one of 518 8.8 us.
+// 32 heads over 8 of 128, bf16: 64 sequences to 32768 tokens 165 us, 5.4 TB/s of K and V; one of 32000 28 us, one of 518 8.8 us.
 // fp32, 2 sequences to 100004, 10 heads over 2 of 64: 42 us, 4.9 TB/s.
 #include <algorithm>
 
@@ -443,7 +443,19 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
 // them where there are many units), and as many of the parts at a time as it has threads for.
 template <bool kBf16>
 __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int rows, int cols, int row_cuts, int col_cuts) {
-  __shared__ float got[kThreads][6];
+  constexpr int kAhead = 4;  // parts whose values are on their way at a time
+  struct Share {
+    f32x4 o;
+    float m, l;
+  };
+  __shared__ Share got[kThreads];
+  const auto join = [](float &top, float &sum, f32x4 &v, float m, float l, f32x4 o) {
+    const float next = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(top - next), f = __builtin_amdgcn_exp2f(m - next);
+    top = next;
+    sum = fmaf(sum, keep, l * f);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = fmaf(v[r], keep, o[r] * f);
+  };
   unsigned id = blockIdx.x;
   const int col_cut = static_cast<int>(id % col_cuts), row_cut = static_cast<int>(id / col_cuts % row_cuts);
   id /= static_cast<unsigned>(col_cuts * row_cuts);
@@ -466,35 +478,41 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int ro
     float top = kNone, sum = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (mine) {
-#pragma unroll 4
-      for (int w = first + lane; w <= last; w += abreast) {
-        const int slot_row = (2 * w + (w == first ? 1 : 0)) * kRows + row;
-        const float *part = a.part + static_cast<int64_t>(slot_row) * (a.d.D + 4);
-        const float m = part[a.d.D], l = part[a.d.D + 1];
-        const f32x4 o = *reinterpret_cast<const f32x4 *>(part + col);
-        const float next = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(top - next), f = __builtin_amdgcn_exp2f(m - next);
-        top = next;
-        sum = fmaf(sum, keep, l * f);
+      for (int w0 = first + lane; w0 <= last; w0 += kAhead * abreast) {
+        float m[kAhead], l[kAhead];
+        f32x4 o[kAhead];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = fmaf(v[r], keep, o[r] * f);
+        for (int i = 0; i < kAhead; ++i) {
+          const int w = w0 + i * abreast;
+          m[i] = kNone;
+          l[i] = 0.f;
+          o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (w <= last) {
+            const float *part = a.part + static_cast<int64_t>((2 * w + (w == first ? 1 : 0)) * kRows + row) * (a.d.D + 4);
+            m[i] = part[a.d.D];
+            l[i] = part[a.d.D + 1];
+            o[i] = *reinterpret_cast<const f32x4 *>(part + col);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) join(top, sum, v, m[i], l[i], o[i]);
       }
     }
     if (abreast > 1) {
-      float *g = got[threadIdx.x];
-      g[0] = top;
-      g[1] = sum;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) g[2 + r] = v[r];
-      __syncthreads();
-      if (mine && lane == 0)
-        for (int i = 1; i < abreast; ++i) {
-          const float *p = got[threadIdx.x + i * items];
-          const float next = fmaxf(top, p[0]), keep = __builtin_amdgcn_exp2f(top - next), f = __builtin_amdgcn_exp2f(p[0] - next);
-          top = next;
-          sum = fmaf(sum, keep, p[1] * f);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] = fmaf(v[r], keep, p[2 + r] * f);
+      Share &mine_of = got[threadIdx.x];
+      mine_of.m = top;
+      mine_of.l = sum;
+      mine_of.o = v;
+      for (int d = 1 << (31 - __builtin_clz(abreast - 1)); d > 0; d >>= 1) {
+        __syncthreads();
+        if (mine && lane < d && lane + d < abreast) {
+          const Share &other = got[threadIdx.x + d * items];
+          join(top, sum, v, other.m, other.l, other.o);
+          mine_of.m = top;
+          mine_of.l = sum;
+          mine_of.o = v;
         }
+      }
     }
     if (mine && lane == 0) {
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -510,9 +528,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int ro
 }
 
 // Whether work is dealt, from the most tokens that a sequence can have: half of them are reckoned with.  In us, with 32 heads over
-// 8 of 128, bf16: a unit to a workgroup takes 4 and its bytes at 52 GB/s, or all units' at 6 TB/s; dealing takes 10 and all units'
-// bytes at 5.2 TB/s, and is charged 2 more, for lengths that are alike lose more by it than uneven ones win.  One sequence of 518
-// tokens: 8.8 and 10.9 dealt; of 2000: 22 and 11; 16 of 2000: 23 and 31.  A sequence of more than a MiB a key head, 20 us for a
+// 8 of 128, bf16: a unit to a workgroup takes 4 and its bytes at 52 GB/s, or all units' at 6 TB/s; dealing takes 9 and all units'
+// bytes at 5.2 TB/s, and is charged 3 more, for lengths that are alike lose more by it than uneven ones win.  One sequence of 518
+// tokens: 8.8 and 9.9 dealt; of 2000: 22 and 10; 16 of 2000: 23 and 30.  A sequence of more than a MiB a key head, 20 us for a
 // workgroup, may be the only one that long: then work is dealt.
 bool dealt(const AttnDims &d) {
   const double longest = 2.0 * d.capacity() * d.D * (d.bf16 ? 2 : 4), all = 0.5 * longest * d.B * units_of(d);
