@@ -42,14 +42,23 @@ constexpr int tokens_of_tile(bool bf16) { return bf16 ? 64 : 32; }
 // 2.0 in fp32.
 constexpr int least_tiles(int tokens) { return tokens == tokens_of_tile(true) ? 8 : 4; }
 // There is no search for the largest score of a step: the sum of a lane's probabilities, which is needed anyway, says whether one is
-// too large for the running maximum.  Until then probabilities are up to this, which costs no accuracy, and O need not be scaled again.
-constexpr float kMost = 65536.f;
+// too large for the running maximum.  Until then they are up to this (bf16, 16384 tokens: 2.07 ms, a search for every step 2.28).
+// bf16: what is summed are the probabilities as they are rounded for their product with the values, so that the rounding of a token
+// that outweighs the others drops out: error against 64 bits, 24 rows that see 920 tokens, logits of deviation 2, in units of the
+// result's rounding: 1.30 on average and 1.48 at most of 150 draws, with exact sums 1.40 and 1.81.
+constexpr float kMost = 256.f;
+
+// A unit as the joining launch needs it; each workgroup leaves one, with splits = 0 if it is not the first of a shared unit.
+struct Record {
+  int rows, first_row, begin, splits;
+};
 
 struct PrefillArgs {
   const int32_t *cu, *lens, *table;
   const void *q, *k, *v;
   void *y;
-  void *part;        // for each unit and split
+  void *part;        // of each workgroup
+  Record *record;    // likewise
   AttnDims d;
   uint32_t inv_group;
   int units;         // at most, of a key head
@@ -67,7 +76,6 @@ struct Unit {
   int pos0;        // that token's position
   int base, tiles, splits;
   int split;       // this workgroup's
-  int part;        // place of its first workgroup among all (of a key head)
 };
 template <int kTokens>
 __device__ __forceinline__ void see(const PrefillArgs &a, Unit &r) {
@@ -108,14 +116,14 @@ __device__ __forceinline__ int64_t shuffle_up64(int64_t v, int k) {
   const int lo = __shfl_up(static_cast<int>(v), k), hi = __shfl_up(static_cast<int>(v >> 32), k);
   return static_cast<int64_t>(hi) << 32 | static_cast<uint32_t>(lo);
 }
-// Unit (kByUnit) or workgroup k of a key head, in the order in which they are begun: the sequences whose workgroups have the most
+// The unit of workgroup k of a key head, in the order in which they are begun: the sequences whose workgroups have the most
 // tiles first, of a sequence the last units first, which see the most tokens.  A long unit is shared by as many workgroups as give
 // each a little more than the average CU's load, which only the device knows.  They have neighbouring numbers, and there are no
 // gaps but where a prompt's first units need fewer: a workgroup without work that is between others leaves its CU idle for as long
 // as theirs take.  Every wave finds out by itself, a lane a sequence.  Ten pieces of 0 to 512 tokens behind up to 20000, 20 heads over
 // 4, window 4096: 63 us, with units in the order of the sequences and the same shares for all 71; eight prompts of 1 to 4096 tokens,
 // 16 heads over 4: 141 and 153.
-template <int kTokens, bool kByUnit>
+template <int kTokens>
 __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
   const int lane = threadIdx.x & 63, lanes = min(a.d.B, 64);
   Unit r = {};
@@ -128,7 +136,7 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
     work = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(work)));
     share = fmaxf(work * static_cast<float>(a.d.Hk) * kShare, static_cast<float>(least_tiles(kTokens)));
   }
-  int done = 0, done_units = 0;  // of the sequences in front of these 64
+  int done = 0;  // workgroups of the sequences in front of these 64
   for (int b0 = 0; b0 < a.d.B; b0 += 64) {
     if (b0 > 0) line = line_of<kTokens>(a, b0 + lane);
     const int splits = a.splits > 1 ? min(max(static_cast<int>(ceilf(static_cast<float>(line.tiles) / share)), 1), a.splits) : 1;
@@ -137,22 +145,15 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
     for (int d = 1; d < lanes; d <<= 1) most = max(most, __shfl_xor(most, d));
     const bool front = 2 * per > most;
     // workgroups of those in front in the upper half, of the others in the lower one
-    const int64_t mine = front ? static_cast<int64_t>(n) << 32 : n, mine_units = front ? static_cast<int64_t>(line.units) << 32 : line.units;
-    int64_t sum = mine, units = mine_units;
+    const int64_t mine = front ? static_cast<int64_t>(n) << 32 : n;
+    int64_t sum = mine;
     for (int d = 1; d < lanes; d <<= 1) {
       const int64_t o = shuffle_up64(sum, d);
       if (lane >= d) sum += o;
-      if (kByUnit) {
-        const int64_t p = shuffle_up64(units, d);
-        if (lane >= d) units += p;
-      }
     }
-    const auto before = [&](int64_t sum, int64_t mine, int done) {
-      const int fronts = __builtin_amdgcn_readlane(static_cast<int>(sum >> 32), lanes - 1);
-      return done + (front ? static_cast<int>((sum - mine) >> 32) : fronts + static_cast<int>(sum - mine));
-    };
-    const int first = before(sum, mine, done), first_unit = kByUnit ? before(units, mine_units, done_units) : 0;
-    const uint64_t here = kByUnit ? __ballot(k >= first_unit && k < first_unit + line.units) : __ballot(k >= first && k < first + n);
+    const int fronts = __builtin_amdgcn_readlane(static_cast<int>(sum >> 32), lanes - 1);
+    const int first = done + (front ? static_cast<int>((sum - mine) >> 32) : fronts + static_cast<int>(sum - mine));
+    const uint64_t here = __ballot(k >= first && k < first + n);
     if (here != 0) {
       const int l = __builtin_ctzll(here);
       const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
@@ -160,9 +161,8 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
       r.begin = of(line.begin);
       r.pos0 = of(line.pos0);
       r.splits = of(splits);
-      const int place = k - of(kByUnit ? first_unit : first), u = kByUnit ? place : place / r.splits;
-      r.split = kByUnit ? 0 : place - u * r.splits;
-      r.part = of(first) + u * r.splits;
+      const int place = k - of(first), u = place / r.splits;
+      r.split = place - u * r.splits;
       r.first_row = (of(line.units) - 1 - u) * kUnitRows;
       r.rows = min(kUnitRows, of(line.all) - r.first_row);
       see<kTokens>(a, r);
@@ -171,7 +171,6 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
       return r;
     }
     done += __builtin_amdgcn_readlane(static_cast<int>(sum >> 32) + static_cast<int>(sum), lanes - 1);
-    if (kByUnit) done_units += __builtin_amdgcn_readlane(static_cast<int>(units >> 32) + static_cast<int>(units), lanes - 1);
   }
   return r;
 }
@@ -289,6 +288,12 @@ __device__ __forceinline__ bool join_groups(Part<DP> &part, int group, int wave,
   return true;
 }
 
+// c and the two bf16 values of a register.
+__device__ __forceinline__ float add_both(uint32_t two, float c) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3f803f80u), c, false);
+}
+
 // The larger of the two values that lanes l and l + 32 hold, in both.
 __device__ __forceinline__ float both_halves_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -313,7 +318,9 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
   static_assert(kGroups == 1 || sizeof(Part<DP>) <= sizeof(lds));
 
   const int hk = static_cast<int>(blockIdx.x) % a.d.Hk;
-  const Unit unit = find_unit<kTokens, false>(a, static_cast<int>(blockIdx.x) / a.d.Hk);
+  const Unit unit = find_unit<kTokens>(a, static_cast<int>(blockIdx.x) / a.d.Hk);
+  if (a.splits > 1 && threadIdx.x == 0)
+    a.record[blockIdx.x] = Record{unit.rows, unit.first_row, unit.begin, unit.rows > 0 && unit.split == 0 && unit.splits > 1 ? unit.splits : 0};
   if (unit.rows == 0) return;
 
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane / 32;
@@ -492,14 +499,16 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
         u32x4 p[2];
         float sum;
         auto exponentials = [&] {
-          sum = 0.f;
+          float sums[2] = {0.f, 0.f};
 #pragma unroll
-          for (int r = 0; r < 16; r += 2) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[r + 1], a.scale_log2, -m));
-            sum += x;
-            sum += y;
-            p[r / 8][r / 2 % 4] = pack2(x, y);
-          }
+          for (int r = 0; r < 8; r += 2)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * g + r], a.scale_log2, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[8 * g + r + 1], a.scale_log2, -m));
+              p[g][r / 2] = pack2(x, y);
+              sums[g] = add_both(p[g][r / 2], sums[g]);
+            }
+          sum = sums[0] + sums[1];
         };
         // the values of the step, by groups of 16 tokens and 32 columns
         const char *const v_lane = vt + (32 * step + 4 * h + v_row) * Geo::kRowBytes;
@@ -574,7 +583,9 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
   static_assert(kGroups == 1 || sizeof(Part<DP>) <= sizeof(all_lds));
 
   const int hk = static_cast<int>(blockIdx.x) % a.d.Hk;
-  const Unit unit = find_unit<kTokens, false>(a, static_cast<int>(blockIdx.x) / a.d.Hk);
+  const Unit unit = find_unit<kTokens>(a, static_cast<int>(blockIdx.x) / a.d.Hk);
+  if (a.splits > 1 && threadIdx.x == 0)
+    a.record[blockIdx.x] = Record{unit.rows, unit.first_row, unit.begin, unit.rows > 0 && unit.split == 0 && unit.splits > 1 ? unit.splits : 0};
   if (unit.rows == 0) return;
 
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane / 32;
@@ -779,30 +790,49 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
 // Joins the parts of a unit, 32 of its columns a workgroup.
 template <bool kBf16, int DP>
 __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillArgs a) {
-  constexpr int kTokens = tokens_of_tile(kBf16);
-  int id = blockIdx.x;
-  const int cut = id % (DP / 32);
-  id /= DP / 32;
-  const int hk = id % a.d.Hk;
-  const Unit unit = find_unit<kTokens, true>(a, id / a.d.Hk);
-  if (unit.rows == 0 || unit.splits == 1) return;
-  // (boundaries that make sequences overlap could have more parts than there is room for)
-  if (unit.part < 0 || static_cast<int64_t>(unit.part + unit.splits) * a.d.Hk > a.parts) return;
+  constexpr int kAbreast = 4;
+  const int slot = static_cast<int>(blockIdx.x) / (DP / 32), cut = static_cast<int>(blockIdx.x) - slot * (DP / 32), hk = slot % a.d.Hk;
+  const Record unit = a.record[slot];
+  if (unit.splits == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, local = 32 * wave + (lane & 31), h = lane / 32;
   float top = kNone, sum = 0.f;
   f32x4 o[4] = {};
-#pragma unroll 2
-  for (int split = 0; split < unit.splits; ++split) {
-    const Part<DP> &part = static_cast<const Part<DP> *>(a.part)[static_cast<int64_t>(unit.part + split) * a.d.Hk + hk];
-    const float m = part.m[wave][lane], l = part.l[wave][lane];
-    const float next = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(top - next), f = __builtin_amdgcn_exp2f(m - next);
+  for (int split0 = 0; split0 < unit.splits; split0 += kAbreast) {
+    float m[kAbreast], l[kAbreast];
+    f32x4 q[kAbreast][4];
+#pragma unroll
+    for (int s = 0; s < kAbreast; ++s) {
+      const int at = slot + (split0 + s) * a.d.Hk;
+      m[s] = kNone;
+      l[s] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[s][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (split0 + s < unit.splits && at < a.parts) {  // (boundaries that make sequences overlap could have more than there is room for)
+        const Part<DP> &part = static_cast<const Part<DP> *>(a.part)[at];
+        m[s] = part.m[wave][lane];
+        l[s] = part.l[wave][lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[s][i] = part.o[wave][4 * cut + i][lane];
+      }
+    }
+    float next = top;
+#pragma unroll
+    for (int s = 0; s < kAbreast; ++s) next = fmaxf(next, m[s]);
+    const float keep = __builtin_amdgcn_exp2f(top - next);
     top = next;
-    sum = fmaf(sum, keep, l * f);
+    sum *= keep;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x4 q = part.o[wave][4 * cut + i][lane];
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) o[i][r] = fmaf(o[i][r], keep, q[r] * f);
+      for (int r = 0; r < 4; ++r) o[i][r] *= keep;
+#pragma unroll
+    for (int s = 0; s < kAbreast; ++s) {
+      const float f = __builtin_amdgcn_exp2f(m[s] - next);
+      sum = fmaf(l[s], f, sum);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[i][r] = fmaf(q[s][i][r], f, o[i][r]);
     }
   }
   if (local >= unit.rows) return;
@@ -871,7 +901,7 @@ hipError_t launch(const PrefillArgs &a, hipStream_t stream) {
       hipLaunchKernelGGL((prefill_bf16_kernel<DP, false, 1>), grid, threads, 0, stream, a);
   }
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-  hipLaunchKernelGGL((prefill_join_kernel<kBf16, DP>), dim3(static_cast<unsigned>(a.units) * a.d.Hk * (DP / 32)), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((prefill_join_kernel<kBf16, DP>), dim3(grid.x * (DP / 32)), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 template <bool kBf16>
@@ -879,12 +909,14 @@ hipError_t launch(const PrefillArgs &a, hipStream_t stream) {
   return a.d.D <= 64 ? launch<kBf16, 64>(a, stream) : a.d.D <= 128 ? launch<kBf16, 128>(a, stream) : launch<kBf16, 256>(a, stream);
 }
 
+size_t part_bytes(const AttnDims &d) { return d.D <= 64 ? sizeof(Part<64>) : d.D <= 128 ? sizeof(Part<128>) : sizeof(Part<256>); }
+
 }  // namespace
 
 size_t attn_prefill_workspace_bytes(const AttnDims &d) {
   const Plan p = plan_of(d);
   if (!p.shared) return 256;
-  return (static_cast<size_t>(p.units) * d.Hk + kMostParts) * (d.D <= 64 ? sizeof(Part<64>) : d.D <= 128 ? sizeof(Part<128>) : sizeof(Part<256>));
+  return (static_cast<size_t>(p.units) * d.Hk + kMostParts) * (part_bytes(d) + sizeof(Record));
 }
 
 hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32_t *lens, const int32_t *table, const void *q,
@@ -899,12 +931,13 @@ hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32
   a.k = k_cache;
   a.v = v_cache;
   a.y = y;
-  a.part = workspace;
   a.d = d;
   a.inv_group = inverse_of(d.G);
   a.units = p.units;
   a.splits = p.shared ? kMostSplits : 1;
-  a.parts = p.units * d.Hk + kMostParts;
+  a.parts = p.shared ? p.units * d.Hk + kMostParts : 0;
+  a.part = workspace;
+  a.record = reinterpret_cast<Record *>(static_cast<char *>(workspace) + a.parts * part_bytes(d));
   a.groups = p.groups;
   a.scale_log2 = scale * 1.44269504f;
   return d.bf16 ? launch<true>(a, stream) : launch<false>(a, stream);
