@@ -120,13 +120,39 @@ __device__ __forceinline__ int64_t shuffle_up64(int64_t v, int k) {
 // tiles first, of a sequence the last units first, which see the most tokens.  A long unit is shared by as many workgroups as give
 // each a little more than the average CU's load, which only the device knows.  They have neighbouring numbers, and there are no
 // gaps but where a prompt's first units need fewer: a workgroup without work that is between others leaves its CU idle for as long
-// as theirs take.  Every wave finds out by itself, a lane a sequence.  Ten pieces of 0 to 512 tokens behind up to 20000, 20 heads over
+// as theirs take.  Every wave finds out by itself, a lane a sequence.  (Many sequences, whose units are many and not shared, are not
+// gone through: 1024 of 4 tokens behind 200, 32 heads over 8: 232 us, gone through in order 432.)  Ten pieces of 0 to 512 tokens behind up to 20000, 20 heads over
 // 4, window 4096: 63 us, with units in the order of the sequences and the same shares for all 71; eight prompts of 1 to 4096 tokens,
 // 16 heads over 4: 141 and 153.
 template <int kTokens>
 __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
   const int lane = threadIdx.x & 63, lanes = min(a.d.B, 64);
   Unit r = {};
+  if (a.splits == 1 && a.d.B > 64) {
+    // Sequence b's units are counted from cu[b] * group / rows + b on: these are at least as far apart as its units are many.
+    const int u = a.units - 1 - k;
+    const auto first_unit = [&](int b) { return static_cast<int64_t>(min(max(a.cu[b], 0), a.d.T)) * a.d.G / kUnitRows + b; };
+    int low = 0, high = a.d.B;  // the last one that does not begin behind u is in [low, high)
+    while (high - low > 1) {
+      const int step = (high - low + 63) / 64, b = low + lane * step;
+      const uint64_t m = __ballot(b < high && first_unit(b) <= u);
+      if (m == 0) return r;
+      low += (63 - __builtin_clzll(m)) * step;
+      high = min(high, low + step);
+    }
+    low = __builtin_amdgcn_readfirstlane(low);
+    const Line line = line_of<kTokens>(a, low);
+    const int64_t place = u - first_unit(low);
+    if (place < 0 || place >= line.units) return r;
+    r.seq = low;
+    r.begin = line.begin;
+    r.pos0 = line.pos0;
+    r.splits = 1;
+    r.first_row = static_cast<int>(place) * kUnitRows;
+    r.rows = min(kUnitRows, line.all - r.first_row);
+    see<kTokens>(a, r);
+    return r;
+  }
   Line line = line_of<kTokens>(a, lane);
   float share = 0.f;  // tiles that a workgroup is to have
   if (a.splits > 1) {

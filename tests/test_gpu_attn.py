@@ -150,6 +150,21 @@ def test_prefill_many_sequences(ssd, batch, io):
         assert_close(y, ref, TOL[io], "prefill")
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("batch", [65, 200, 4200])
+def test_prefill_many_units(ssd, batch, io):
+    """Units enough for every CU several times over: sequences are searched for, in steps of 64."""
+    rng = np.random.default_rng(batch)
+    new, prior = rng.integers(0, 9, batch), rng.integers(0, 20, batch)
+    new[rng.integers(0, batch, batch // 4)] = 0
+    new[-1] = 0
+    new[batch // 2] = 150
+    s = make([int(n) for n in new + prior], 24, 12, 16, 8, io, new=[int(n) for n in new], seed=batch)
+    print("prefill", batch, io, flush=True)
+    y = run_prefill(ssd, s)
+    assert_close(y, block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], s["cu"]), TOL[io], "prefill")
+
+
 def test_prefill_overlapping_boundaries_stay_inside(ssd):
     """Boundaries that count tokens many times over: results are anything, what surrounds y and the caches stays as it was."""
     s = make([3000] * 40, 4, 1, 64, 16, "bf16", new=[20] * 40, seed=50)
