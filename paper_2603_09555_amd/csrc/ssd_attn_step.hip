@@ -13,13 +13,13 @@
 //     neighbouring columns of each, and makes the columns' operands by exchanging halves of registers (bf16; fp32 needs none).
 //
 // The waves of a workgroup take every kWaves-th tile of a unit (a sequence and key head) and are joined through LDS at its end.
-// What hides the latency of memory is other waves' requests; where a SIMD has no more than two waves, the next tile's keys are asked
-// for before this one is worked on, and its page numbers a tile earlier.
+// What hides the latency of memory is other waves' requests; where there are too few, the next tile's keys are asked for before
+// this one is worked on, and its page numbers a tile earlier.
 //
 // Work is dealt by length: the visible tokens of all sequences and key heads, in blocks of 128, make one long list of which every
 // workgroup takes an equal run, whatever the lengths are.  A unit within one workgroup is finished there; the others leave
-// (m, l, O) in the workspace, which a second launch joins.  Where no sequence can be long, a workgroup of eight waves takes a unit
-// and there is no second launch.
+// (m, l, O) in the workspace, which a second launch joins.  Where no sequence can be long, a workgroup of eight waves, or four
+// where there are many units, takes a unit and there is no second launch.
 //
 // 32 heads over 8 of 128, bf16: 64 sequences to 32768 tokens 165 us, 5.4 TB/s of K and V; one of 32000 28 us, one of 518 8.8 us.
 // fp32, 2 sequences to 100004, 10 heads over 2 of 64: 42 us, 4.9 TB/s.
@@ -36,7 +36,7 @@ constexpr int kThreads = kDealers, kTile = 32, kBlock = kThreads / 64 * kTile, k
 // Workgroups that work is dealt to: as many as are in work at a time, four to one a CU as their registers allow.
 constexpr int workgroups_of(bool bf16, int dp) { return 256 * (dp == 256 ? 1 : bf16 ? (dp == 64 ? 4 : 3) : dp == 64 ? 3 : 2); }
 constexpr int kMostWorkgroups = 1024;
-constexpr unsigned kFewUnits = 256;
+constexpr unsigned kFewUnits = 256, kCUs = 256;
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
 
 // The workgroups that have blocks of a unit.  They write it down, so that the joining launch need not deal again.
@@ -182,7 +182,8 @@ __device__ __forceinline__ int64_t run_of(const StepArgs &a, int64_t total) { re
 template <bool kBf16, int DP, int kWaves, bool kDealt>
 __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_kernel(const StepArgs a) {
   using T = Tile<kBf16, DP>;
-  constexpr bool kAhead = kDealt ? kBf16 && DP == 256 : kBf16 || DP == 64;
+  // keys are asked for a tile ahead where that costs no wave, or where there is none to lose
+  constexpr bool kAhead = kDealt ? kBf16 && DP == 256 : kWaves == 8 ? kBf16 || DP == 64 : kBf16 && DP != 128;
   __shared__ union {
     Prefix prefix;
     struct {
@@ -533,18 +534,25 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int ro
 // tokens: 8.8 and 9.9 dealt; of 2000: 22 and 10; 16 of 2000: 23 and 30.  A sequence of more than a MiB a key head, 20 us for a
 // workgroup, may be the only one that long: then work is dealt.
 bool dealt(const AttnDims &d) {
-  const double longest = 2.0 * d.capacity() * d.D * (d.bf16 ? 2 : 4), all = 0.5 * longest * d.B * units_of(d);
+  const double tokens = d.window > 0 ? std::min(d.capacity(), d.window) : d.capacity();
+  const double longest = 2.0 * tokens * d.D * (d.bf16 ? 2 : 4), all = 0.5 * longest * d.B * units_of(d);
   if (longest > 1048576.0) return true;
   return 4.0 + std::max(longest / 52.0e3, all / 6.0e6) > 12.0 + all / 5.2e6;
 }
 
+// A unit to a workgroup: of eight waves where there is a CU for each; of four otherwise, of which two or three share a CU, so that
+// the start of one is beside the others' work.  32 heads over 8 of 128, bf16: 16 sequences of 500 tokens 9.1 us and 12.5, 64 of 250
+// 15.0 and 12.5, of 1000 41.7 and 38.7, 1024 of 1 to 200 134 and 52.
 template <bool kBf16, int DP>
 void launch_step(const StepArgs &a, hipStream_t stream) {
   constexpr int kWide = DP <= 128 ? 8 : 4;  // waves: two a SIMD, where registers allow
+  const unsigned units = static_cast<unsigned>(a.units) * a.d.B;
   if (dealt(a.d))
     hipLaunchKernelGGL((step_kernel<kBf16, DP, kThreads / 64, true>), dim3(a.workgroups), dim3(kThreads), 0, stream, a);
+  else if (units <= kCUs)
+    hipLaunchKernelGGL((step_kernel<kBf16, DP, kWide, false>), dim3(units), dim3(64 * kWide), 0, stream, a);
   else
-    hipLaunchKernelGGL((step_kernel<kBf16, DP, kWide, false>), dim3(static_cast<unsigned>(a.units) * a.d.B), dim3(64 * kWide), 0, stream, a);
+    hipLaunchKernelGGL((step_kernel<kBf16, DP, 4, false>), dim3(units), dim3(256), 0, stream, a);
 }
 
 template <bool kBf16>

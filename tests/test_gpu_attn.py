@@ -99,6 +99,19 @@ def test_step_many_sequences_dealt(ssd, batch):
         assert_close(y, block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], window=window), TOL["bf16"], "step")
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [(4, 2, 64, 16), (3, 1, 128, 1), (2, 1, 256, 64), (20, 1, 72, 8)], ids=lambda h: "x".join(map(str, h)))
+def test_step_many_short_sequences(ssd, heads, io):
+    """More sequences and key heads than CUs, none of them long."""
+    lengths = np.random.default_rng(7).integers(0, 200, 300)
+    lengths[::7] = 0
+    s = make([int(n) for n in lengths], *heads, io, seed=60)
+    for window in (0, 33):
+        print("step", heads, io, window, flush=True)
+        y = run_step(ssd, s, window=window)
+        assert_close(y, block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], window=window), TOL[io], "step")
+
+
 PIECES = [  # new tokens, cached tokens
     ([1], [0]), ([5], [0]), ([0, 3, 0, 0, 70, 1], [9, 0, 0, 5, 130, 64]), ([64, 65, 63], [0, 64, 1]), ([260], [0]), ([7, 129], [1000, 513]),
 ]
