@@ -30,7 +30,8 @@ using namespace block;
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kWaveRows = 32, kUnitRows = kWaves * kWaveRows;
 constexpr int kWorkgroups = 256;  // of eight waves, which fill the GPU
 constexpr int kManyUnits = 768;   // units that four waves each take,
-constexpr int kManyTiles = 16;    // unless they have fewer tiles
+constexpr int kManyTiles = 16;    // unless they have fewer tiles,
+constexpr int kFewTiles = 6;      // or, where there is a CU for each, fewer than these
 constexpr int kMostSplits = 64;   // of a unit
 // Where units are shared, a workgroup is to have a little more than its part of all tiles.  A unit has less than twice its
 // sequence's average of them, so that there are at most 2 kWorkgroups / 1.125 workgroups more than units.
@@ -38,9 +39,10 @@ constexpr float kShare = 1.125f / kWorkgroups;
 constexpr int kMostParts = 2 * kWorkgroups;
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
 constexpr int tokens_of_tile(bool bf16) { return bf16 ? 64 : 32; }
-// Tiles that a workgroup at least takes where several share a unit: 1.0 us of work in bf16 a tile and CU with heads of 128 values,
-// 2.0 in fp32.
-constexpr int least_tiles(int tokens) { return tokens == tokens_of_tile(true) ? 8 : 4; }
+// Tiles that a workgroup at least takes where several share a unit, in us 5 in bf16 and 8 in fp32 with heads of 128 values alone on
+// a CU: fewer cost more in parts than they save.  (bf16, 3 tokens behind 27000, 8 heads over 1, window 927: 15 us, with 8 tiles 18; 90
+// pieces of 0 to 6 tokens behind up to 2000, 16 heads over 2: 28.6 and 26.7.)
+inline int least_tiles(const AttnDims &d) { return d.bf16 ? 5 : 4; }
 // There is no search for the largest score of a step: the sum of a lane's probabilities, which is needed anyway, says whether one is
 // too large for the running maximum.  Until then they are up to this (bf16, 16384 tokens: 2.07 ms, a search for every step 2.28).
 // bf16: what is summed are the probabilities as they are rounded for their product with the values, so that the rounding of a token
@@ -63,6 +65,7 @@ struct PrefillArgs {
   uint32_t inv_group;
   int units;         // at most, of a key head
   int splits;        // at most, of a unit
+  int least;         // tiles of a split
   int parts;         // there is room for
   int groups;        // of waves, a workgroup (bf16)
   float scale_log2;  // scale * log2(e)
@@ -160,7 +163,7 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
     for (int b0 = 64; b0 < a.d.B; b0 += 64) work += line_of<kTokens>(a, b0 + lane).work;
     for (int d = 1; d < lanes; d <<= 1) work += __shfl_xor(work, d);
     work = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(work)));
-    share = fmaxf(work * static_cast<float>(a.d.Hk) * kShare, static_cast<float>(least_tiles(kTokens)));
+    share = fmaxf(work * static_cast<float>(a.d.Hk) * kShare, static_cast<float>(a.least));
   }
   int done = 0;  // workgroups of the sequences in front of these 64
   for (int b0 = 0; b0 < a.d.B; b0 += 64) {
@@ -192,7 +195,7 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
       r.first_row = (of(line.units) - 1 - u) * kUnitRows;
       r.rows = min(kUnitRows, of(line.all) - r.first_row);
       see<kTokens>(a, r);
-      r.splits = max(1, min(r.splits, (r.tiles + least_tiles(kTokens) - 1) / least_tiles(kTokens)));
+      r.splits = max(1, min(r.splits, (r.tiles + a.least - 1) / a.least));
       if (r.split >= r.splits) r.rows = 0;
       return r;
     }
@@ -875,7 +878,8 @@ struct Plan {
 };
 // bf16: two groups of waves share a unit where that leaves every CU a workgroup or few more: 2048 tokens, 32 heads over 8 of 128, 520
 // units: 52 us, with a group each 56; 4096 tokens, 1032 units: 170 and 155.  Units of few tiles are not worth it: four times 512
-// tokens, 8 tiles: 31 and 25; 1024 tokens, 16 tiles: 24 and 27.
+// tokens, 8 tiles: 31 and 25; 1024 tokens, 16 tiles: 24 and 27; but where there is a CU for each, once 512 tokens: 17.4 and 18.3, 200
+// tokens, 4 tiles: 12.8 and 11.6.
 //
 // A unit's tiles may be shared by several workgroups where that could shorten the longest row of units a CU works on by more than
 // the parts' way through memory and the second launch take.  The host knows the rows of all sequences together, not of each, and
@@ -887,7 +891,7 @@ Plan plan_of(const AttnDims &d) {
   const int64_t all = static_cast<int64_t>(p.units) * d.Hk;
   const int64_t most_seen = d.window > 0 ? std::min<int64_t>(d.capacity(), static_cast<int64_t>(d.window) + kUnitRows / d.G) : d.capacity();
   const int64_t tiles = (most_seen + tokens_of_tile(d.bf16) - 1) / tokens_of_tile(d.bf16);
-  p.groups = d.bf16 && d.D <= 128 && all < kManyUnits && tiles >= kManyTiles ? 2 : 1;
+  p.groups = d.bf16 && d.D <= 128 && all < kManyUnits && tiles >= (all <= kWorkgroups ? kFewTiles : kManyTiles) ? 2 : 1;
   p.shared = false;
   if (all >= kManyUnits) return p;
   // in us: a tile on a CU, a part written and read
@@ -897,7 +901,7 @@ Plan plan_of(const AttnDims &d) {
   // the same each, and the last CU to begin one decides
   const bool prompts = most_seen <= 2 * static_cast<int64_t>(d.T / d.B);
   double whole = 0.0;
-  for (int s = 1; s == 1 || (s <= kMostSplits && (s - 1) * least_tiles(tokens_of_tile(d.bf16)) < tiles); ++s) {
+  for (int s = 1; s == 1 || (s <= kMostSplits && (s - 1) * least_tiles(d) < tiles); ++s) {
     const double longest = static_cast<double>(tiles) / s;
     const double row = prompts ? std::max(longest, units * tiles / 2 / kWorkgroups) + longest / 4 : std::ceil(units * s / kWorkgroups) * longest;
     const double cost = row * tile + (s > 1 ? launch + part * units * s : 0.0);
@@ -961,6 +965,7 @@ hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32
   a.inv_group = inverse_of(d.G);
   a.units = p.units;
   a.splits = p.shared ? kMostSplits : 1;
+  a.least = least_tiles(d);
   a.parts = p.shared ? p.units * d.Hk + kMostParts : 0;
   a.part = workspace;
   a.record = reinterpret_cast<Record *>(static_cast<char *>(workspace) + a.parts * part_bytes(d));
