@@ -34,15 +34,16 @@ constexpr int kManyTiles = 16;    // unless they have fewer tiles,
 constexpr int kFewTiles = 6;      // or, where there is a CU for each, fewer than these
 constexpr int kMostSplits = 64;   // of a unit
 // Where units are shared, a workgroup is to have a little more than its part of all tiles.  A unit has less than twice its
-// sequence's average of them, so that there are at most 2 kWorkgroups / 1.125 workgroups more than units.
-constexpr float kShare = 1.125f / kWorkgroups;
+// sequence's average of them, so that there are at most 2 kWorkgroups / 1.25 workgroups more than units.
+constexpr float kShare = 1.25f / kWorkgroups;
 constexpr int kMostParts = 2 * kWorkgroups;
+constexpr float kLongShare = 64.f;  // tiles, from which on the number of rounds is looked at
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
 constexpr int tokens_of_tile(bool bf16) { return bf16 ? 64 : 32; }
 // Tiles that a workgroup at least takes where several share a unit, in us 5 in bf16 and 8 in fp32 with heads of 128 values alone on
 // a CU: fewer cost more in parts than they save.  (bf16, 3 tokens behind 27000, 8 heads over 1, window 927: 15 us, with 8 tiles 18; 90
 // pieces of 0 to 6 tokens behind up to 2000, 16 heads over 2: 28.6 and 26.7.)
-inline int least_tiles(const AttnDims &d) { return d.bf16 ? 5 : 4; }
+inline int least_tiles(const AttnDims &d) { return d.bf16 ? 5 : d.D <= 128 ? 4 : 2; }
 // There is no search for the largest score of a step: the sum of a lane's probabilities, which is needed anyway, says whether one is
 // too large for the running maximum.  Until then they are up to this (bf16, 16384 tokens: 2.07 ms, a search for every step 2.28).
 // bf16: what is summed are the probabilities as they are rounded for their product with the values, so that the rounding of a token
@@ -115,9 +116,44 @@ __device__ __forceinline__ Line line_of(const PrefillArgs &a, int b) {
   r.work = 0.5f * static_cast<float>(r.units) * static_cast<float>(first_tiles + r.tiles);
   return r;
 }
+__device__ __forceinline__ int splits_of(const PrefillArgs &a, float tiles, float share) {
+  return min(max(static_cast<int>(ceilf(tiles / share)), 1), a.splits);
+}
 __device__ __forceinline__ int64_t shuffle_up64(int64_t v, int k) {
   const int lo = __shfl_up(static_cast<int>(v), k), hi = __shfl_up(static_cast<int>(v >> 32), k);
   return static_cast<int64_t>(hi) << 32 | static_cast<uint32_t>(lo);
+}
+// Where workgroups have much to do and there are more than CUs, the number that a CU gets one after the other decides.  A lane
+// reckons for the longest unit shared by as many workgroups as the lane's number and one: how many rounds those make which have
+// about the most to do, and what the parts cost, in tiles.  (It takes 3 us.)  32 heads over 8 of 128: 640 tokens behind 30000 484 us
+// without this and 357 with, twice 300 behind 8000 144 and 115; four times 156 behind 32000, 25 heads over 5, 510 and 394.
+__device__ __forceinline__ float best_share(const PrefillArgs &a, const Line &line, int lanes, float load, float share) {
+  const int lane = threadIdx.x & 63;
+  int longest = line.tiles, simply = line.units * splits_of(a, static_cast<float>(line.tiles), share);
+#pragma unroll 1
+  for (int d = 1; d < lanes; d <<= 1) {
+    longest = max(longest, __shfl_xor(longest, d));
+    simply += __shfl_xor(simply, d);
+  }
+  if (__builtin_amdgcn_readfirstlane(simply) * a.d.Hk <= kWorkgroups) return share;
+  const float tiles_of_longest = 1.0001f * static_cast<float>(__builtin_amdgcn_readfirstlane(longest));
+  const float mine = fmaxf(tiles_of_longest / static_cast<float>(lane + 1), static_cast<float>(a.least));
+  int all = 0, front = 0;
+#pragma unroll 1
+  for (int b = 0; b < lanes; ++b) {
+    const int units = __builtin_amdgcn_readlane(line.units, b);
+    const float tiles = static_cast<float>(__builtin_amdgcn_readlane(line.tiles, b));
+    const int splits = splits_of(a, tiles, mine);
+    all += units * splits;
+    if (2.f * tiles > mine * static_cast<float>(splits)) front += units * splits;
+  }
+  const float cost = fmaxf(ceilf(static_cast<float>(front * a.d.Hk) * (1.f / kWorkgroups)) * mine, load) + 0.04f * static_cast<float>(all * a.d.Hk);
+  // (the least of them, with its lane in the last bits)
+  uint32_t least = all * a.d.Hk > a.parts ? 0xffffffffu : (__float_as_uint(cost) & ~63u) | static_cast<uint32_t>(lane);
+#pragma unroll 1
+  for (int d = 1; d < 64; d <<= 1) least = min(least, static_cast<uint32_t>(__shfl_xor(static_cast<int>(least), d)));
+  least = __builtin_amdgcn_readfirstlane(least);
+  return least == 0xffffffffu ? share : fmaxf(tiles_of_longest / static_cast<float>((least & 63u) + 1u), static_cast<float>(a.least));
 }
 // The unit of workgroup k of a key head, in the order in which they are begun: the sequences whose workgroups have the most
 // tiles first, of a sequence the last units first, which see the most tokens.  A long unit is shared by as many workgroups as give
@@ -164,11 +200,12 @@ __device__ __forceinline__ Unit find_unit(const PrefillArgs &a, int k) {
     for (int d = 1; d < lanes; d <<= 1) work += __shfl_xor(work, d);
     work = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(work)));
     share = fmaxf(work * static_cast<float>(a.d.Hk) * kShare, static_cast<float>(a.least));
+    if (a.d.B <= 64 && share > kLongShare) share = best_share(a, line, lanes, work * static_cast<float>(a.d.Hk) / kWorkgroups, share);
   }
   int done = 0;  // workgroups of the sequences in front of these 64
   for (int b0 = 0; b0 < a.d.B; b0 += 64) {
     if (b0 > 0) line = line_of<kTokens>(a, b0 + lane);
-    const int splits = a.splits > 1 ? min(max(static_cast<int>(ceilf(static_cast<float>(line.tiles) / share)), 1), a.splits) : 1;
+    const int splits = a.splits > 1 ? splits_of(a, static_cast<float>(line.tiles), share) : 1;
     const int n = line.units * splits, per = line.tiles / splits;
     int most = per;
     for (int d = 1; d < lanes; d <<= 1) most = max(most, __shfl_xor(most, d));

@@ -178,6 +178,19 @@ def test_prefill_many_units(ssd, batch, io):
     assert_close(y, block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], s["cu"]), TOL[io], "prefill")
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_prefill_late_pieces_of_many_heads(ssd, io):
+    """Pieces with enough to do for every CU that the number of rounds decides how units are shared."""
+    new, prior = [40, 30, 23, 0, 40], [19000, 18500, 17000, 100, 18990]
+    s = make([a + b for a, b in zip(new, prior)], 48, 24, 16, 32, io, new=new, seed=70)
+    print("prefill late", io, flush=True)
+    y = run_prefill(ssd, s)
+    some = slice(None, None, 11)
+    q, cu = s["q"], s["cu"]
+    ref = block_oracle.attention(q, s["k"], s["v"], s["table"], s["lens"], cu)
+    assert_close(y[some], ref[some], TOL[io], "prefill")
+
+
 def test_prefill_overlapping_boundaries_stay_inside(ssd):
     """Boundaries that count tokens many times over: results are anything, what surrounds y and the caches stays as it was."""
     s = make([3000] * 40, 4, 1, 64, 16, "bf16", new=[20] * 40, seed=50)
