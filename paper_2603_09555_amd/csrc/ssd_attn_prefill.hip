@@ -8,14 +8,14 @@
 //   S^T (tokens x rows) = K Q^T,   p = 2^(S - m),   O^T (values x rows) += V^T P^T
 //
 // Tiles of K and V (64 tokens; fp32: 32) go through LDS, the next one being on its way while one is worked on.  fp32 is taken apart
-// into three values of bf16 each, and six products stand for one.  The first
-// product leaves a lane with tokens 8i + 4h .. 8i + 4h + 3 (h = lane / 32) of its row; these are what it supplies as the second
-// operand of V^T P^T, whose first operand comes from LDS by transposing reads, with the same order of tokens.
+// into three values of bf16 each, and six products stand for one.  The first product leaves a lane with tokens 8i + 4h .. 8i + 4h + 3
+// (h = lane / 32) of its row; these are what it supplies as the second operand of V^T P^T, whose first operand comes from LDS by
+// transposing reads, with the same order of tokens.
 //
 // Where there are few units, several workgroups share one's tokens and leave (m, l, O) in the workspace for a second launch.
 //
 // 32 heads over 8 of 128, bf16: 16384 tokens 2.05 ms, 1070 TFLOP/s of the causal products (the library's large product: 1316); 4096
-// tokens 147 us, 1024 tokens 24 us; 64 tokens behind 32000 51 us.  fp32: see its kernel.
+// tokens 147 us, 1024 tokens 25 us; 64 tokens behind 32000 54 us.  fp32: see its kernel.
 #include <algorithm>
 #include <cmath>
 
@@ -29,9 +29,9 @@ using namespace block;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kWaveRows = 32, kUnitRows = kWaves * kWaveRows;
 constexpr int kWorkgroups = 256;  // of eight waves, which fill the GPU
-constexpr int kManyUnits = 768;   // units that four waves each take,
-constexpr int kManyTiles = 16;    // unless they have fewer tiles,
-constexpr int kFewTiles = 6;      // or, where there is a CU for each, fewer than these
+constexpr int kManyUnits = 768;   // from so many on, a unit is for one group of four waves, and not shared
+constexpr int kManyTiles = 16;    // two groups of waves are for units of so many tiles,
+constexpr int kFewTiles = 6;      // of so many where there is a CU for each unit
 constexpr int kMostSplits = 64;   // of a unit
 // Where units are shared, a workgroup is to have a little more than its part of all tiles.  A unit has less than twice its
 // sequence's average of them, so that there are at most 2 kWorkgroups / 1.25 workgroups more than units.
