@@ -21,7 +21,7 @@
 // (m, l, O) in the workspace, which a second launch joins.  Where no sequence can be long, a workgroup of eight waves, or four
 // where there are many units, takes a unit and there is no second launch.
 //
-// 32 heads over 8 of 128, bf16: 64 sequences to 32768 tokens 165 us, 5.4 TB/s of K and V; one of 32000 28 us, one of 518 8.8 us.
+// 32 heads over 8 of 128, bf16: 64 sequences to 32768 tokens 150 us, 5.9 TB/s of K and V; one of 32000 28 us, one of 518 8.8 us.
 // fp32, 2 sequences to 100004, 10 heads over 2 of 64: 42 us, 4.9 TB/s.
 #include <algorithm>
 
@@ -111,6 +111,7 @@ struct Tile {
       keys.of[half][i] = q;
     }
   }
+  template <bool kOnce>
   __device__ __forceinline__ void load_value(int i, const char *row, int n, int bytes) {
 #pragma unroll
     for (int p = 0; p < kValuePieces; ++p) {
@@ -118,11 +119,11 @@ struct Tile {
       u32x4 q = {0u, 0u, 0u, 0u};
       if (at < bytes) {
         if (kHalfPiece) {
-          const u32x2 h = *reinterpret_cast<const u32x2 *>(row + at);
+          const u32x2 h = kOnce ? __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(row + at)) : *reinterpret_cast<const u32x2 *>(row + at);
           q[0] = h[0];
           q[1] = h[1];
         } else {
-          q = *reinterpret_cast<const u32x4 *>(row + at);
+          q = kOnce ? __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(row + at)) : *reinterpret_cast<const u32x4 *>(row + at);
         }
       }
       val[i][p] = q;
@@ -179,7 +180,8 @@ __device__ __forceinline__ int64_t quotient64(int64_t n, int64_t d) {
 }
 __device__ __forceinline__ int64_t run_of(const StepArgs &a, int64_t total) { return quotient64(total + a.workgroups - 1, a.workgroups); }
 
-template <bool kBf16, int DP, int kWaves, bool kDealt>
+// kOnce: values go past the caches.
+template <bool kBf16, int DP, int kWaves, bool kDealt, bool kOnce>
 __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_kernel(const StepArgs a) {
   using T = Tile<kBf16, DP>;
   // keys are asked for a tile ahead where that costs no wave, or where there is none to lose
@@ -317,7 +319,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
           for (int r = 0; r < 4; ++r) {
             const int token = min(max(first + 16 * h + 4 * j + r, sp.lo), sp.len - 1);
             const int64_t row = token >> 2 == (first + 16 * h + 4 * j) >> 2 ? where + (token & page_mask) * bytes : where;
-            t.load_value(4 * h + r, vh + row, n, bytes);
+            t.template load_value<kOnce>(4 * h + r, vh + row, n, bytes);
           }
         }
       } else {
@@ -326,7 +328,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int token = min(max(first + 16 * h + 4 * j + r, sp.lo), sp.len - 1);
-            t.load_value(4 * h + r, vh + __shfl(pages.of[h], 4 * j + r) * page_bytes + (token & page_mask) * bytes, n, bytes);
+            t.template load_value<kOnce>(4 * h + r, vh + __shfl(pages.of[h], 4 * j + r) * page_bytes + (token & page_mask) * bytes, n, bytes);
           }
       }
       if (kAhead) {  // (behind the last tile: the last token's, not used)
@@ -543,16 +545,27 @@ bool dealt(const AttnDims &d) {
 // A unit to a workgroup: of eight waves where there is a CU for each; of four otherwise, of which two or three share a CU, so that
 // the start of one is beside the others' work.  32 heads over 8 of 128, bf16: 16 sequences of 500 tokens 9.1 us and 12.5, 64 of 250
 // 15.0 and 12.5, of 1000 41.7 and 38.7, 1024 of 1 to 200 134 and 52.
-template <bool kBf16, int DP>
+//
+// Caches that do not fit the last-level cache (256 MiB) have been pushed out of it by the time they are read again: there, values, of
+// which an instruction reads whole lines, are loaded as data of no further use, and leave room for the keys, of which one reads half
+// lines.  64 sequences to 32768 165 us and 150, 16 of 8000 103 and 84; with caches that fit 16 of 2000 23 and 27.  (Both so: 16 of 8000
+// 90.)
+template <bool kBf16, int DP, bool kOnce>
 void launch_step(const StepArgs &a, hipStream_t stream) {
   constexpr int kWide = DP <= 128 ? 8 : 4;  // waves: two a SIMD, where registers allow
   const unsigned units = static_cast<unsigned>(a.units) * a.d.B;
   if (dealt(a.d))
-    hipLaunchKernelGGL((step_kernel<kBf16, DP, kThreads / 64, true>), dim3(a.workgroups), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((step_kernel<kBf16, DP, kThreads / 64, true, kOnce>), dim3(a.workgroups), dim3(kThreads), 0, stream, a);
   else if (units <= kCUs)
-    hipLaunchKernelGGL((step_kernel<kBf16, DP, kWide, false>), dim3(units), dim3(64 * kWide), 0, stream, a);
+    hipLaunchKernelGGL((step_kernel<kBf16, DP, kWide, false, false>), dim3(units), dim3(64 * kWide), 0, stream, a);
   else
-    hipLaunchKernelGGL((step_kernel<kBf16, DP, 4, false>), dim3(units), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((step_kernel<kBf16, DP, 4, false, kOnce>), dim3(units), dim3(256), 0, stream, a);
+}
+template <bool kBf16, int DP>
+void launch_step(const StepArgs &a, hipStream_t stream) {
+  const double caches = 2.0 * a.d.npages * (static_cast<double>(a.d.Hk) * (1 << a.d.lg_page)) * a.d.D * (kBf16 ? 2 : 4);
+  if (caches > 335544320.0) launch_step<kBf16, DP, true>(a, stream);
+  else launch_step<kBf16, DP, false>(a, stream);
 }
 
 template <bool kBf16>

@@ -112,6 +112,24 @@ def test_step_many_short_sequences(ssd, heads, io):
         assert_close(y, block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"], window=window), TOL[io], "step")
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("headdim", [64, 128, 256])
+@pytest.mark.parametrize("batch", [3, 150])
+def test_step_on_large_caches(ssd, batch, headdim, io):
+    """Caches of more than the last-level cache holds, of which little is used: work dealt, and a unit to a workgroup."""
+    lengths = np.random.default_rng(8).integers(1, 300, batch)
+    s = make([int(n) for n in lengths], 4, 2, headdim, 16, io, seed=61, more_pages=-(-600000 // headdim // 16) if batch == 3 else 0)
+    d = dev(s)
+    pages = 360 * 1024 * 1024 // (2 * 2 * 16 * headdim * (2 if io == "bf16" else 4))
+    k, v = (torch.full((pages, 2, 16, headdim), float("nan"), dtype=t.dtype, device="cuda") for t in (d["k"], d["v"]))
+    k[-d["k"].shape[0]:], v[-d["v"].shape[0]:] = d["k"], d["v"]
+    table = torch.where(d["table"] < 0, d["table"], d["table"] + pages - d["k"].shape[0])
+    print("step", batch, headdim, io, pages, flush=True)
+    y = ssd.ssd_attn_step(d["q"], k, v, table, d["lens"])
+    torch.cuda.synchronize()
+    assert_close(y, block_oracle.attention(s["q"], s["k"], s["v"], s["table"], s["lens"]), TOL[io], "step")
+
+
 PIECES = [  # new tokens, cached tokens
     ([1], [0]), ([5], [0]), ([0, 3, 0, 0, 70, 1], [9, 0, 0, 5, 130, 64]), ([64, 65, 63], [0, 64, 1]), ([260], [0]), ([7, 129], [1000, 513]),
 ]
