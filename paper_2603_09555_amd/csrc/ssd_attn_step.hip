@@ -22,7 +22,7 @@
 // where there are many units, takes a unit and there is no second launch.
 //
 // 32 heads over 8 of 128, bf16: 64 sequences to 32768 tokens 150 us, 5.9 TB/s of K and V; one of 32000 28 us, one of 518 8.8 us.
-// fp32, 2 sequences to 100004, 10 heads over 2 of 64: 42 us, 4.9 TB/s.
+// fp32, 2 sequences to 100004, 10 heads over 2 of 64: 41 us, 5.0 TB/s.
 #include <algorithm>
 
 #include "ssd_attn.hpp"
@@ -442,11 +442,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
   }
 }
 
-// Joins what the workgroups of a unit left.  A workgroup takes `rows` heads and `cols` pieces of four values of a unit (all of
-// them where there are many units), and as many of the parts at a time as it has threads for.
+// Joins what the workgroups of a unit left.  A workgroup takes `rows` heads and `cols` pieces of four values of a unit, and as many
+// of the parts at a time as it has threads for.
 template <bool kBf16>
 __global__ __launch_bounds__(kThreads) void join_kernel(const StepArgs a, int rows, int cols, int row_cuts, int col_cuts) {
-  constexpr int kAhead = 4;  // parts whose values are on their way at a time
+  constexpr int kAhead = 2;  // parts whose values are on their way at a time
   struct Share {
     f32x4 o;
     float m, l;
@@ -574,11 +574,11 @@ hipError_t launch(const StepArgs &a, hipStream_t stream) {
   else if (a.d.D <= 128) launch_step<kBf16, 128>(a, stream);
   else launch_step<kBf16, 256>(a, stream);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || !dealt(a.d)) return e;
-  // Few units have many parts each, up to one of every workgroup: a workgroup for 32 values of a head.
+  // Few units have many parts each, up to one of every workgroup: a workgroup for 32 values of a head.  Otherwise one for half the heads.
   const unsigned units = static_cast<unsigned>(a.units) * a.d.B;
   const int tile_rows = a.d.G < kRows ? a.d.G : kRows, all_cols = a.d.D / 4;
   const bool few = units < kFewUnits;
-  const int rows = few ? 1 : tile_rows, cols = few && all_cols > 8 ? 8 : all_cols;
+  const int rows = few ? 1 : (tile_rows + 1) / 2, cols = few && all_cols > 8 ? 8 : all_cols;
   const int row_cuts = (tile_rows + rows - 1) / rows, col_cuts = (all_cols + cols - 1) / cols;
   hipLaunchKernelGGL(join_kernel<kBf16>, dim3(units * row_cuts * col_cuts), dim3(kThreads), 0, stream, a, rows, cols, row_cuts, col_cuts);
   return hipGetLastError();
