@@ -383,12 +383,14 @@ SSD_API ssd_status ssd_norm_residual(int64_t rows, int32_t width, int32_t io_dty
  * values), results are rounded once.
  *
  * What the device arrays hold is not checked on the host, and cannot make a
- * kernel leave its tensors: seq_lens is cut to [0, max_pages * page_size];
- * boundaries to [0, tokens] (a sequence whose end precedes its beginning has no
+ * kernel leave its tensors: a negative seq_lens[b] counts as 0;
+ * boundaries are cut to [0, tokens] (a sequence whose end precedes its beginning has no
  * new tokens); tokens whose page table entry is not in [0, npages) are not
- * appended and not seen.  A new token in front of its sequence's beginning
- * (seq_lens[b] smaller than the number of its new tokens) is not appended and
- * sees nothing.  A token that sees nothing gets y = 0.  What lies in a page
+ * appended and not seen.  A new token that has no place in its sequence's row of
+ * the page table -- in front of its beginning (seq_lens[b] smaller than the number
+ * of its new tokens), or at max_pages * page_size or behind (a sequence that has
+ * outgrown its row) -- is not appended, sees nothing, and is seen by none; the
+ * others keep their places.  A token that sees nothing gets y = 0.  What lies in a page
  * behind a sequence's end is never used, whatever its value, nor are keys that a
  * token does not see.  Values that it does not see are not used by ssd_attn_step;
  * in ssd_attn_prefill, where rows share a tile of tokens, those of its own
@@ -425,8 +427,8 @@ typedef struct {
  *                     that a row of the page table can hold (rope_positions >=
  *                     max_pages * page_size); both NULL if rotary is 0
  *   rotary            even, <= headdim
- * q_out is left untouched for tokens outside every sequence and in front of its
- * beginning.  All tensors are 16-byte aligned, strides a multiple of 16 bytes.
+ * q_out is left untouched for tokens outside every sequence and without a place
+ * in theirs.  All tensors are 16-byte aligned, strides a multiple of 16 bytes.
  * k_cache and v_cache must not overlap anything else.
  * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _HIP.
  */

@@ -36,15 +36,17 @@ def norm_residual(residual, x, weight, scale, eps):
 
 
 def new_tokens(cu, lens, tokens, capacity):
-    """(packed index, sequence, position) of every new token that is in a sequence; position may be negative."""
-    lens = np.clip(_f64(lens), 0, capacity)
+    """(packed index, sequence, position) of every new token that is in a sequence; negative: it has no place in it."""
+    def place(pos):
+        return pos if pos < capacity else -1
+    lens = np.maximum(_f64(lens), 0)
     if cu is None:
-        return [(b, b, int(lens[b]) - 1) for b in range(len(lens))]
+        return [(b, b, place(int(lens[b]) - 1)) for b in range(len(lens))]
     cu = [int(v) for v in _f64(cu)]
     out = []
     for b in range(len(lens)):
         lo, hi = max(cu[b], 0), min(cu[b + 1], tokens)
-        out += [(t, b, int(lens[b]) - (hi - t)) for t in range(lo, hi)]
+        out += [(t, b, place(int(lens[b]) - (hi - t))) for t in range(lo, hi)]
     return out
 
 

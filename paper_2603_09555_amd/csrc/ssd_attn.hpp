@@ -7,11 +7,8 @@
 
 namespace ssd {
 
-// A sequence's length as the kernels use it.
-__device__ __forceinline__ int cut_length(const AttnDims &d, int len) { return min(max(len, 0), d.capacity()); }
-
 struct Token {
-  int seq, pos;  // pos < 0: in no sequence, or in front of its beginning
+  int seq, pos;  // pos < 0: in no sequence, or without a place in it (in front of its beginning, behind its row of the table)
 };
 
 // The sequence and position of a packed new token (cu == nullptr: one for each sequence).
@@ -29,7 +26,8 @@ __device__ __forceinline__ Token find_token(const AttnDims &d, const int32_t *cu
     if (cu[last] > token || token >= end) return t;
     t.seq = last;
   }
-  t.pos = cut_length(d, lens[t.seq]) - (end - token);
+  t.pos = max(lens[t.seq], 0) - (end - token);
+  if (t.pos >= d.capacity()) t.pos = -1;
   return t;
 }
 

@@ -84,14 +84,28 @@ struct Unit {
 template <int kTokens>
 __device__ __forceinline__ void see(const PrefillArgs &a, Unit &r) {
   const int lowest = r.pos0 + quotient(r.first_row, a.d.G, a.inv_group);
-  const int highest = r.pos0 + quotient(r.first_row + r.rows - 1, a.d.G, a.inv_group);
+  const int highest = min(r.pos0 + quotient(r.first_row + r.rows - 1, a.d.G, a.inv_group), a.d.capacity() - 1);
   r.base = (a.d.window > 0 ? max(0, lowest + 1 - a.d.window) : 0) & ~(kTokens - 1);
-  r.tiles = highest < 0 ? 0 : (highest + 1 - r.base + kTokens - 1) / kTokens;
+  r.tiles = highest < max(0, lowest) ? 0 : (highest + 1 - r.base + kTokens - 1) / kTokens;
 }
+// What this lane's row sees, and its wave's 32 rows, whose positions do not decrease.
+struct Seen {
+  int from, to;                  // the row: [from, to]
+  int all_from, all_to, any_to;  // of the wave: every row sees [all_from, all_to], none sees beyond any_to
+  __device__ __forceinline__ Seen(const PrefillArgs &a, int pos) {
+    const int capacity = a.d.capacity(), lowest = __builtin_amdgcn_readfirstlane(pos), highest = __builtin_amdgcn_readlane(pos, 31);
+    // (a token behind the row of the page table has no place, and sees nothing)
+    to = pos < capacity ? pos : -1;
+    from = a.d.window > 0 ? pos - a.d.window + 1 : 0;
+    all_from = __builtin_amdgcn_readlane(from, 31);
+    all_to = highest < capacity ? lowest : -1;
+    any_to = highest < capacity ? highest : lowest < capacity ? capacity - 1 : -1;
+  }
+};
 // A sequence's units.
 struct Line {
   int begin, pos0, all;  // all: rows
-  int units, tiles;      // tiles of the last unit, which has the most
+  int units, tiles;      // tiles of the last unit, which has the most (rows behind the page table's row have none)
   float work;            // tiles of all, about
 };
 template <int kTokens>
@@ -100,7 +114,7 @@ __device__ __forceinline__ Line line_of(const PrefillArgs &a, int b) {
   if (b >= a.d.B) return r;
   r.begin = min(max(a.cu[b], 0), a.d.T);
   const int count = min(max(a.cu[b + 1], 0), a.d.T) - r.begin;
-  r.pos0 = cut_length(a.d, a.lens[b]) - count;
+  r.pos0 = max(a.lens[b], 0) - count;
   if (count <= 0) return r;
   r.all = count * a.d.G;
   r.units = (r.all - 1) / kUnitRows + 1;
@@ -402,7 +416,7 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
   const int local = wave * 32 + n;
   const bool mine = local < unit.rows;
   const int row = unit.first_row + min(local, unit.rows - 1), token = quotient(row, a.d.G, a.inv_group);
-  const int pos = unit.pos0 + token, seen_from = a.d.window > 0 ? pos - a.d.window + 1 : 0;
+  const Seen seen(a, unit.pos0 + token);
   const int64_t out_row = static_cast<int64_t>(unit.begin + token) * a.d.H + hk * a.d.G + (row - token * a.d.G);
   u32x4 query[kPieces];
 #pragma unroll
@@ -411,16 +425,13 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
     query[i] = u32x4{0u, 0u, 0u, 0u};
     if (mine && byte < bytes) query[i] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q) + out_row * bytes + byte);
   }
-  // of the wave: every row sees [all_from, all_to], none sees beyond any_to
-  const int all_to = __builtin_amdgcn_readfirstlane(pos), any_to = __builtin_amdgcn_readlane(pos, 31);
-  const int all_from = __builtin_amdgcn_readlane(seen_from, 31);
   const bool idle = wave * 32 >= unit.rows;
 
   // the split's tiles, of which the group takes every kGroups-th
   const int tile1 = static_cast<int>(static_cast<int64_t>(unit.tiles) * (unit.split + 1) / unit.splits);
   const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * unit.split / unit.splits) + group;
   const int rounds = (tile1 - (tile0 - group) + kGroups - 1) / kGroups;
-  const int end = unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1;  // tokens seen by any row
+  const int end = min(unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1, a.d.capacity());  // tokens seen by any row
 
   // ---- bringing tiles: memory to LDS, a piece a lane; lane t of a wave knows the page of the tile's token t ----
   const int my_row = thread / Geo::kPieces, my_slot = thread % Geo::kPieces;
@@ -549,13 +560,13 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
     where_v = where_k;
     page_v = page_k;
     page_k = page_of(tile + 3 * kGroups);
-    if (!idle && tile < tile1 && first <= any_to) {
+    if (!idle && tile < tile1 && first <= seen.any_to) {
 #pragma unroll
       for (int step = 0; step < kSteps; ++step) {
-        if (first + 32 * step + 31 > all_to || first + 32 * step < all_from || gone[0] != 0) {
+        if (first + 32 * step + 31 > seen.all_to || first + 32 * step < seen.all_from || gone[0] != 0) {
           asm volatile("" ::: "memory");  // (nothing of this is computed where the branch isn't taken)
           const uint32_t out = static_cast<uint32_t>(gone[0] >> (32 * step)) >> (4 * h);
-          const int to = pos - (first + 32 * step + 4 * h), from = seen_from - (first + 32 * step + 4 * h);
+          const int to = seen.to - (first + 32 * step + 4 * h), from = seen.from - (first + 32 * step + 4 * h);
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int t = 8 * (r / 4) + r % 4;
@@ -669,12 +680,8 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
   const int local = wave * kWaveRows + n;
   const bool mine = local < unit.rows;
   const int row = unit.first_row + min(local, unit.rows - 1), token = quotient(row, a.d.G, a.inv_group);
-  const int pos = unit.pos0 + token;
+  const Seen seen(a, unit.pos0 + token);
   const int64_t out_row = static_cast<int64_t>(unit.begin + token) * a.d.H + hk * a.d.G + (row - token * a.d.G);
-  const int seen_from = a.d.window > 0 ? pos - a.d.window + 1 : 0;  // (a position)
-  // of the wave: every row sees [all_from, all_to], none sees beyond any_to
-  const int all_to = __builtin_amdgcn_readfirstlane(pos), any_to = __builtin_amdgcn_readlane(pos, 31);
-  const int all_from = __builtin_amdgcn_readlane(seen_from, 31);
   const bool idle = wave * kWaveRows >= unit.rows;
 
   auto take_apart = [](const u32x4 (&q)[2], Op (&o)[3]) {
@@ -706,7 +713,7 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
   const int tile1 = static_cast<int>(static_cast<int64_t>(unit.tiles) * (unit.split + 1) / unit.splits);
   const int tile0 = static_cast<int>(static_cast<int64_t>(unit.tiles) * unit.split / unit.splits) + group;
   const int rounds = (tile1 - (tile0 - group) + kGroups - 1) / kGroups;
-  const int end = unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1;  // tokens seen by any row
+  const int end = min(unit.pos0 + quotient(unit.first_row + unit.rows - 1, a.d.G, a.inv_group) + 1, a.d.capacity());  // tokens seen by any row
 
   u32x4 fetched[2][kFetch][2];
   uint64_t gone = 0, gone_next = 0;  // tokens of the tile whose page is not in the cache
@@ -759,7 +766,7 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
   for (int round = 0; round < rounds; ++round) {
     const int tile = tile0 + kGroups * round, first = unit.base + tile * kTokens;
     const uint64_t gone_now = gone;
-    const bool busy = !idle && tile < tile1 && first <= any_to;
+    const bool busy = !idle && tile < tile1 && first <= seen.any_to;
     const int page_next = page_of(tile + kGroups);
     if (kEarly && round + 1 < rounds) fetch(tile + kGroups, page_next);
     f32x16 s;
@@ -778,10 +785,10 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
         s = split::mfma6(k[i & 1], query[i], s);
         if (DP > 64) asm volatile("" ::: "memory");  // (no reads further ahead: there are no registers for them)
       }
-      if (first + kTokens - 1 > all_to || first < all_from || gone_now != 0) {
+      if (first + kTokens - 1 > seen.all_to || first < seen.all_from || gone_now != 0) {
         asm volatile("" ::: "memory");  // (nothing of this is computed where the branch isn't taken)
         const uint32_t out = static_cast<uint32_t>(gone_now) >> (4 * h);
-        const int to = pos - (first + 4 * h), from = seen_from - (first + 4 * h);
+        const int to = seen.to - (first + 4 * h), from = seen.from - (first + 4 * h);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int t = 8 * (r / 4) + r % 4;

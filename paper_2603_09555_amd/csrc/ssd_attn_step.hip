@@ -65,7 +65,8 @@ struct Span {
 };
 __device__ __forceinline__ Span span_of(const StepArgs &a, int b) {
   Span s;
-  s.len = cut_length(a.d, a.lens[b]);
+  s.len = max(a.lens[b], 0);
+  if (s.len > a.d.capacity()) s.len = 0;  // (the new token has no place: it sees nothing)
   s.lo = a.d.window > 0 ? max(0, s.len - a.d.window) : 0;
   s.base = s.lo & ~(kTile - 1);
   s.blocks = (s.len - s.base + kBlock - 1) / kBlock;

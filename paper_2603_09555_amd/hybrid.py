@@ -39,9 +39,10 @@ class HybridConfig:
 
 @dataclass
 class HybridCache:
-    """What a batch of sequences leaves between calls.  ``lens`` counts the tokens of each sequence."""
+    """What a batch of sequences leaves between calls.  ``lens`` counts the tokens of each sequence, ``held`` on the host."""
     lens: torch.Tensor                     # (batch) int32
     page_table: torch.Tensor               # (batch, max_pages) int32
+    held: list
     conv: dict = field(default_factory=dict)    # block -> (batch, channels, taps - 1)
     state: dict = field(default_factory=dict)   # block -> (batch, nheads, headdim, dstate) fp32
     keys: dict = field(default_factory=dict)    # block -> (npages, kv_heads, page_size, headdim)
@@ -90,7 +91,7 @@ class HybridStack:
         pages = -(-max_tokens // c.page_size)
         order = torch.randperm(batch * pages, generator=torch.Generator().manual_seed(seed))
         cache = HybridCache(torch.zeros((batch,), dtype=torch.int32, device=self.device),
-                            order.to(torch.int32).view(batch, pages).to(self.device))
+                            order.to(torch.int32).view(batch, pages).to(self.device), [0] * batch)
         for i, b in enumerate(self.blocks):
             if b["kind"] == "M":
                 cache.conv[i] = torch.zeros((batch, sum(self.conv_split), c.conv_taps - 1), dtype=self.dtype, device=self.device)
@@ -105,6 +106,13 @@ class HybridStack:
             angle = torch.arange(capacity, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(half, dtype=torch.float64) / half)
             self.rope = (angle.cos().float().to(self.device), angle.sin().float().to(self.device))
         return cache
+
+    def _grow(self, cache, new):
+        """Sequences get ``new`` tokens each, for which there must be pages."""
+        held = [h + n for h, n in zip(cache.held, new, strict=True)]
+        if max(held) > cache.page_table.shape[1] * self.config.page_size:
+            raise ValueError("a sequence has outgrown its pages")
+        cache.held = held
 
     def _mamba(self, i, b, h, cache, lengths, cu):
         """``lengths``: new tokens of each sequence, or None for one each."""
@@ -161,6 +169,7 @@ class HybridStack:
         """``x (tokens,width)``: ``lengths[b]`` new tokens of every sequence, packed.  Returns the normalised stream of every token."""
         if x.shape[0] != sum(lengths):
             raise ValueError("x must hold the sequences' new tokens")
+        self._grow(cache, lengths)
         new = torch.tensor(lengths, dtype=torch.int32)
         cu = torch.cat((torch.zeros(1, dtype=torch.int32), new.cumsum(0).to(torch.int32))).to(self.device)
         cache.lens += new.to(self.device)
@@ -168,6 +177,7 @@ class HybridStack:
 
     def step(self, x, cache: HybridCache):
         """``x (batch,width)``: one new token of every sequence."""
+        self._grow(cache, [1] * len(cache.held))
         cache.lens += 1
         return self._run(x, cache, None, None)
 
