@@ -394,8 +394,9 @@ SSD_API ssd_status ssd_norm_residual(int64_t rows, int32_t width, int32_t io_dty
  * behind a sequence's end is never used, whatever its value, nor are keys that a
  * token does not see.  Values that it does not see are not used by ssd_attn_step;
  * in ssd_attn_prefill, where rows share a tile of tokens, those of its own
- * sequence are multiplied by a probability of zero if they are less than 64
- * tokens from what it sees, and have to be finite.  With fp32 io, ssd_attn_prefill
+ * sequence are multiplied by a probability of zero if they are less than 96
+ * tokens (fp32: 64) from what it sees, and have to be finite; a token that sees
+ * nothing gets y = 0 whatever they are.  With fp32 io, ssd_attn_prefill
  * takes queries, keys and values apart for its products, which is exact up to
  * 2^127 in magnitude; a larger or infinite one that is seen gives NaN.
  */

@@ -91,13 +91,15 @@ __device__ __forceinline__ void see(const PrefillArgs &a, Unit &r) {
 // What this lane's row sees, and its wave's 32 rows, whose positions do not decrease.
 struct Seen {
   int from, to;                  // the row: [from, to]
-  int all_from, all_to, any_to;  // of the wave: every row sees [all_from, all_to], none sees beyond any_to
+  int all_from, all_to;          // of the wave: every row sees [all_from, all_to],
+  int any_from, any_to;          // none sees what is not in [any_from, any_to]
   __device__ __forceinline__ Seen(const PrefillArgs &a, int pos) {
     const int capacity = a.d.capacity(), lowest = __builtin_amdgcn_readfirstlane(pos), highest = __builtin_amdgcn_readlane(pos, 31);
     // (a token behind the row of the page table has no place, and sees nothing)
     to = pos < capacity ? pos : -1;
     from = a.d.window > 0 ? pos - a.d.window + 1 : 0;
     all_from = __builtin_amdgcn_readlane(from, 31);
+    any_from = __builtin_amdgcn_readfirstlane(from);
     all_to = highest < capacity ? lowest : -1;
     any_to = highest < capacity ? highest : lowest < capacity ? capacity - 1 : -1;
   }
@@ -374,6 +376,16 @@ __device__ __forceinline__ float add_both(uint32_t two, float c) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3f803f80u), c, false);
 }
 
+// Rows that see nothing of a part keep no product with what others see.
+template <int kColTiles>
+__device__ __forceinline__ void clear_unseen(f32x16 (&o)[kColTiles], float l) {
+  if (!__any(l == 0.f)) return;
+#pragma unroll
+  for (int c = 0; c < kColTiles; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[c][r] = l == 0.f ? 0.f : o[c][r];
+}
+
 // The larger of the two values that lanes l and l + 32 hold, in both.
 __device__ __forceinline__ float both_halves_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -541,17 +553,11 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
     bring(lds_k[1], kh, where_v, tile0 + kGroups, p1, true);
   }
   arrived(lds_v[0], gone[0]);
-  if (kEarly) read_keys(lds_k[0], 0);
-  f32x16 s = scores(lds_k[0], 0);
-  if (kEarly) read_keys(lds_k[0], 1);
-  __syncthreads();
-  int at_k = 0;
+  int at_k = 0, round = 0;
   const auto wrap = [](int i) { return i >= kKeyTiles ? i - kKeyTiles : i; };
-  for (int round = 0; round < rounds; ++round) {
+  // the next tile's values and the keys of the one behind it
+  const auto bring_next = [&](char *kt2, char *vt1) {
     const int tile = tile0 + kGroups * round;
-    const int first = unit.base + tile * kTokens, odd = round & 1;
-    char *const kt = lds_k[at_k], *const kt1 = lds_k[wrap(at_k + 1)], *const kt2 = lds_k[wrap(at_k + 2)];
-    char *const vt = lds_v[odd], *const vt1 = lds_v[odd ^ 1];
     // (tiles behind the last one repeat its last token: they are brought and not used)
     const Where where_k = where_of(tile + 2 * kGroups, page_k);
     bring(vt1, vh, where_v, tile + kGroups, page_v, false);
@@ -560,6 +566,38 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
     where_v = where_k;
     page_v = page_k;
     page_k = page_of(tile + 3 * kGroups);
+  };
+  const auto next_round = [&](char *vt1) {
+    gone[0] = gone[1];
+    gone[1] = gone[2];
+    at_k = wrap(at_k + 1);
+    arrived(vt1, gone[0]);
+  };
+  f32x16 s;
+  const auto begin = [&](const char *tile) {
+    if (kEarly) read_keys(tile, 0);
+    s = scores(tile, 0);
+    if (kEarly) read_keys(tile, 1);
+  };
+  // Tiles in front of all that the wave's rows see are brought for the other waves, and left out here: their values may be
+  // anything, infinities included.  (32 tokens at a time, behind the rows too, by a branch in the loop: 4 % more time.)
+  const int skipped = min(max(0, (seen.any_from - unit.base) / kTokens - tile0 + kGroups - 1) / kGroups, rounds);
+  if (kEarly && skipped == 0) begin(lds_k[0]);
+  __syncthreads();
+#pragma unroll 1
+  for (; round < skipped; ++round) {
+    char *const vt1 = lds_v[(round & 1) ^ 1];
+    bring_next(lds_k[wrap(at_k + 2)], vt1);
+    if (kEarly && round + 1 == skipped) begin(lds_k[wrap(at_k + 1)]);
+    next_round(vt1);
+  }
+  if (!kEarly) begin(lds_k[at_k]);
+  for (; round < rounds; ++round) {
+    const int tile = tile0 + kGroups * round;
+    const int first = unit.base + tile * kTokens;
+    char *const kt = lds_k[at_k], *const kt1 = lds_k[wrap(at_k + 1)], *const kt2 = lds_k[wrap(at_k + 2)];
+    char *const vt = lds_v[round & 1], *const vt1 = lds_v[(round & 1) ^ 1];
+    bring_next(kt2, vt1);
     if (!idle && tile < tile1 && first <= seen.any_to) {
 #pragma unroll
       for (int step = 0; step < kSteps; ++step) {
@@ -627,12 +665,10 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
         s = next;
       }
     }
-    gone[0] = gone[1];
-    gone[1] = gone[2];
-    at_k = wrap(at_k + 1);
-    arrived(vt1, gone[0]);
+    next_round(vt1);
   }
   l += __shfl_xor(l, 32);
+  clear_unseen(o, l);
   if (kGroups == 2 && !join_groups<DP>(*reinterpret_cast<Part<DP> *>(lds), group, wave, o, m, l)) return;
   finish<true, DP>(a, unit.splits == 1, blockIdx.x, mine, wave, out_row, o, m, l);
 }
@@ -766,7 +802,7 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
   for (int round = 0; round < rounds; ++round) {
     const int tile = tile0 + kGroups * round, first = unit.base + tile * kTokens;
     const uint64_t gone_now = gone;
-    const bool busy = !idle && tile < tile1 && first <= seen.any_to;
+    const bool busy = !idle && tile < tile1 && first <= seen.any_to && first + kTokens > seen.any_from;
     const int page_next = page_of(tile + kGroups);
     if (kEarly && round + 1 < rounds) fetch(tile + kGroups, page_next);
     f32x16 s;
@@ -856,6 +892,7 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
   }
 
   l += __shfl_xor(l, 32);
+  clear_unseen(o, l);
   if (kGroups == 2 && !join_groups<DP>(*reinterpret_cast<Part<DP> *>(all_lds), group, wave, o, m, l)) return;
   finish<false, DP>(a, unit.splits == 1, blockIdx.x, mine, wave, out_row, o, m, l);
 }
