@@ -98,7 +98,7 @@ __device__ __forceinline__ float silu(float v) {
 struct AttnDims {
   int B, T, H, Hk, D, G;   // sequences, new tokens, heads, key heads, headdim, H / Hk
   int npages, lg_page, max_pages;
-  int window;              // 0 = no limit
+  int window;              // 0 = no limit, otherwise smaller than capacity()
   bool bf16;
   __host__ __device__ int capacity() const { return max_pages << lg_page; }  // tokens of a sequence, at most 2^30
 };

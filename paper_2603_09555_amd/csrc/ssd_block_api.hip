@@ -39,10 +39,11 @@ ssd_status make_dims(const ssd_attn_shape *s, bool packed, AttnDims *out) {
   d.npages = s->npages;
   while ((1 << d.lg_page) < s->page_size) ++d.lg_page;
   d.max_pages = s->max_pages;
-  d.window = s->window;
   d.bf16 = s->io_dtype == SSD_BF16;
   // positions fit 30 bits; tensors are addressable with head-room
   if (static_cast<long double>(d.max_pages) * s->page_size > 1073741824.0L) return SSD_ERR_SHAPE;
+  // a window as wide as a row of the page table is no limit, and positions minus smaller ones fit 32 bits
+  d.window = s->window < d.capacity() ? s->window : 0;
   if (static_cast<long double>(d.npages) * d.Hk * s->page_size * d.D > 1.0e15L || d.T > (1 << 30) || d.B > (1 << 30) ||
       static_cast<long double>(d.T) * d.H > 2147483647.0L || static_cast<long double>(d.B) * d.H > 2147483647.0L)
     return SSD_ERR_SHAPE;

@@ -537,6 +537,7 @@ def ssd_norm_residual(residual, x, weight, scale=1.0, eps=1e-5, out=None, residu
 def make_attn_shape(batch, tokens, nheads, k_cache, page_table, window=0) -> ssd_attn_shape:
     """The ``ssd_attn_shape`` of a call on ``k_cache (npages,nkvheads,page_size,headdim)`` and ``page_table (batch,max_pages)``."""
     npages, nkv, page, headdim = k_cache.shape
+    window = max(-1, min(window, 2 ** 31 - 1))     # (anything that large is no limit, anything below zero refused)
     return ssd_attn_shape(batch, tokens, nheads, nkv, headdim, npages, page, page_table.shape[1], window, _IO_DTYPES.get(k_cache.dtype, -1))
 
 
