@@ -14,7 +14,7 @@ bool is_dtype(int32_t t) { return t == SSD_F32 || t == SSD_BF16; }
 ssd_status norm_shape(int64_t rows, int32_t width, int32_t groups, int32_t io_dtype, float eps) {
   if (!is_dtype(io_dtype)) return SSD_ERR_DTYPE;
   if (rows < 1 || width < 1 || groups < 1 || width % groups != 0 || !(eps >= 0.f)) return SSD_ERR_SHAPE;
-  if (static_cast<long double>(rows) * groups > 2147483647.0L || width > (1 << 30)) return SSD_ERR_SHAPE;  // one grid axis
+  if (static_cast<long double>(rows) * groups > 2147483647.0L || width > (1 << 30)) return SSD_ERR_SHAPE;
   if (static_cast<long double>(rows) * width > 1.0e15L) return SSD_ERR_SHAPE;
   return SSD_OK;
 }

@@ -8,6 +8,8 @@
 // once.  A thread owns pieces of 8 neighbouring values (bf16: 16 bytes; fp32: 32).  Both are streams; with few rows they are a
 // chain of two memory latencies and a reduction, and the unit is spread over as many threads as it has pieces for.
 // 16384 rows of 5120, gated, bf16: 100 us, 5.0 TB/s (a copy: 4.9); 16383 of 768, residual, fp32: 40 us, 5.0 TB/s; one row: 3.1 us, a launch.
+#include <algorithm>
+
 #include "ssd_block.hpp"
 
 namespace ssd {
@@ -17,6 +19,7 @@ using namespace block;
 
 constexpr int kPiece = 8;
 constexpr int kFewUnits = 512;
+constexpr int64_t kMostThreads = int64_t{1} << 31;  // of a launch, which takes less than 2^32
 
 enum Mode { kGateFirst = 0, kNormFirst = 1, kResidual = 2 };
 
@@ -26,7 +29,7 @@ struct NormArgs {
   const float *weight;
   void *out;
   void *side_out;        // residual_out
-  int64_t units;
+  int64_t units, first;  // units; the first one of this launch
   int64_t side_stride;   // of z, in elements
   int width, n;          // values in a row, and in a unit
   int groups;
@@ -53,7 +56,7 @@ template <typename Io, typename Side, int kMode, int kThreads, int kHold>
 __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(const NormArgs a) {
   constexpr int kBlock = kThreads < 256 ? 256 : kThreads, kUnits = kBlock / kThreads, kWaves = kThreads < 64 ? 1 : kThreads / 64;
   const int t = threadIdx.x % kThreads;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kUnits + threadIdx.x / kThreads;
+  const int64_t unit = a.first + static_cast<int64_t>(blockIdx.x) * kUnits + threadIdx.x / kThreads;
   if (unit >= a.units) return;  // (all threads of a unit; workgroups of several waves a unit have one unit)
   int64_t row = unit;
   int first = 0;
@@ -141,11 +144,17 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(c
 }
 
 template <typename Io, typename Side, int kMode, int kThreads, int kHold>
-hipError_t launch_shape(const NormArgs &a, hipStream_t stream) {
+hipError_t launch_shape(NormArgs a, hipStream_t stream) {
   constexpr int kBlock = kThreads < 256 ? 256 : kThreads, kUnits = kBlock / kThreads;
-  hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, kThreads, kHold>), dim3(static_cast<unsigned>((a.units + kUnits - 1) / kUnits)), dim3(kBlock), 0,
-                     stream, a);
-  return hipGetLastError();
+  constexpr int64_t kMost = kMostThreads / kBlock * kUnits;
+  hipError_t e = hipSuccess;
+  for (; a.first < a.units && e == hipSuccess; a.first += kMost) {
+    const int64_t units = std::min(a.units - a.first, kMost);
+    hipLaunchKernelGGL((norm_kernel<Io, Side, kMode, kThreads, kHold>), dim3(static_cast<unsigned>((units + kUnits - 1) / kUnits)), dim3(kBlock), 0,
+                       stream, a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 // Threads and pieces a thread by the unit's width: no more registers than the pieces need, which leave room for other units'
