@@ -376,7 +376,9 @@ SSD_API ssd_status ssd_norm_residual(int64_t rows, int32_t width, int32_t io_dty
  *                       of its seq_lens[b]
  * all of them device arrays, 4-byte aligned.  Query head h reads key head h / (nheads / nkvheads).
  * headdim is a multiple of 8 up to 256, page_size a power of two up to 65536; a
- * page (all its key heads) is smaller than 2 GiB.
+ * page (all its key heads) is smaller than 2 GiB.  A call whose launches would have
+ * 2^32 threads or more is refused with SSD_ERR_SHAPE; that is not so below 2^22
+ * sequences times heads, 2^24 tokens and 2^30 tokens times heads.
  * A token sees the tokens of its sequence up to itself; with window > 0 only the
  * last `window` of them.  io dtype is fp32 or bf16; scores, softmax and sums are
  * fp32 (bf16 io: the probabilities are rounded to bf16 for their product with the

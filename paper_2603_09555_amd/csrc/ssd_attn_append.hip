@@ -172,6 +172,21 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
 
 }  // namespace
 
+namespace {
+
+int row_pieces(const AttnDims &d, bool queries) { return ((queries ? d.H : 0) + 2 * d.Hk) * (d.D / (d.bf16 ? 8 : 4)); }
+int parts_of(int pieces) { return (pieces + 255) / 256; }
+int run_of(const AttnDims &d, int parts) {
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMostTokens, static_cast<int64_t>(d.T) * parts / kFewWorkgroups)));
+}
+
+}  // namespace
+
+bool attn_append_fits(const AttnDims &d, bool queries) {
+  const int run = run_of(d, parts_of(row_pieces(d, queries)));
+  return (static_cast<int64_t>(d.T) + run - 1) / run <= kMostWorkgroups256;
+}
+
 hipError_t launch_attn_append(const AttnDims &d, const Rope &rope, const int32_t *cu, const int32_t *lens, const int32_t *table,
                               const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                               void *q_out, void *k_cache, void *v_cache, hipStream_t stream) {
@@ -193,9 +208,9 @@ hipError_t launch_attn_append(const AttnDims &d, const Rope &rope, const int32_t
   a.q_heads = q != nullptr ? d.H : 0;
   a.head_pieces = d.D / (d.bf16 ? 8 : 4);
   a.inv_head_pieces = inverse_of(a.head_pieces);
-  a.row_pieces = (a.q_heads + 2 * d.Hk) * a.head_pieces;
-  const int parts = (a.row_pieces + 255) / 256;
-  a.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMostTokens, static_cast<int64_t>(d.T) * parts / kFewWorkgroups)));
+  a.row_pieces = row_pieces(d, q != nullptr);
+  const int parts = parts_of(a.row_pieces);
+  a.run = run_of(d, parts);
   const dim3 grid((d.T + a.run - 1) / a.run, parts);
   const int width = rope.interleaved ? 2 * rope.half : rope.half;
   const bool whole = width % (d.bf16 ? 8 : 4) == 0;

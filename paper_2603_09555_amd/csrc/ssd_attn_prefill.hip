@@ -1024,6 +1024,8 @@ size_t part_bytes(const AttnDims &d) { return d.D <= 64 ? sizeof(Part<64>) : d.D
 
 }  // namespace
 
+bool attn_prefill_fits(const AttnDims &d) { return static_cast<int64_t>(plan_of(d).units) * d.Hk <= kMostWorkgroups256; }
+
 size_t attn_prefill_workspace_bytes(const AttnDims &d) {
   const Plan p = plan_of(d);
   if (!p.shared) return 256;

@@ -569,25 +569,43 @@ void launch_step(const StepArgs &a, hipStream_t stream) {
   else launch_step<kBf16, DP, false>(a, stream);
 }
 
+// The joining launch.  Few units have many parts each, up to one of every workgroup: a workgroup for 32 values of a head.  Otherwise one
+// for half the heads.
+struct Join {
+  int rows, cols, row_cuts, col_cuts;
+  int64_t workgroups;
+};
+Join join_of(const AttnDims &d) {
+  const int64_t units = static_cast<int64_t>(units_of(d)) * d.B;
+  const int tile_rows = d.G < kRows ? d.G : kRows, all_cols = d.D / 4;
+  const bool few = units < kFewUnits;
+  Join j;
+  j.rows = few ? 1 : (tile_rows + 1) / 2;
+  j.cols = few && all_cols > 8 ? 8 : all_cols;
+  j.row_cuts = (tile_rows + j.rows - 1) / j.rows;
+  j.col_cuts = (all_cols + j.cols - 1) / j.cols;
+  j.workgroups = units * j.row_cuts * j.col_cuts;
+  return j;
+}
+
 template <bool kBf16>
 hipError_t launch(const StepArgs &a, hipStream_t stream) {
   if (a.d.D <= 64) launch_step<kBf16, 64>(a, stream);
   else if (a.d.D <= 128) launch_step<kBf16, 128>(a, stream);
   else launch_step<kBf16, 256>(a, stream);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || !dealt(a.d)) return e;
-  // Few units have many parts each, up to one of every workgroup: a workgroup for 32 values of a head.  Otherwise one for half the heads.
-  const unsigned units = static_cast<unsigned>(a.units) * a.d.B;
-  const int tile_rows = a.d.G < kRows ? a.d.G : kRows, all_cols = a.d.D / 4;
-  const bool few = units < kFewUnits;
-  const int rows = few ? 1 : (tile_rows + 1) / 2, cols = few && all_cols > 8 ? 8 : all_cols;
-  const int row_cuts = (tile_rows + rows - 1) / rows, col_cuts = (all_cols + cols - 1) / cols;
-  hipLaunchKernelGGL(join_kernel<kBf16>, dim3(units * row_cuts * col_cuts), dim3(kThreads), 0, stream, a, rows, cols, row_cuts, col_cuts);
+  const Join j = join_of(a.d);
+  hipLaunchKernelGGL(join_kernel<kBf16>, dim3(static_cast<unsigned>(j.workgroups)), dim3(kThreads), 0, stream, a, j.rows, j.cols, j.row_cuts, j.col_cuts);
   return hipGetLastError();
 }
 
 size_t part_bytes(const AttnDims &d) { return (static_cast<size_t>(2 * kMostWorkgroups * kRows) * (d.D + 4) * 4 + 255) / 256 * 256; }
 
 }  // namespace
+
+bool attn_step_fits(const AttnDims &d) {
+  return dealt(d) ? join_of(d).workgroups <= kMostWorkgroups256 : static_cast<int64_t>(units_of(d)) * d.B <= kMostWorkgroups256;
+}
 
 size_t attn_step_workspace_bytes(const AttnDims &d) {
   if (!dealt(d)) return 256;

@@ -113,6 +113,11 @@ hipError_t launch_norm_gated(int64_t rows, int width, int groups, bool bf16, con
                              const float *weight, float eps, bool norm_first, void *out, hipStream_t stream);
 hipError_t launch_norm_residual(int64_t rows, int width, bool bf16, bool stream_bf16, const void *x, const void *residual,
                                 float scale, const float *weight, float eps, void *out, void *residual_out, hipStream_t stream);
+// Whether the launches of an attention call of this shape have less than 2^32 threads each, which is what a launch takes.
+constexpr int64_t kMostWorkgroups256 = (int64_t{1} << 24) - 1;  // of 256 threads
+bool attn_append_fits(const AttnDims &d, bool queries);
+bool attn_step_fits(const AttnDims &d);
+bool attn_prefill_fits(const AttnDims &d);
 hipError_t launch_attn_append(const AttnDims &d, const Rope &rope, const int32_t *cu, const int32_t *lens, const int32_t *table,
                               const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                               void *q_out, void *k_cache, void *v_cache, hipStream_t stream);

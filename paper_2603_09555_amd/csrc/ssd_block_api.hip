@@ -53,6 +53,15 @@ ssd_status make_dims(const ssd_attn_shape *s, bool packed, AttnDims *out) {
   return SSD_OK;
 }
 
+ssd_status step_dims(const ssd_attn_shape *s, AttnDims *d) {
+  const ssd_status st = make_dims(s, false, d);
+  return st == SSD_OK && !ssd::attn_step_fits(*d) ? SSD_ERR_SHAPE : st;
+}
+ssd_status prefill_dims(const ssd_attn_shape *s, AttnDims *d) {
+  const ssd_status st = make_dims(s, true, d);
+  return st == SSD_OK && !ssd::attn_prefill_fits(*d) ? SSD_ERR_SHAPE : st;
+}
+
 // The device arrays and the caches, of either attention call.
 ssd_status attn_pointers(const int32_t *seq_lens, const int32_t *page_table, const void *q, const void *k_cache,
                          const void *v_cache, const void *y) {
@@ -105,6 +114,7 @@ ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *rope, co
                            const void *v, int64_t v_stride, void *q_out, void *k_cache, void *v_cache, void *hip_stream) {
   AttnDims d;
   if (const ssd_status st = make_dims(shape, cu_seqlens != nullptr, &d); st != SSD_OK) return st;
+  if (!ssd::attn_append_fits(d, q != nullptr)) return SSD_ERR_SHAPE;
   if (!rope || !seq_lens || !page_table || !k || !v || !k_cache || !v_cache || (q == nullptr) != (q_out == nullptr))
     return SSD_ERR_NULL;
   if (rope->rotary < 0 || rope->rotary % 2 != 0 || rope->rotary > d.D || (rope->interleaved != 0 && rope->interleaved != 1))
@@ -131,14 +141,14 @@ ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *rope, co
 
 size_t ssd_attn_step_workspace_bytes(const ssd_attn_shape *shape) {
   AttnDims d;
-  return make_dims(shape, false, &d) == SSD_OK ? ssd::attn_step_workspace_bytes(d) : 0;
+  return step_dims(shape, &d) == SSD_OK ? ssd::attn_step_workspace_bytes(d) : 0;
 }
 
 ssd_status ssd_attn_step(const ssd_attn_shape *shape, const int32_t *seq_lens, const int32_t *page_table, const void *q,
                          const void *k_cache, const void *v_cache, float scale, void *y, void *workspace, size_t workspace_bytes,
                          void *hip_stream) {
   AttnDims d;
-  if (const ssd_status st = make_dims(shape, false, &d); st != SSD_OK) return st;
+  if (const ssd_status st = step_dims(shape, &d); st != SSD_OK) return st;
   if (!scale_ok(scale)) return SSD_ERR_SHAPE;
   if (const ssd_status st = attn_pointers(seq_lens, page_table, q, k_cache, v_cache, y); st != SSD_OK) return st;
   if (!workspace_ok(workspace, workspace_bytes, ssd::attn_step_workspace_bytes(d))) return SSD_ERR_WORKSPACE;
@@ -148,14 +158,14 @@ ssd_status ssd_attn_step(const ssd_attn_shape *shape, const int32_t *seq_lens, c
 
 size_t ssd_attn_prefill_workspace_bytes(const ssd_attn_shape *shape) {
   AttnDims d;
-  return make_dims(shape, true, &d) == SSD_OK ? ssd::attn_prefill_workspace_bytes(d) : 0;
+  return prefill_dims(shape, &d) == SSD_OK ? ssd::attn_prefill_workspace_bytes(d) : 0;
 }
 
 ssd_status ssd_attn_prefill(const ssd_attn_shape *shape, const int32_t *cu_seqlens, const int32_t *seq_lens,
                             const int32_t *page_table, const void *q, const void *k_cache, const void *v_cache, float scale,
                             void *y, void *workspace, size_t workspace_bytes, void *hip_stream) {
   AttnDims d;
-  if (const ssd_status st = make_dims(shape, true, &d); st != SSD_OK) return st;
+  if (const ssd_status st = prefill_dims(shape, &d); st != SSD_OK) return st;
   if (!scale_ok(scale)) return SSD_ERR_SHAPE;
   if (!cu_seqlens) return SSD_ERR_NULL;
   if (const ssd_status st = attn_pointers(seq_lens, page_table, q, k_cache, v_cache, y); st != SSD_OK) return st;
