@@ -426,6 +426,7 @@ typedef struct {
  *                     k, v (tokens, nkvheads, headdim) likewise: slices of one
  *                     projection's output.  q (with q_out) may be NULL
  *   q_out             (tokens, nheads, headdim) dense, rotated; must not overlap q, k, v
+ *                     (SSD_ERR_UNSUPPORTED)
  *   rope_cos, rope_sin  (rope_positions, rotary / 2) fp32, for every position
  *                     that a row of the page table can hold (rope_positions >=
  *                     max_pages * page_size); both NULL if rotary is 0
@@ -433,7 +434,7 @@ typedef struct {
  * q_out is left untouched for tokens outside every sequence and without a place
  * in theirs.  All tensors are 16-byte aligned, strides a multiple of 16 bytes.
  * k_cache and v_cache must not overlap anything else.
- * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _HIP.
+ * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _UNSUPPORTED, _ALIGN, _HIP.
  */
 typedef struct {
   const float *cos, *sin;
@@ -458,7 +459,7 @@ SSD_API ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *
  * captured call follows seq_lens as they grow.  A call repeats bit for bit; where
  * a sequence's sum is divided, and with it the last bits of its result, depends
  * on the lengths of the whole batch.
- * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _WORKSPACE, _HIP.
+ * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _UNSUPPORTED, _ALIGN, _WORKSPACE, _HIP.
  */
 SSD_API size_t ssd_attn_step_workspace_bytes(const ssd_attn_shape *shape);
 SSD_API ssd_status ssd_attn_step(const ssd_attn_shape *shape, const int32_t *seq_lens, const int32_t *page_table,
@@ -473,7 +474,7 @@ SSD_API ssd_status ssd_attn_step(const ssd_attn_shape *shape, const int32_t *seq
  *                     tokens outside every sequence is left untouched
  *   scale             positive and finite
  *   workspace         at least ssd_attn_prefill_workspace_bytes() bytes, 256-byte aligned
- * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _WORKSPACE, _HIP.
+ * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _UNSUPPORTED, _ALIGN, _WORKSPACE, _HIP.
  */
 SSD_API size_t ssd_attn_prefill_workspace_bytes(const ssd_attn_shape *shape);
 SSD_API ssd_status ssd_attn_prefill(const ssd_attn_shape *shape, const int32_t *cu_seqlens,

@@ -75,6 +75,15 @@ ssd_status attn_pointers(const int32_t *seq_lens, const int32_t *page_table, con
 // A scale of the logits: positive and finite.
 bool scale_ok(float scale) { return scale > 0.f && scale <= 1.0e30f; }
 
+// Whether `bytes` at `out` reach into one of `count` rows of `row` bytes, `stride` apart.
+bool reaches(const void *out, int64_t bytes, const void *rows, int64_t stride, int64_t row, int64_t count) {
+  const uintptr_t o = reinterpret_cast<uintptr_t>(out), first = reinterpret_cast<uintptr_t>(rows);
+  if (o + bytes <= first || o >= first + (count - 1) * stride + row) return false;
+  if (o < first) return true;
+  const int64_t at = static_cast<int64_t>((o - first) % static_cast<uintptr_t>(stride));  // (behind the row, up to the next one: a gap)
+  return at < row || at + bytes > stride;
+}
+
 bool workspace_ok(const void *workspace, size_t given, size_t need) {
   return workspace && given >= need && (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0;
 }
@@ -134,6 +143,12 @@ ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *rope, co
   if (!aligned4(seq_lens) || !aligned4(page_table) || !aligned4(cu_seqlens) ||
       !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_cache) || !aligned16(v_cache))
     return SSD_ERR_ALIGN;
+  if (q) {  // a thread that rotates reads what its neighbour writes
+    const int64_t size = d.bf16 ? 2 : 4, head = d.D * size, out = static_cast<int64_t>(d.T) * d.H * head;
+    const void *const from[3] = {q, k, v};
+    for (int i = 0; i < 3; ++i)
+      if (reaches(q_out, out, from[i], strides[i] * size, (i == 0 ? d.H : d.Hk) * head, d.T)) return SSD_ERR_UNSUPPORTED;
+  }
   const ssd::Rope r = {rope->cos, rope->sin, rope->rotary / 2, rope->interleaved};
   return status_of(ssd::launch_attn_append(d, r, cu_seqlens, seq_lens, page_table, q, strides[0], k, k_stride, v, v_stride, q_out,
                                            k_cache, v_cache, static_cast<hipStream_t>(hip_stream)));
