@@ -347,9 +347,10 @@ SSD_API ssd_status ssd_conv1d_step(int32_t batch, int32_t ksize, int32_t io_dtyp
  *                     block's input);  residual_out may be residual
  *   residual_dtype    SSD_F32, or io_dtype.  The norm takes r before it is
  *                     rounded to residual_dtype.
- * Arithmetic and sums are fp32, one rounding (RNE) per output.  Any width, and
- * any number of rows up to 2^31 - 1 rows * groups; y, x, out, residual* and weight are 16-byte aligned, z is
- * aligned to its elements.
+ * Arithmetic and sums are fp32, one rounding (RNE) per output; a row's bits do not
+ * depend on the other rows, nor on how many there are.  Any width, and any number
+ * of rows up to 2^31 - 1 rows * groups; y, x, out, residual* and weight are
+ * 16-byte aligned, z is aligned to its elements.
  * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _HIP.
  */
 SSD_API ssd_status ssd_norm_gated(int64_t rows, int32_t width, int32_t groups, int32_t io_dtype,

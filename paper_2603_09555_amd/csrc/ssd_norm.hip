@@ -52,6 +52,8 @@ __device__ __forceinline__ void combine(float v[kPiece], float s[kPiece], float 
 
 // kThreads threads a unit, kHold pieces a thread in registers (0: units too wide for that are read a second time, from the
 // caches).  Units of a wave or less share a workgroup of four waves.
+// The sum is that of runs of 64 pieces, added up in their order, whatever the number of threads: it does not depend on how many
+// units there are, by which that number is chosen.
 template <typename Io, typename Side, int kMode, int kThreads, int kHold>
 __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(const NormArgs a) {
   constexpr int kBlock = kThreads < 256 ? 256 : kThreads, kUnits = kBlock / kThreads, kWaves = kThreads < 64 ? 1 : kThreads / 64;
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(c
   const int pieces = (a.n + kPiece - 1) / kPiece;
   constexpr int kKeep = kHold > 0 ? kHold : 1;
   float v[kKeep][kPiece], g[kMode == kNormFirst ? kKeep : 1][kPiece];
-  float sum = 0.f;
+  float sums[kKeep] = {};
   auto fetch = [&](int p, float x[kPiece], float s[kPiece]) {
     const int at = p * kPiece, left = a.n - at;
     Io::load(in + at, left, x);
@@ -95,7 +97,7 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(c
         combine<kMode>(v[k], s[k], a.scale);
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) {
-          sum = fmaf(v[k][i], v[k][i], sum);
+          sums[k] = fmaf(v[k][i], v[k][i], sums[k]);
           if (kMode == kNormFirst) g[k][i] = s[k][i];
         }
       }
@@ -105,18 +107,23 @@ __global__ __launch_bounds__(kThreads < 256 ? 256 : kThreads) void norm_kernel(c
       fetch(p, v[0], s);
       combine<kMode>(v[0], s, a.scale);
 #pragma unroll
-      for (int i = 0; i < kPiece; ++i) sum = fmaf(v[0][i], v[0][i], sum);
+      for (int i = 0; i < kPiece; ++i) sums[0] = fmaf(v[0][i], v[0][i], sums[0]);
     }
   }
 #pragma unroll
-  for (int d = (kThreads < 64 ? kThreads : 64) / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  for (int k = 0; k < kKeep; ++k)
+#pragma unroll
+    for (int d = (kThreads < 64 ? kThreads : 64) / 2; d > 0; d >>= 1) sums[k] += __shfl_xor(sums[k], d);
+  float sum = sums[0];
   if (kWaves > 1) {
-    __shared__ float part[kWaves];
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = sum;
+    __shared__ float part[kKeep * kWaves];
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < kKeep; ++k) part[k * kWaves + threadIdx.x / 64] = sums[k];
     __syncthreads();
     sum = part[0];
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) sum += part[i];
+    for (int i = 1; i < kKeep * kWaves; ++i) sum += part[i];
   }
   const float r = 1.f / sqrtf(fmaf(sum, a.inv_n, a.eps));
   auto finish = [&](int p, const float x[kPiece], const float *gate) {
