@@ -455,7 +455,8 @@ SSD_API ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *
  *   q, y              (batch, nheads, headdim) dense; y must not be q
  *   scale             positive and finite
  *   workspace         at least ssd_attn_step_workspace_bytes() bytes, 256-byte
- *                     aligned; its size depends on the shape alone
+ *                     aligned; its size depends on the shape alone, and serves
+ *                     shapes of fewer sequences, otherwise the same, too
  * Work is dealt to the workgroups by the lengths as the device holds them, so a
  * captured call follows seq_lens as they grow.  A call repeats bit for bit; where
  * a sequence's sum is divided, and with it the last bits of its result, depends
@@ -474,7 +475,9 @@ SSD_API ssd_status ssd_attn_step(const ssd_attn_shape *shape, const int32_t *seq
  *   q, y              (tokens, nheads, headdim) dense; y must not be q; y of
  *                     tokens outside every sequence is left untouched
  *   scale             positive and finite
- *   workspace         at least ssd_attn_prefill_workspace_bytes() bytes, 256-byte aligned
+ *   workspace         at least ssd_attn_prefill_workspace_bytes() bytes, 256-byte
+ *                     aligned; serves shapes of fewer sequences and tokens,
+ *                     otherwise the same, too
  * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _UNSUPPORTED, _ALIGN, _WORKSPACE, _HIP.
  */
 SSD_API size_t ssd_attn_prefill_workspace_bytes(const ssd_attn_shape *shape);

@@ -955,6 +955,7 @@ __global__ __launch_bounds__(kThreads) void prefill_join_kernel(const PrefillArg
 
 struct Plan {
   int units, groups;
+  int64_t tiles;  // at most, of a unit
   bool shared;
 };
 // bf16: two groups of waves share a unit where that leaves every CU a workgroup or few more: 2048 tokens, 32 heads over 8 of 128, 520
@@ -971,7 +972,7 @@ Plan plan_of(const AttnDims &d) {
   p.units = static_cast<int>(rows / kUnitRows + d.B);
   const int64_t all = static_cast<int64_t>(p.units) * d.Hk;
   const int64_t most_seen = d.window > 0 ? std::min<int64_t>(d.capacity(), static_cast<int64_t>(d.window) + kUnitRows / d.G) : d.capacity();
-  const int64_t tiles = (most_seen + tokens_of_tile(d.bf16) - 1) / tokens_of_tile(d.bf16);
+  const int64_t tiles = p.tiles = (most_seen + tokens_of_tile(d.bf16) - 1) / tokens_of_tile(d.bf16);
   p.groups = d.bf16 && d.D <= 128 && all < kManyUnits && tiles >= (all <= kWorkgroups ? kFewTiles : kManyTiles) ? 2 : 1;
   p.shared = false;
   if (all >= kManyUnits) return p;
@@ -1026,10 +1027,22 @@ size_t part_bytes(const AttnDims &d) { return d.D <= 64 ? sizeof(Part<64>) : d.D
 
 bool attn_prefill_fits(const AttnDims &d) { return static_cast<int64_t>(plan_of(d).units) * d.Hk <= kMostWorkgroups256; }
 
+namespace {
+
+size_t bytes_of(const AttnDims &d, int64_t units) {
+  return (static_cast<size_t>(units + kMostParts) * (part_bytes(d) + sizeof(Record)) + 255) / 256 * 256;
+}
+
+}  // namespace
+
+size_t attn_prefill_used_bytes(const AttnDims &d) {
+  const Plan p = plan_of(d);
+  return p.shared ? bytes_of(d, static_cast<int64_t>(p.units) * d.Hk) : 256;
+}
 size_t attn_prefill_workspace_bytes(const AttnDims &d) {
   const Plan p = plan_of(d);
-  if (!p.shared) return 256;
-  return (static_cast<size_t>(p.units) * d.Hk + kMostParts) * (part_bytes(d) + sizeof(Record));
+  if (p.tiles <= least_tiles(d)) return 256;  // (no unit has two splits' tiles)
+  return bytes_of(d, std::min<int64_t>(static_cast<int64_t>(p.units) * d.Hk, kManyUnits - 1));
 }
 
 hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32_t *lens, const int32_t *table, const void *q,

@@ -607,8 +607,14 @@ bool attn_step_fits(const AttnDims &d) {
   return dealt(d) ? join_of(d).workgroups <= kMostWorkgroups256 : static_cast<int64_t>(units_of(d)) * d.B <= kMostWorkgroups256;
 }
 
-size_t attn_step_workspace_bytes(const AttnDims &d) {
+size_t attn_step_used_bytes(const AttnDims &d) {
   if (!dealt(d)) return 256;
+  return part_bytes(d) + (static_cast<size_t>(d.B) * units_of(d) * sizeof(Spread) + 255) / 256 * 256;
+}
+size_t attn_step_workspace_bytes(const AttnDims &d) {
+  AttnDims one = d;  // (dealt's two sides come closer with every sequence: if it deals the work of some, then that of one)
+  one.B = 1;
+  if (!dealt(one)) return 256;
   return part_bytes(d) + (static_cast<size_t>(d.B) * units_of(d) * sizeof(Spread) + 255) / 256 * 256;
 }
 

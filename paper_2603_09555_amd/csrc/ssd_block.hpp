@@ -121,9 +121,12 @@ bool attn_prefill_fits(const AttnDims &d);
 hipError_t launch_attn_append(const AttnDims &d, const Rope &rope, const int32_t *cu, const int32_t *lens, const int32_t *table,
                               const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                               void *q_out, void *k_cache, void *v_cache, hipStream_t stream);
+// What a call uses of its workspace; what no call of fewer sequences and tokens, otherwise the same, uses more of.
+size_t attn_step_used_bytes(const AttnDims &d);
 size_t attn_step_workspace_bytes(const AttnDims &d);
 hipError_t launch_attn_step(const AttnDims &d, const int32_t *lens, const int32_t *table, const void *q, const void *k_cache,
                             const void *v_cache, float scale, void *y, void *workspace, hipStream_t stream);
+size_t attn_prefill_used_bytes(const AttnDims &d);
 size_t attn_prefill_workspace_bytes(const AttnDims &d);
 hipError_t launch_attn_prefill(const AttnDims &d, const int32_t *cu, const int32_t *lens, const int32_t *table, const void *q,
                                const void *k_cache, const void *v_cache, float scale, void *y, void *workspace,

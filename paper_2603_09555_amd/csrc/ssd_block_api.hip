@@ -166,7 +166,7 @@ ssd_status ssd_attn_step(const ssd_attn_shape *shape, const int32_t *seq_lens, c
   if (const ssd_status st = step_dims(shape, &d); st != SSD_OK) return st;
   if (!scale_ok(scale)) return SSD_ERR_SHAPE;
   if (const ssd_status st = attn_pointers(seq_lens, page_table, q, k_cache, v_cache, y); st != SSD_OK) return st;
-  if (!workspace_ok(workspace, workspace_bytes, ssd::attn_step_workspace_bytes(d))) return SSD_ERR_WORKSPACE;
+  if (!workspace_ok(workspace, workspace_bytes, ssd::attn_step_used_bytes(d))) return SSD_ERR_WORKSPACE;
   return status_of(ssd::launch_attn_step(d, seq_lens, page_table, q, k_cache, v_cache, scale, y, workspace,
                                          static_cast<hipStream_t>(hip_stream)));
 }
@@ -185,7 +185,7 @@ ssd_status ssd_attn_prefill(const ssd_attn_shape *shape, const int32_t *cu_seqle
   if (!cu_seqlens) return SSD_ERR_NULL;
   if (const ssd_status st = attn_pointers(seq_lens, page_table, q, k_cache, v_cache, y); st != SSD_OK) return st;
   if (!aligned4(cu_seqlens)) return SSD_ERR_ALIGN;
-  if (!workspace_ok(workspace, workspace_bytes, ssd::attn_prefill_workspace_bytes(d))) return SSD_ERR_WORKSPACE;
+  if (!workspace_ok(workspace, workspace_bytes, ssd::attn_prefill_used_bytes(d))) return SSD_ERR_WORKSPACE;
   return status_of(ssd::launch_attn_prefill(d, cu_seqlens, seq_lens, page_table, q, k_cache, v_cache, scale, y, workspace,
                                             static_cast<hipStream_t>(hip_stream)));
 }
