@@ -453,7 +453,7 @@ SSD_API ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *
  * Attention of one new token of each sequence over its cache:
  *     y[b][h] = sum_t softmax_t(scale * q[b][h] . K[t]) V[t]
  *   q, y              (batch, nheads, headdim) dense; y must not be q
- *   scale             positive and finite
+ *   scale             positive, up to 1e30
  *   workspace         at least ssd_attn_step_workspace_bytes() bytes, 256-byte
  *                     aligned; its size depends on the shape alone, and serves
  *                     shapes of fewer sequences, otherwise the same, too
@@ -474,7 +474,7 @@ SSD_API ssd_status ssd_attn_step(const ssd_attn_shape *shape, const int32_t *seq
  * what is cached) over the cache, to which they have been appended.
  *   q, y              (tokens, nheads, headdim) dense; y must not be q; y of
  *                     tokens outside every sequence is left untouched
- *   scale             positive and finite
+ *   scale             positive, up to 1e30
  *   workspace         at least ssd_attn_prefill_workspace_bytes() bytes, 256-byte
  *                     aligned; serves shapes of fewer sequences and tokens,
  *                     otherwise the same, too
