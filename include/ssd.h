@@ -387,8 +387,9 @@ SSD_API ssd_status ssd_norm_residual(int64_t rows, int32_t width, int32_t io_dty
  *
  * What the device arrays hold is not checked on the host, and cannot make a
  * kernel leave its tensors: a negative seq_lens[b] counts as 0;
- * boundaries are cut to [0, tokens] (a sequence whose end precedes its beginning has no
- * new tokens); tokens whose page table entry is not in [0, npages) are not
+ * boundaries are cut to [0, tokens], and where they decrease, so that sequences
+ * overlap, the call's results are anything (a sequence whose end precedes its
+ * beginning has no new tokens); tokens whose page table entry is not in [0, npages) are not
  * appended and not seen.  A new token that has no place in its sequence's row of
  * the page table -- in front of its beginning (seq_lens[b] smaller than the number
  * of its new tokens), or at max_pages * page_size or behind (a sequence that has
