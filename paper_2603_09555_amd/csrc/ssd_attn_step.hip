@@ -38,6 +38,7 @@ constexpr int workgroups_of(bool bf16, int dp) { return 256 * (dp == 256 ? 1 : b
 constexpr int kMostWorkgroups = 1024;
 constexpr unsigned kFewUnits = 256, kCUs = 256;
 constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
+constexpr float kMost = 3.0e38f;   // the largest maximum: behind it, probabilities are infinite and y is not a number
 
 // The workgroups that have blocks of a unit.  They write it down, so that the joining launch need not deal again.
 struct Spread {
@@ -339,11 +340,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
       }
       f32x4 s[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        s[h] = T::scores(keys, h, query);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[h][r] *= a.scale_log2;
-      }
+      for (int h = 0; h < 2; ++h) s[h] = T::scores(keys, h, query);
       if (seen != 0xffffffffu) {  // (what isn't seen may hold anything: no product with it is kept)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -357,8 +354,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
       float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
+      top *= a.scale_log2;
       if (__any(top > m)) {
-        const float next = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(m - next);
+        const float next = fmaxf(m, fminf(top, kMost)), keep = __builtin_amdgcn_exp2f(m - next);
         m = next;
         l *= keep;
 #pragma unroll
@@ -369,7 +367,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_a_simd(kBf16, DP)) void step_ker
       float p[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(s[i / 4][i % 4] - m);
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], a.scale_log2, -m));  // (rounded at the difference's size, not the logit's)
         l += p[i];
       }
       t.add(p, o);
