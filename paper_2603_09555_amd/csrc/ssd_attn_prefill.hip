@@ -38,7 +38,9 @@ constexpr int kMostSplits = 64;   // of a unit
 constexpr float kShare = 1.25f / kWorkgroups;
 constexpr int kMostParts = 2 * kWorkgroups;
 constexpr float kLongShare = 64.f;  // tiles, from which on the number of rounds is looked at
-constexpr float kNone = -3.0e38f;  // a maximum of nothing: finite, so that differences are numbers
+// A maximum of nothing: finite, so that differences are numbers.  None is larger than its opposite: behind that, probabilities are
+// infinite and y is not a number, where those of an infinite maximum would all be zero.
+constexpr float kNone = -3.0e38f;
 constexpr int tokens_of_tile(bool bf16) { return bf16 ? 64 : 32; }
 // Tiles that a workgroup at least takes where several share a unit, in us 5 in bf16 and 8 in fp32 with heads of 128 values alone on
 // a CU: fewer cost more in parts than they save.  (bf16, 3 tokens behind 27000, 8 heads over 1, window 927: 15 us, with 8 tiles 18; 90
@@ -647,7 +649,7 @@ __global__ __launch_bounds__(kThreads * kGroups, DP == 256 ? 1 : 2) void prefill
           float top = s[0];
 #pragma unroll
           for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
-          const float larger = fmaxf(m, both_halves_max(top) * a.scale_log2), keep = __builtin_amdgcn_exp2f(m - larger);
+          const float larger = fmaxf(m, fminf(both_halves_max(top) * a.scale_log2, -kNone)), keep = __builtin_amdgcn_exp2f(m - larger);
           m = larger;
           l *= keep;
 #pragma unroll
@@ -846,7 +848,7 @@ __global__ __launch_bounds__(kThreads * f32_groups(DP), DP == 256 ? 1 : 2) void 
         float top = s[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
-        const float larger = fmaxf(m, both_halves_max(top) * a.scale_log2), keep = __builtin_amdgcn_exp2f(m - larger);
+        const float larger = fmaxf(m, fminf(both_halves_max(top) * a.scale_log2, -kNone)), keep = __builtin_amdgcn_exp2f(m - larger);
         m = larger;
         l *= keep;
 #pragma unroll
