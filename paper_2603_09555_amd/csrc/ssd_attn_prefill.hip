@@ -14,8 +14,8 @@
 //
 // Where there are few units, several workgroups share one's tokens and leave (m, l, O) in the workspace for a second launch.
 //
-// 32 heads over 8 of 128, bf16: 16384 tokens 2.05 ms, 1070 TFLOP/s of the causal products (the library's large product: 1316); 4096
-// tokens 147 us, 1024 tokens 25 us; 64 tokens behind 32000 54 us.  fp32: see its kernel.
+// 32 heads over 8 of 128, bf16: 16384 tokens 2.04 to 2.19 ms from card to card, 1000 to 1080 TFLOP/s of the causal products (the
+// library's large product: 1316); 4096 tokens 148 us, 1024 tokens 26 us; 64 tokens behind 32000 55 us.  fp32: see its kernel.
 #include <algorithm>
 #include <cmath>
 

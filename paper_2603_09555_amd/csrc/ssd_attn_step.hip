@@ -22,7 +22,7 @@
 // where there are many units, takes a unit and there is no second launch.
 //
 // 32 heads over 8 of 128, bf16: 64 sequences to 32768 tokens 150 us, 5.9 TB/s of K and V; one of 32000 28 us, one of 518 8.8 us.
-// fp32, 2 sequences to 100004, 10 heads over 2 of 64: 41 us, 5.0 TB/s.
+// fp32, 2 sequences to 100004, 10 heads over 2 of 64: 48 us, 4.2 TB/s, of which the joining launch is 5.
 #include <algorithm>
 
 #include "ssd_attn.hpp"
@@ -545,7 +545,8 @@ bool dealt(const AttnDims &d) {
 // the start of one is beside the others' work.  32 heads over 8 of 128, bf16: 16 sequences of 500 tokens 9.1 us and 12.5, 64 of 250
 // 15.0 and 12.5, of 1000 41.7 and 38.7, 1024 of 1 to 200 134 and 52.
 //
-// Caches that do not fit the last-level cache (256 MiB) have been pushed out of it by the time they are read again: there, values, of
+// Caches that do not fit the last-level cache (256 MiB; the rule takes 320 of the caches, since the host does not know what is used
+// of them; what was measured nearest is 125 and 500 MiB) have been pushed out of it by the time they are read again: there, values, of
 // which an instruction reads whole lines, are loaded as data of no further use, and leave room for the keys, of which one reads half
 // lines.  64 sequences to 32768 165 us and 150, 16 of 8000 103 and 84; with caches that fit 16 of 2000 23 and 27.  (Both so: 16 of 8000
 // 90.)

@@ -7,7 +7,8 @@
 // A unit -- a row, or one group of a row -- is read once, kept in registers as fp32 while its squares are summed, and written
 // once.  A thread owns pieces of 8 neighbouring values (bf16: 16 bytes; fp32: 32).  Both are streams; with few rows they are a
 // chain of two memory latencies and a reduction, and the unit is spread over as many threads as it has pieces for.
-// 16384 rows of 5120, gated, bf16: 100 us, 5.0 TB/s (a copy: 4.9); 16383 of 768, residual, fp32: 40 us, 5.0 TB/s; one row: 3.1 us, a launch.
+// 16384 rows of 5120, gated, bf16: 100 us, 5.0 TB/s (a copy: 4.9), fp32: 183 us, 5.5; 16383 of 768, residual, fp32: 40 us, 5.0; 16384 of
+// 2560, bf16 on an fp32 stream: 95 us, 5.3, on a bf16 one: 66 us, 5.1; one row: 3 us, a launch.
 #include <algorithm>
 
 #include "ssd_block.hpp"

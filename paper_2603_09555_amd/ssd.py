@@ -571,7 +571,8 @@ def ssd_attn_append(q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens=
     """``ssd_attn_append``: ``k, v (tokens,nkvheads,headdim)`` go to the caches ``(npages,nkvheads,page_size,headdim)``, rotated
     as ``q (tokens,nheads,headdim)`` (or None) is on its way to ``q_out``.  ``rope = (cos, sin)``, each ``(positions,rotary/2)``
     fp32 with a row for every position that ``page_table (batch,max_pages)`` can hold, or None.  ``seq_lens (batch)`` counts the new
-    tokens too; without ``cu_seqlens (batch+1)`` every sequence has one.  ``q``, ``k`` and ``v`` may be slices of one projection's
+    tokens too; without ``cu_seqlens (batch+1)`` every sequence has one.  Tokens whose positions are not in their row of ``page_table`` are
+    left out, and see nothing in the attention calls.  ``q``, ``k`` and ``v`` may be slices of one projection's
     output, of which ``q_out`` may not be a part.  Returns ``q_out``, or None without ``q``."""
     out = _native.attn_append(q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved, q_out)
     if out is not None:
