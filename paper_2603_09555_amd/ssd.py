@@ -203,6 +203,12 @@ def _check_types(io, ios, f32s):
         raise ValueError("x, B and C must share one dtype; dt, A, D and states must be fp32")
 
 
+def _check_sizes(*sizes):
+    """Sizes as the C ABI takes them (ctypes would cut them to 32 bits)."""
+    if not all(-2 ** 31 <= n < 2 ** 31 for n in sizes):
+        raise ValueError("a size does not fit 32 bits")
+
+
 def _check_output(t, dtype, numel):
     """An output that the caller brings: of the type that is written, and no smaller than what is."""
     if t is not None and (t.dtype != dtype or t.numel() < numel):
@@ -494,6 +500,7 @@ def ssd_norm_gated(y, z, weight, eps=1e-5, groups=1, norm_first=False, out=None)
     if done is not None:
         return _done(done, "ssd_norm_gated")
     rows, width = y.shape
+    _check_sizes(width, groups)
     if z.shape != y.shape or z.dtype != y.dtype or weight.shape != (width,) or weight.dtype != torch.float32:
         raise ValueError("z must be like y, and weight fp32 of the rows' width")
     if not z.is_cuda or (width > 1 and z.stride(1) != 1) or (rows > 1 and z.stride(0) < width):
@@ -517,6 +524,7 @@ def ssd_norm_residual(residual, x, weight, scale=1.0, eps=1e-5, out=None, residu
     if done is not None:
         return _done(done, "ssd_norm_residual")
     rows, width = x.shape
+    _check_sizes(width)
     if weight.shape != (width,) or weight.dtype != torch.float32 or (residual is not None and residual.shape != x.shape):
         raise ValueError("residual must have the shape of x, and weight must be fp32 of the rows' width")
     stream = residual.dtype if residual is not None else residual_out.dtype if residual_out is not None else torch.float32
@@ -537,6 +545,7 @@ def ssd_norm_residual(residual, x, weight, scale=1.0, eps=1e-5, out=None, residu
 def make_attn_shape(batch, tokens, nheads, k_cache, page_table, window=0) -> ssd_attn_shape:
     """The ``ssd_attn_shape`` of a call on ``k_cache (npages,nkvheads,page_size,headdim)`` and ``page_table (batch,max_pages)``."""
     npages, nkv, page, headdim = k_cache.shape
+    _check_sizes(batch, tokens, nheads, *k_cache.shape, page_table.shape[1])
     window = max(-1, min(window, 2 ** 31 - 1))     # (anything that large is no limit, anything below zero refused)
     return ssd_attn_shape(batch, tokens, nheads, nkv, headdim, npages, page, page_table.shape[1], window, _IO_DTYPES.get(k_cache.dtype, -1))
 
@@ -588,6 +597,7 @@ def ssd_attn_append(q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens=
         cos, sin = rope
         if cos.dim() != 2 or sin.shape != cos.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32:
             raise ValueError("rope must be two fp32 tensors (positions, rotary / 2)")
+        _check_sizes(cos.shape[0], 2 * cos.shape[1])
         _check_dev(cos, sin)
         xr = ssd_rope(_ptr(cos), _ptr(sin), 2 * cos.shape[1], cos.shape[0], int(bool(interleaved)))
     heads, q_stride = nkv, 0
