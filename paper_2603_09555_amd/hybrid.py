@@ -42,12 +42,12 @@ class HybridCache:
     """What a batch of sequences leaves between calls.  ``lens`` counts the tokens of each sequence, ``held`` on the host."""
     lens: torch.Tensor                     # (batch) int32
     page_table: torch.Tensor               # (batch, max_pages) int32
-    held: list
     conv: dict = field(default_factory=dict)    # block -> (batch, channels, taps - 1)
     state: dict = field(default_factory=dict)   # block -> (batch, nheads, headdim, dstate) fp32
     keys: dict = field(default_factory=dict)    # block -> (npages, kv_heads, page_size, headdim)
     values: dict = field(default_factory=dict)
     workspace: torch.Tensor | None = None       # of the single-token attention, kept from step to step
+    held: list | None = None                    # lens on the host (None: not read yet)
 
 
 class HybridStack:
@@ -91,7 +91,7 @@ class HybridStack:
         pages = -(-max_tokens // c.page_size)
         order = torch.randperm(batch * pages, generator=torch.Generator().manual_seed(seed))
         cache = HybridCache(torch.zeros((batch,), dtype=torch.int32, device=self.device),
-                            order.to(torch.int32).view(batch, pages).to(self.device), [0] * batch)
+                            order.to(torch.int32).view(batch, pages).to(self.device), held=[0] * batch)
         for i, b in enumerate(self.blocks):
             if b["kind"] == "M":
                 cache.conv[i] = torch.zeros((batch, sum(self.conv_split), c.conv_taps - 1), dtype=self.dtype, device=self.device)
@@ -109,6 +109,8 @@ class HybridStack:
 
     def _grow(self, cache, new):
         """Sequences get ``new`` tokens each, for which there must be pages."""
+        if cache.held is None:
+            cache.held = cache.lens.tolist()
         held = [h + n for h, n in zip(cache.held, new, strict=True)]
         if max(held) > cache.page_table.shape[1] * self.config.page_size:
             raise ValueError("a sequence has outgrown its pages")

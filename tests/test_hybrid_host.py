@@ -17,3 +17,7 @@ def test_sequences_do_not_outgrow_their_pages():
     assert cache.held == [32, 5] and cache.lens.tolist() == [32, 5]
     with pytest.raises(ValueError):
         stack.prefill(torch.zeros(3, 32), [3], cache)      # a length for every sequence
+    cache.held = None                                      # (read from lens)
+    with pytest.raises(ValueError, match="outgrown"):
+        stack.step(torch.zeros(2, 32), cache)
+    assert cache.held == [32, 5]
