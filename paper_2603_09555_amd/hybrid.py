@@ -179,7 +179,7 @@ class HybridStack:
 
     def step(self, x, cache: HybridCache):
         """``x (batch,width)``: one new token of every sequence."""
-        self._grow(cache, [1] * len(cache.held))
+        self._grow(cache, [1] * len(cache.lens))
         cache.lens += 1
         return self._run(x, cache, None, None)
 
