@@ -325,6 +325,93 @@ SSD_API ssd_status ssd_conv1d_step(int32_t batch, int32_t ksize, int32_t io_dtyp
                            void *hip_stream);
 
 /*
+ * ssd_conv1d_prefill for a packed, variable-length batch (ragged prompts, or later
+ * pieces of prompts): `batch` sequences laid back to back along the token axis,
+ * each filtered from its own cached inputs.
+ *   cu_seqlens        DEVICE array of batch + 1 int32, 4-byte aligned: sequence q owns
+ *                     tokens [cu_seqlens[q], cu_seqlens[q+1]) of `tokens`.  Boundaries
+ *                     are cut to [0, tokens]; a sequence whose end precedes its
+ *                     beginning has no token; where boundaries decrease, so that
+ *                     sequences overlap, the call's results are anything
+ *   u                 (tokens, channels) io dtype, rows u_stride >= channels elements
+ *                     apart (a slice of the input projection's output), aligned to its
+ *                     elements
+ *   z0..z2            (tokens, split[i]); rows of tokens outside every sequence are left
+ *                     untouched
+ *   conv_state_in     (batch, channels, ksize-1) or NULL = zeros
+ *   conv_state_out    likewise, or NULL; may be conv_state_in (updated in place), and
+ *                     must not overlap it otherwise.  A sequence without a token keeps
+ *                     its cache
+ * Everything else, and every bit of the outputs, is as for ssd_conv1d_prefill of
+ * each sequence by itself.  A call of 2^32 threads or more (one a channel and 16
+ * tokens, or a channel and sequence, at most) is refused with SSD_ERR_SHAPE.
+ * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _HIP.
+ */
+SSD_API ssd_status ssd_conv1d_varlen(int32_t batch, int32_t tokens, int32_t ksize, int32_t io_dtype,
+                             const int32_t *split, const int32_t *cu_seqlens,
+                             const void *u, int64_t u_stride, const float *weight,
+                             const float *bias, const void *conv_state_in,
+                             void *z0, void *z1, void *z2, void *conv_state_out,
+                             int32_t activation, void *hip_stream);
+
+/*
+ * Selective state space scan (the layer core of a Mamba-1 block, for stacks that
+ * mix such blocks with others): a step size for every channel, a decay for every
+ * channel and state, B and C shared by all channels.  Token by token
+ *     d       = clamp(softplus(dt + dt_bias[c]), dt_min, dt_max)
+ *     h[c][n] = exp(d A[c][n]) h[c][n] + d x[c] B[n]
+ *     y[c]    = (sum_n C[n] h[c][n] + D[c] x[c]) * silu(z[c])
+ *   x, y              (tokens, channels) io dtype, dense; y must not overlap an input
+ *   dt                (tokens, channels) of dt_dtype (SSD_F32, or io_dtype), dense; the map
+ *                     of dt_transform is applied as for ssd_prefill_dt (dt_bias is
+ *                     (channels)); dt_transform may be NULL: dt is the step size
+ *   A                 (channels, dstate) fp32, <= 0
+ *   B, C              (tokens, dstate) io dtype, rows B_stride, C_stride >= dstate elements
+ *                     apart (slices of one projection's output), aligned to their elements
+ *   D                 (channels) fp32, or NULL = zeros
+ *   z                 (tokens, channels) io dtype, rows z_stride >= channels elements apart,
+ *                     aligned to its elements; or NULL: no gate
+ *   state, h0, final_state  (batch, channels, dstate) fp32
+ * dstate is at most 256 (SSD_ERR_UNSUPPORTED), channels at most 2^22; the other pointers
+ * are 16-byte aligned.  Arithmetic, sums and states are fp32; y is rounded once.
+ *
+ * ssd_selective_prefill scans a packed batch; cu_seqlens as for ssd_conv1d_varlen.
+ * A sequence starts from h0[q] (h0 NULL: zeros) and leaves final_state[q], also
+ * without a token; final_state may be h0, and must not overlap it otherwise.
+ *   workspace         at least ssd_selective_prefill_workspace_bytes() bytes, 256-byte
+ *                     aligned, whose size depends on the shape alone; calls that may
+ *                     overlap in time need one each
+ * A sequence's last bits may depend on where the batch's other sequences lie: time is
+ * cut into segments of the packed tokens.  A call repeats bit for bit.
+ *
+ * ssd_selective_step scans one token of each sequence: tokens is batch, state is
+ * updated in place; shape->tokens is ignored.
+ * A call whose launches would have 2^32 threads or more is refused with SSD_ERR_SHAPE;
+ * that is not so below 2^24 tokens times states and 2^24 sequences times channels.
+ * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _UNSUPPORTED, _ALIGN, _WORKSPACE, _HIP.
+ */
+typedef struct {
+  int32_t batch;    /* sequences */
+  int32_t tokens;   /* all sequences together (ssd_selective_step: ignored, one each) */
+  int32_t channels;
+  int32_t dstate;   /* states of a channel */
+  int32_t io_dtype; /* ssd_dtype of x, B, C, z and y */
+  int32_t dt_dtype; /* of dt: SSD_F32, or io_dtype */
+} ssd_selective_shape;
+SSD_API size_t ssd_selective_prefill_workspace_bytes(const ssd_selective_shape *shape);
+SSD_API ssd_status ssd_selective_prefill(const ssd_selective_shape *shape, const ssd_dt_transform *dt_transform,
+                                 const int32_t *cu_seqlens, const void *x, const void *dt,
+                                 const float *A, const void *B, int64_t B_stride, const void *C,
+                                 int64_t C_stride, const float *D, const void *z, int64_t z_stride,
+                                 const float *h0, void *y, float *final_state, void *workspace,
+                                 size_t workspace_bytes, void *hip_stream);
+SSD_API ssd_status ssd_selective_step(const ssd_selective_shape *shape, const ssd_dt_transform *dt_transform,
+                              float *state, const void *x, const void *dt, const float *A,
+                              const void *B, int64_t B_stride, const void *C, int64_t C_stride,
+                              const float *D, const void *z, int64_t z_stride, void *y,
+                              void *hip_stream);
+
+/*
  * The norms on either side of a Mamba-2 block (Alg. 1 and 2 name the block's
  * projections and residual stream around the core; section "Mapping SSD onto
  * JAX primitives" keeps residual and norm arithmetic in fp32).
@@ -449,6 +536,24 @@ SSD_API ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *
                            const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                            const void *v, int64_t v_stride, void *q_out,
                            void *k_cache, void *v_cache, void *hip_stream);
+
+/*
+ * ssd_attn_append with norms of the heads: every head of queries and keys is
+ * normalised by itself, in front of the rotation,
+ *     u = v * rsqrt(mean(v^2) + eps) * weight
+ * in fp32, and rounded once behind it.  Values are copied.
+ *   q_weight, k_weight  (headdim) fp32, 16-byte aligned; q_weight may be NULL if q is
+ *   eps               >= 0
+ * Everything else is as for ssd_attn_append, but for the sizes that are refused with
+ * SSD_ERR_SHAPE: none below 2^24 tokens and 2^27 tokens times heads (of queries, keys
+ * and values).
+ */
+SSD_API ssd_status ssd_attn_append_norm(const ssd_attn_shape *shape, const ssd_rope *rope, const int32_t *cu_seqlens,
+                                const int32_t *seq_lens, const int32_t *page_table,
+                                const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                const void *v, int64_t v_stride, const float *q_weight,
+                                const float *k_weight, float eps, void *q_out,
+                                void *k_cache, void *v_cache, void *hip_stream);
 
 /*
  * Attention of one new token of each sequence over its cache:

@@ -48,6 +48,15 @@ struct BlockApi {
   decltype(&ssd_attn_prefill) attn_prefill;
 } block_api;
 
+// Blocks of other kinds in such a stack: packed convolution, selective scan, normed heads.
+struct MixerApi {
+  decltype(&ssd_conv1d_varlen) conv_varlen;
+  decltype(&ssd_selective_prefill_workspace_bytes) selective_workspace_bytes;
+  decltype(&ssd_selective_prefill) selective_prefill;
+  decltype(&ssd_selective_step) selective_step;
+  decltype(&ssd_attn_append_norm) attn_append_norm;
+} mixer_api;
+
 // An argument: a plain dense device tensor, or None.
 struct Arg {
   const at::Tensor *t = nullptr;
@@ -80,6 +89,13 @@ int io_of(const Arg &a) {
 bool fits(std::initializer_list<int64_t> values) {
   for (int64_t v : values)
     if (v < 0 || v > INT32_MAX) return false;
+  return true;
+}
+// Whether the tensors that are there are on the current device, whose stream the call takes.
+bool here(std::initializer_list<const Arg *> args) {
+  const auto device = c10::hip::current_device();
+  for (const Arg *a : args)
+    if (a->t != nullptr && a->t->get_device() != device) return false;
   return true;
 }
 void *stream() { return c10::hip::getCurrentHIPStream().stream(); }
@@ -462,10 +478,14 @@ Cache cache_of(PyObject *k, PyObject *v, PyObject *table, PyObject *lens, PyObje
   return c;
 }
 
-// (q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved, q_out)
-PyObject *attn_append(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+// (q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved, q_out); with norms: q_weight, k_weight
+// before the caches, eps before q_out
+template <bool kNorm>
+PyObject *attn_append(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
-  SSD_ARGS(11);
+  SSD_ARGS(kNorm ? 14 : 11);
+  PyObject *a[11];
+  for (int i = 0; i < 11; ++i) a[i] = args[i + (!kNorm || i < 3 ? 0 : i < 10 ? 2 : 3)];
   const Arg q = a[0] == Py_None ? Arg() : rows_of(a[0], 3), k = rows_of(a[1], 3), v = rows_of(a[2], 3);
   const bool queries = a[0] != Py_None;
   if ((queries && !q.ok) || !k.ok || !v.ok || (!queries && a[10] != Py_None)) return none();
@@ -491,6 +511,7 @@ PyObject *attn_append(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     rope.sin = (const float *)sn.ptr();
     rope.rotary = (int32_t)(2 * cs.t->size(1));
     rope.positions = (int32_t)cs.t->size(0);
+    if (kNorm && !here({&cs, &sn})) return none();
   }
   at::Tensor own;
   Arg out;
@@ -502,15 +523,27 @@ PyObject *attn_append(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
       return none();
     }
   }
+  Arg qw, kw;
+  float eps = 0.f;
+  if (kNorm) {
+    qw = tensor_or_none(args[3]);
+    kw = tensor(args[4]);
+    if (!qw.ok || !kw.ok || (qw.t != nullptr) != queries || !f32(kw) || !is(kw, {D}) || (queries && (!f32(qw) || !is(qw, {D}))) ||
+        !number_of(args[12], &eps) || !here({&q, &k, &v, &qw, &kw, &c.k, &c.v, &c.table, &c.lens, &c.cu, &out}))
+      return none();
+  }
   c.shape.tokens = (int32_t)tokens;
   c.shape.nheads = (int32_t)heads;
   void *const s = stream();
+  const float *const qwp = (const float *)qw.ptr(), *const kwp = (const float *)kw.ptr();
   const void *const qp = q.ptr(), *const kp = k.ptr(), *const vp = v.ptr();
   void *const op = out.ptr(), *const kc = c.k.ptr(), *const vc = c.v.ptr();
   const int32_t *const cu = (const int32_t *)c.cu.ptr(), *const lens = (const int32_t *)c.lens.ptr(), *const table = (const int32_t *)c.table.ptr();
   const int64_t qs = stride(q), ks = stride(k), vs = stride(v);
-  const ssd_status st =
-      released([&] { return block_api.attn_append(&c.shape, &rope, cu, lens, table, qp, qs, kp, ks, vp, vs, op, kc, vc, s); });
+  const ssd_status st = released([&] {
+    return kNorm ? mixer_api.attn_append_norm(&c.shape, &rope, cu, lens, table, qp, qs, kp, ks, vp, vs, qwp, kwp, eps, op, kc, vc, s)
+                 : block_api.attn_append(&c.shape, &rope, cu, lens, table, qp, qs, kp, ks, vp, vs, op, kc, vc, s);
+  });
   if (st != SSD_OK) return failed(st);
   // (nothing to return is not the same as nothing done: False)
   if (!queries) Py_RETURN_FALSE;
@@ -558,7 +591,146 @@ PyObject *attn(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// init(addresses), init_block(addresses): the functions of the C ABI in the order of Api, of BlockApi
+// elements between the rows of a tensor of dense ones; -1: rows overlap
+int64_t row_stride(const Arg &t) {
+  const int64_t rows = t.t->size(0), width = t.t->size(1);
+  return rows <= 1 ? width : t.t->stride(0) >= width ? t.t->stride(0) : -1;
+}
+
+// (u, weight, bias, cu_seqlens, conv_state, split, activation, outs, conv_state_out)
+PyObject *conv1d_varlen(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  SSD_ARGS(9);
+  const Arg u = rows_of(a[0], 2), weight = tensor(a[1]), bias = tensor_or_none(a[2]), cu = tensor(a[3]), state = tensor_or_none(a[4]);
+  const int act = activation_of(a[6]);
+  if (!u.ok || !weight.ok || !bias.ok || !cu.ok || !state.ok || act < 0 || weight.t->dim() != 2 || cu.t->scalar_type() != at::kInt) return none();
+  const int64_t T = u.t->size(0), C = u.t->size(1), k = weight.t->size(1), nseq = cu.t->numel() - 1, stride = row_stride(u);
+  const int io = io_of(u);
+  int32_t w[3];
+  if (io < 0 || nseq < 1 || stride < 0 || !fits({nseq, T, C, k}) || k < 1 || !split_of(a[5], C, w) || !f32(weight) || !is(weight, {C, k}) ||
+      (bias.t != nullptr && (!f32(bias) || !is(bias, {C}))) ||
+      (state.t != nullptr && (state.t->scalar_type() != u.t->scalar_type() || !is(state, {nseq, C, k - 1}))))
+    return none();
+  int n = 0;
+  for (int i = 0; i < 3; ++i) n += w[i] > 0;
+  at::Tensor own[3], own_state;
+  Arg out[3], new_state;
+  const bool given = a[7] != Py_None;
+  if (given && (!PyList_CheckExact(a[7]) || PyList_GET_SIZE(a[7]) != n)) return none();
+  if (a[8] != Py_None && (!(new_state = tensor(a[8])).ok || new_state.t->scalar_type() != u.t->scalar_type() || new_state.t->numel() < nseq * C * (k - 1)))
+    return none();
+  if (given)
+    for (int i = 0, at = 0; i < 3; ++i)
+      if (w[i] > 0 && (!(out[i] = tensor(PyList_GET_ITEM(a[7], at++))).ok || io_of(out[i]) != io || out[i].t->numel() < T * w[i])) return none();
+  if (!here({&u, &weight, &bias, &cu, &state, &new_state, &out[0], &out[1], &out[2]})) return none();
+  void *z[3] = {nullptr, nullptr, nullptr};
+  for (int i = 0; i < 3; ++i)
+    if (w[i] > 0) {
+      if (!given) {
+        own[i] = at::empty({T, w[i]}, u.t->options());
+        out[i].t = &own[i];
+      }
+      z[i] = out[i].ptr();
+    }
+  if (a[8] == Py_None) {
+    own_state = at::empty({nseq, C, k - 1}, u.t->options());
+    new_state.t = &own_state;
+  }
+  void *const s = stream(), *const np = new_state.ptr();
+  const void *const up = u.ptr(), *const sp = state.ptr();
+  const float *const Wp = (const float *)weight.ptr(), *const bp = (const float *)bias.ptr();
+  const int32_t *const cp = (const int32_t *)cu.ptr();
+  const ssd_status st = released([&] {
+    return mixer_api.conv_varlen((int32_t)nseq, (int32_t)T, (int32_t)k, io, w, cp, up, stride, Wp, bp, sp, z[0], z[1], z[2], np, act, s);
+  });
+  if (st != SSD_OK) return failed(st);
+  PyObject *const outs = given ? new_ref(a[7]) : PyList_New(n);
+  if (outs == nullptr) return nullptr;
+  if (!given)
+    for (int i = 0, at = 0; i < 3; ++i)
+      if (w[i] > 0) PyList_SET_ITEM(outs, at++, THPVariable_Wrap(std::move(own[i])));
+  PyObject *const rs = result(a[8], own_state);
+  PyObject *const both = rs != nullptr ? PyTuple_Pack(2, outs, rs) : nullptr;
+  Py_DECREF(outs);
+  Py_XDECREF(rs);
+  return both;
+  END_HANDLE_TH_ERRORS
+}
+
+// prefill: (x, dt, A, B, C, D, cu_seqlens, z, h0, y, final_state, workspace, dt_bias, dt_softplus, dt_limit)
+// step: (state, x, dt, A, B, C, D, z, y, dt_bias, dt_softplus, dt_limit)
+template <bool kStep>
+PyObject *selective(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  SSD_ARGS(kStep ? 12 : 15);
+  PyObject *const *const a = args + (kStep ? 1 : 0);
+  const Arg x = tensor(a[0]), dt = tensor(a[1]), A = tensor(a[2]), B = rows_of(a[3], 2), C = rows_of(a[4], 2), D = tensor_or_none(a[5]);
+  PyObject *const zo = a[kStep ? 6 : 7], *const yo = a[kStep ? 7 : 9];
+  const Arg z = zo == Py_None ? tensor_or_none(zo) : rows_of(zo, 2);
+  if (!x.ok || !dt.ok || !A.ok || !B.ok || !C.ok || !D.ok || !z.ok || x.t->dim() != 2 || A.t->dim() != 2) return none();
+  const int64_t T = x.t->size(0), channels = x.t->size(1), N = A.t->size(1);
+  const int io = io_of(x), dio = io_of(dt);
+  if (io < 0 || dio < 0 || !is(dt, {T, channels}) || !f32(A) || !is(A, {channels, N}) || io_of(B) != io || io_of(C) != io || !is(B, {T, N}) ||
+      !is(C, {T, N}) || (D.t != nullptr && (!f32(D) || !is(D, {channels}))) || (z.t != nullptr && (io_of(z) != io || !is(z, {T, channels}))) ||
+      !fits({T, channels, N}))
+    return none();
+  const int64_t bs = row_stride(B), cs = row_stride(C), zs = z.t != nullptr ? row_stride(z) : 0;
+  if (bs < 0 || cs < 0 || zs < 0) return none();
+  const DtArgs dx = dt_args(a[kStep ? 8 : 12], a[kStep ? 9 : 13], a[kStep ? 10 : 14], {channels});
+  if (!dx.ok) return none();
+  Arg bias;
+  if (dx.x.dt_bias != nullptr) bias = tensor(a[kStep ? 8 : 12]);
+  Arg cu, h0, state, w, y;
+  int64_t nseq = T;
+  if (kStep) {
+    state = tensor(args[0]);
+    if (!state.ok || !f32(state) || !is(state, {T, channels, N})) return none();
+  } else {
+    cu = tensor(a[6]);
+    h0 = tensor_or_none(a[8]);
+    if (!cu.ok || cu.t->scalar_type() != at::kInt || !h0.ok) return none();
+    nseq = cu.t->numel() - 1;
+    if (nseq < 1 || !fits({nseq}) || (h0.t != nullptr && (!f32(h0) || !is(h0, {nseq, channels, N})))) return none();
+    if (a[10] != Py_None && (!(state = tensor(a[10])).ok || !f32(state) || state.t->numel() < nseq * channels * N)) return none();
+    if (a[11] != Py_None && !(w = tensor(a[11])).ok) return none();
+  }
+  if (!here({&x, &dt, &A, &B, &C, &D, &z, &bias, &cu, &h0, &state, &w})) return none();
+  at::Tensor own, own_state, own_w;
+  if (!output_like(yo, x, own, y) || !here({&y})) return none();
+  const ssd_selective_shape shape = {(int32_t)nseq, (int32_t)T, (int32_t)channels, (int32_t)N, io, dio};
+  if (!kStep) {
+    if (a[10] == Py_None) {
+      own_state = at::empty({nseq, channels, N}, A.t->options());
+      state.t = &own_state;
+    }
+    if (a[11] == Py_None) {
+      const size_t need = mixer_api.selective_workspace_bytes(&shape);
+      own_w = at::empty({(int64_t)(need > 256 ? need : 256)}, x.t->options().dtype(at::kByte));
+      w.t = &own_w;
+    }
+  }
+  const size_t bytes = w.t != nullptr ? w.t->nbytes() : 0;
+  void *const s = stream(), *const yp = y.ptr(), *const wp = w.ptr();
+  float *const sp = (float *)state.ptr();
+  const void *const xp = x.ptr(), *const dp = dt.ptr(), *const Bp = B.ptr(), *const Cp = C.ptr(), *const zp = z.ptr();
+  const float *const Ap = (const float *)A.ptr(), *const Dp = (const float *)D.ptr(), *const hp = (const float *)h0.ptr();
+  const int32_t *const cp = (const int32_t *)cu.ptr();
+  const ssd_dt_transform *const dtx = dx.given ? &dx.x : nullptr;
+  const ssd_status st = released([&] {
+    return kStep ? mixer_api.selective_step(&shape, dtx, sp, xp, dp, Ap, Bp, bs, Cp, cs, Dp, zp, zs, yp, s)
+                 : mixer_api.selective_prefill(&shape, dtx, cp, xp, dp, Ap, Bp, bs, Cp, cs, Dp, zp, zs, hp, yp, sp, wp, bytes, s);
+  });
+  if (st != SSD_OK) return failed(st);
+  if (kStep) return result(yo, own);
+  PyObject *const r0 = result(yo, own), *const r1 = result(a[10], own_state);
+  PyObject *const both = r0 != nullptr && r1 != nullptr ? PyTuple_Pack(2, r0, r1) : nullptr;
+  Py_XDECREF(r0);
+  Py_XDECREF(r1);
+  return both;
+  END_HANDLE_TH_ERRORS
+}
+
+// init(addresses), init_block(addresses), init_mixer(addresses): the functions of the C ABI in the order of Api, BlockApi, MixerApi
 template <typename A, A *kTo>
 PyObject *init(PyObject *, PyObject *list) {
   constexpr Py_ssize_t kCount = sizeof(A) / sizeof(void *);
@@ -581,6 +753,7 @@ PyObject *init(PyObject *, PyObject *list) {
 PyMethodDef methods[] = {
     {"init", init<Api, &api>, METH_O, nullptr},
     {"init_block", init<BlockApi, &block_api>, METH_O, nullptr},
+    {"init_mixer", init<MixerApi, &mixer_api>, METH_O, nullptr},
     SSD_FAST("decode_step", decode_step),
     SSD_FAST("decode_step_layers", decode_layers<false>),
     SSD_FAST("decode_steps_layers", decode_layers<true>),
@@ -590,7 +763,11 @@ PyMethodDef methods[] = {
     SSD_FAST("conv1d_step", conv1d<true>),
     SSD_FAST("norm_gated", norm_gated),
     SSD_FAST("norm_residual", norm_residual),
-    SSD_FAST("attn_append", attn_append),
+    SSD_FAST("attn_append", attn_append<false>),
+    SSD_FAST("attn_append_norm", attn_append<true>),
+    SSD_FAST("conv1d_varlen", conv1d_varlen),
+    SSD_FAST("selective_prefill", selective<false>),
+    SSD_FAST("selective_step", selective<true>),
     SSD_FAST("attn_step", attn<true>),
     SSD_FAST("attn_prefill", attn<false>),
     {nullptr, nullptr, 0, nullptr}};

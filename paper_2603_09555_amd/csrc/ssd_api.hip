@@ -425,6 +425,29 @@ ssd_status ssd_conv1d_prefill(int32_t batch, int32_t seqlen, int32_t ksize, int3
   return e == hipSuccess ? SSD_OK : SSD_ERR_HIP;
 }
 
+ssd_status ssd_conv1d_varlen(int32_t batch, int32_t tokens, int32_t ksize, int32_t io_dtype, const int32_t *split,
+                             const int32_t *cu_seqlens, const void *u, int64_t u_stride, const float *weight, const float *bias,
+                             const void *conv_state_in, void *z0, void *z1, void *z2, void *conv_state_out, int32_t activation,
+                             void *hip_stream) {
+  void *z[3];
+  int width[3];
+  // (u is aligned to its elements: what conv_args checks of it is whether it is there)
+  const uintptr_t element = io_dtype == SSD_BF16 ? 2 : 4;
+  const ssd_status st = conv_args(batch, ksize, io_dtype, split, u ? weight : u, weight, z0, z1, z2, activation, z, width);
+  if (st != SSD_OK) return st;
+  const int64_t channels = static_cast<int64_t>(split[0]) + split[1] + split[2];
+  if (tokens < 1 || tokens > (1 << 30) || batch > (1 << 30) || u_stride < channels || static_cast<long double>(u_stride) * tokens > 1.0e15L ||
+      !ssd::conv_varlen_fits(batch, tokens, channels))
+    return SSD_ERR_SHAPE;
+  if (!cu_seqlens) return SSD_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(u) % element != 0 || (reinterpret_cast<uintptr_t>(cu_seqlens) & 3) != 0 || !aligned16(bias) ||
+      !aligned16(conv_state_in) || !aligned16(conv_state_out))
+    return SSD_ERR_ALIGN;
+  const hipError_t e = ssd::launch_conv_varlen(batch, tokens, ksize, io_dtype == SSD_BF16, cu_seqlens, u, u_stride, weight, bias, conv_state_in, z,
+                                               width, conv_state_out, activation, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? SSD_OK : SSD_ERR_HIP;
+}
+
 ssd_status ssd_conv1d_step(int32_t batch, int32_t ksize, int32_t io_dtype, const int32_t *split, void *conv_state,
                            const void *u, const float *weight, const float *bias, void *z0, void *z1, void *z2,
                            int32_t activation, void *hip_stream) {

@@ -12,16 +12,12 @@
 // 128: 4.3 us, fp32 the same.
 #include <algorithm>
 
-#include "ssd_attn.hpp"
+#include "ssd_attn_append.hpp"
 
 namespace ssd {
 namespace {
 
-using namespace block;
-
 constexpr int kBatch = 2;        // tokens whose pieces a thread has on their way at a time
-constexpr int kMostTokens = 4;   // a workgroup
-constexpr int kFewWorkgroups = 2048;  // more take several tokens each
 
 struct AppendArgs {
   const void *src[3];      // q, k, v
@@ -36,40 +32,6 @@ struct AppendArgs {
   int q_heads;             // 0: no queries
   int run;                 // tokens a workgroup
 };
-
-struct Place {
-  int pos;       // < 0: none
-  int64_t slot;  // cache row of key head 0, or -1
-};
-
-template <bool kBf16>
-using Element = typename std::conditional<kBf16, uint16_t, float>::type;
-__device__ __forceinline__ float value(float v) { return v; }
-__device__ __forceinline__ float value(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
-template <bool kBf16, int W>
-__device__ __forceinline__ void unpack(const u32x4 &q, float (&v)[W]) {
-#pragma unroll
-  for (int i = 0; i < W; ++i) v[i] = !kBf16 ? __uint_as_float(q[i % 4]) : i % 2 == 0 ? bf_lo(q[i / 2]) : bf_hi(q[i / 2]);
-}
-// N neighbouring values at an address of any multiple of 4
-template <int N>
-__device__ __forceinline__ void load_rope(const float *p, float *v) {
-  typedef f32x4 __attribute__((aligned(4))) vec4;
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  typedef f32x2 __attribute__((aligned(4))) vec2;
-  if constexpr (N == 2) {
-    const f32x2 a = *reinterpret_cast<const vec2 *>(p);
-    v[0] = a[0];
-    v[1] = a[1];
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const f32x4 a = *reinterpret_cast<const vec4 *>(p + i);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[i + k] = a[k];
-    }
-  }
-}
 
 // kWhole: pieces lie in one half of the pairs (interleaved pairs: in the rotated part) or outside it.
 template <bool kBf16, bool kWhole>

@@ -121,6 +121,11 @@ bool attn_prefill_fits(const AttnDims &d);
 hipError_t launch_attn_append(const AttnDims &d, const Rope &rope, const int32_t *cu, const int32_t *lens, const int32_t *table,
                               const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                               void *q_out, void *k_cache, void *v_cache, hipStream_t stream);
+bool attn_append_norm_fits(const AttnDims &d, bool queries);
+hipError_t launch_attn_append_norm(const AttnDims &d, const Rope &rope, const int32_t *cu, const int32_t *lens, const int32_t *table,
+                                   const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                                   const float *q_weight, const float *k_weight, float eps, void *q_out, void *k_cache, void *v_cache,
+                                   hipStream_t stream);
 // What a call uses of its workspace; what no call of fewer sequences and tokens, otherwise the same, uses more of.
 size_t attn_step_used_bytes(const AttnDims &d);
 size_t attn_step_workspace_bytes(const AttnDims &d);

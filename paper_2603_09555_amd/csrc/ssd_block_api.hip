@@ -90,6 +90,36 @@ bool workspace_ok(const void *workspace, size_t given, size_t need) {
 
 ssd_status status_of(hipError_t e) { return e == hipSuccess ? SSD_OK : SSD_ERR_HIP; }
 
+// What the two calls that append check but for the shape; strides: of q, k and v.
+ssd_status append_args(const AttnDims &d, const ssd_rope *rope, const int32_t *cu_seqlens, const int32_t *seq_lens, const int32_t *page_table,
+                       const void *q, const void *k, const void *v, const int64_t (&strides)[3], void *q_out, void *k_cache, void *v_cache) {
+  if (!rope || !seq_lens || !page_table || !k || !v || !k_cache || !v_cache || (q == nullptr) != (q_out == nullptr))
+    return SSD_ERR_NULL;
+  if (rope->rotary < 0 || rope->rotary % 2 != 0 || rope->rotary > d.D || (rope->interleaved != 0 && rope->interleaved != 1))
+    return SSD_ERR_SHAPE;
+  if (rope->rotary > 0) {
+    if (!rope->cos || !rope->sin) return SSD_ERR_NULL;
+    if (!aligned16(rope->cos) || !aligned16(rope->sin)) return SSD_ERR_ALIGN;
+    if (rope->positions < d.capacity()) return SSD_ERR_SHAPE;
+  }
+  const int64_t piece = d.bf16 ? 8 : 4;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t row = static_cast<int64_t>(i == 0 ? d.H : d.Hk) * d.D;
+    if (strides[i] < row || static_cast<long double>(strides[i]) * d.T > 1.0e15L) return SSD_ERR_SHAPE;
+    if (strides[i] % piece != 0) return SSD_ERR_ALIGN;
+  }
+  if (!aligned4(seq_lens) || !aligned4(page_table) || !aligned4(cu_seqlens) ||
+      !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_cache) || !aligned16(v_cache))
+    return SSD_ERR_ALIGN;
+  if (q) {  // a thread that rotates reads what its neighbour writes
+    const int64_t size = d.bf16 ? 2 : 4, head = d.D * size, out = static_cast<int64_t>(d.T) * d.H * head;
+    const void *const from[3] = {q, k, v};
+    for (int i = 0; i < 3; ++i)
+      if (reaches(q_out, out, from[i], strides[i] * size, (i == 0 ? d.H : d.Hk) * head, d.T)) return SSD_ERR_UNSUPPORTED;
+  }
+  return SSD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -124,34 +154,29 @@ ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *rope, co
   AttnDims d;
   if (const ssd_status st = make_dims(shape, cu_seqlens != nullptr, &d); st != SSD_OK) return st;
   if (!ssd::attn_append_fits(d, q != nullptr)) return SSD_ERR_SHAPE;
-  if (!rope || !seq_lens || !page_table || !k || !v || !k_cache || !v_cache || (q == nullptr) != (q_out == nullptr))
-    return SSD_ERR_NULL;
-  if (rope->rotary < 0 || rope->rotary % 2 != 0 || rope->rotary > d.D || (rope->interleaved != 0 && rope->interleaved != 1))
-    return SSD_ERR_SHAPE;
-  if (rope->rotary > 0) {
-    if (!rope->cos || !rope->sin) return SSD_ERR_NULL;
-    if (!aligned16(rope->cos) || !aligned16(rope->sin)) return SSD_ERR_ALIGN;
-    if (rope->positions < d.capacity()) return SSD_ERR_SHAPE;
-  }
-  const int64_t piece = d.bf16 ? 8 : 4;
   const int64_t strides[3] = {q ? q_stride : static_cast<int64_t>(d.H) * d.D, k_stride, v_stride};
-  for (int i = 0; i < 3; ++i) {
-    const int64_t row = static_cast<int64_t>(i == 0 ? d.H : d.Hk) * d.D;
-    if (strides[i] < row || static_cast<long double>(strides[i]) * d.T > 1.0e15L) return SSD_ERR_SHAPE;
-    if (strides[i] % piece != 0) return SSD_ERR_ALIGN;
-  }
-  if (!aligned4(seq_lens) || !aligned4(page_table) || !aligned4(cu_seqlens) ||
-      !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_cache) || !aligned16(v_cache))
-    return SSD_ERR_ALIGN;
-  if (q) {  // a thread that rotates reads what its neighbour writes
-    const int64_t size = d.bf16 ? 2 : 4, head = d.D * size, out = static_cast<int64_t>(d.T) * d.H * head;
-    const void *const from[3] = {q, k, v};
-    for (int i = 0; i < 3; ++i)
-      if (reaches(q_out, out, from[i], strides[i] * size, (i == 0 ? d.H : d.Hk) * head, d.T)) return SSD_ERR_UNSUPPORTED;
-  }
+  if (const ssd_status st = append_args(d, rope, cu_seqlens, seq_lens, page_table, q, k, v, strides, q_out, k_cache, v_cache); st != SSD_OK)
+    return st;
   const ssd::Rope r = {rope->cos, rope->sin, rope->rotary / 2, rope->interleaved};
   return status_of(ssd::launch_attn_append(d, r, cu_seqlens, seq_lens, page_table, q, strides[0], k, k_stride, v, v_stride, q_out,
                                            k_cache, v_cache, static_cast<hipStream_t>(hip_stream)));
+}
+
+ssd_status ssd_attn_append_norm(const ssd_attn_shape *shape, const ssd_rope *rope, const int32_t *cu_seqlens, const int32_t *seq_lens,
+                                const int32_t *page_table, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                const void *v, int64_t v_stride, const float *q_weight, const float *k_weight, float eps,
+                                void *q_out, void *k_cache, void *v_cache, void *hip_stream) {
+  AttnDims d;
+  if (const ssd_status st = make_dims(shape, cu_seqlens != nullptr, &d); st != SSD_OK) return st;
+  if (!ssd::attn_append_norm_fits(d, q != nullptr) || !(eps >= 0.f)) return SSD_ERR_SHAPE;
+  const int64_t strides[3] = {q ? q_stride : static_cast<int64_t>(d.H) * d.D, k_stride, v_stride};
+  if (const ssd_status st = append_args(d, rope, cu_seqlens, seq_lens, page_table, q, k, v, strides, q_out, k_cache, v_cache); st != SSD_OK)
+    return st;
+  if (!k_weight || (q && !q_weight)) return SSD_ERR_NULL;
+  if (!aligned16(k_weight) || !aligned16(q_weight)) return SSD_ERR_ALIGN;
+  const ssd::Rope r = {rope->cos, rope->sin, rope->rotary / 2, rope->interleaved};
+  return status_of(ssd::launch_attn_append_norm(d, r, cu_seqlens, seq_lens, page_table, q, strides[0], k, k_stride, v, v_stride, q_weight,
+                                                k_weight, eps, q_out, k_cache, v_cache, static_cast<hipStream_t>(hip_stream)));
 }
 
 size_t ssd_attn_step_workspace_bytes(const ssd_attn_shape *shape) {

@@ -1,0 +1,269 @@
+// Depthwise causal convolution of a packed batch of prompts of any lengths (or of later pieces of prompts):
+//
+//   z[t][c]  = act( bias[c] + sum_j w[c][j] * window_t[j][c] ),  window_t = the k-1 inputs before token t of its sequence, u_t
+//   cache[q] <- the last k-1 inputs of sequence q                          (channels, k-1)
+//
+// Inputs before a sequence's first token come from its cache, or are zero.  A stream like the batched kernel's, and laid out
+// like it: a thread owns four channels (8 bytes of bf16, 16 of fp32; one channel where an output's width is no multiple of
+// four) and a run of the packed tokens, whatever sequences these belong to, with the window and its weights in registers.  It
+// finds the sequence of its first token once; where the next one begins it fills the window from that one's cache.  Rows of u
+// may be a slice of wider ones, so that the input projection's output need not be copied.
+//
+// The caches are left by threads of their own, one a sequence and channel: in the same launch, or, where they are updated in
+// place, in one behind it (a sequence's first run reads what its last would write).
+#include "ssd_conv.hpp"
+
+namespace ssd {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct VarlenArgs {
+  const void *u;
+  int64_t u_stride;
+  const float *w, *bias;
+  const int32_t *cu;
+  const void *state_in;
+  void *state_out;
+  ConvOut out;
+  int B, T, C, act;
+  int run;                   // tokens a thread
+  unsigned filter_blocks;    // workgroups in front of those that leave the caches
+};
+
+// V neighbouring channels of a row; addresses need no more than the element's alignment.
+template <typename Io, int V>
+struct Row {
+  typename Io::type e[V];
+};
+template <int V>
+struct RowVec;
+template <>
+struct RowVec<2> {
+  typedef u32x2 type __attribute__((aligned(2)));
+};
+template <>
+struct RowVec<4> {
+  typedef f32x4 type __attribute__((aligned(4)));
+};
+template <typename Io, int V>
+__device__ __forceinline__ Row<Io, V> load_row(const typename Io::type *p) {
+  Row<Io, V> r;
+  if constexpr (V == 1) {
+    r.e[0] = *p;
+  } else {
+    static_assert(V == 4, "one channel or four");
+    typedef typename RowVec<sizeof(typename Io::type)>::type Vec;
+    const auto q = __builtin_nontemporal_load(reinterpret_cast<const Vec *>(p));
+    __builtin_memcpy(&r, &q, sizeof(r));
+  }
+  return r;
+}
+template <typename Io>
+__device__ __forceinline__ float to_float(typename Io::type v) {
+  return Io::load(&v, 0);
+}
+
+// The last sequence that begins at or in front of a token (-1: none).  One trip to memory for up to 64 sequences.
+__device__ __forceinline__ int sequence_at(const int32_t *cu, int B, int token) {
+  int last = -1, behind = B;
+  while (behind - last > 1) {
+    const int q = (last + behind) / 2;
+    if (cu[q] <= token) last = q;
+    else behind = q;
+  }
+  return last;
+}
+
+template <typename Io, int K>
+__device__ __forceinline__ void leave_cache(const VarlenArgs &a, int64_t i) {
+  using E = typename Io::type;
+  const int q = static_cast<int>(i / a.C), c = static_cast<int>(i - static_cast<int64_t>(q) * a.C);
+  const int begin = max(a.cu[q], 0), len = max(min(a.cu[q + 1], a.T) - begin, 0);
+  const E *const before = static_cast<const E *>(a.state_in) + (a.state_in ? i * (K - 1) : 0);
+  const E *const u = static_cast<const E *>(a.u) + static_cast<int64_t>(begin) * a.u_stride + c;
+  E keep[K - 1];
+#pragma unroll
+  for (int j = 0; j + 1 < K; ++j) {
+    const int t = len - (K - 1) + j;  // of the sequence's new tokens; negative: cached before
+    if (t >= 0) keep[j] = u[t * a.u_stride];
+    else keep[j] = a.state_in ? before[K - 1 + t] : E(0);
+  }
+  E *const out = static_cast<E *>(a.state_out) + i * (K - 1);
+#pragma unroll
+  for (int j = 0; j + 1 < K; ++j) out[j] = keep[j];
+}
+
+template <typename Io, int K>
+__global__ __launch_bounds__(kConvThreads) void conv_cache_kernel(const VarlenArgs a) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kConvThreads + threadIdx.x;
+  if (i < static_cast<int64_t>(a.B) * a.C) leave_cache<Io, K>(a, i);
+}
+
+template <typename Io, int V, int K>
+__global__ __launch_bounds__(kConvThreads) void conv_varlen_kernel(const VarlenArgs a) {
+  using E = typename Io::type;
+  if (blockIdx.x >= a.filter_blocks) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x - a.filter_blocks) * kConvThreads + threadIdx.x;
+    if (i < static_cast<int64_t>(a.B) * a.C) leave_cache<Io, K>(a, i);
+    return;
+  }
+  const unsigned groups = a.C / V, gid = blockIdx.x * kConvThreads + threadIdx.x;
+  const unsigned run = gid / groups;
+  const int64_t first = static_cast<int64_t>(run) * a.run;
+  if (first >= a.T) return;
+  const int t0 = static_cast<int>(first), t1 = min(a.T, t0 + a.run);
+  const int c0 = static_cast<int>(gid - run * groups) * V;
+  const E *const u = static_cast<const E *>(a.u) + c0;
+  const E *const cached = static_cast<const E *>(a.state_in) + (a.state_in ? static_cast<int64_t>(c0) * (K - 1) : 0);
+
+  constexpr int kBatch = 4;
+  struct Rows {
+    Row<Io, V> r[kBatch];
+  } buf[2];
+  auto request = [&](Rows &r, int tb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) r.r[i] = load_row<Io, V>(u + min(tb + i, t1 - 1) * a.u_stride);  // (surplus ones: the last row)
+  };
+  request(buf[0], t0);
+  float wt[V][K], bs[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) wt[v][j] = a.w[static_cast<int64_t>(c0 + v) * K + j];
+    bs[v] = a.bias ? a.bias[c0 + v] : 0.f;
+  }
+  // the sequence q of token t0 has [begin, end); tokens in front of the first and behind the last one are in none
+  int q = sequence_at(a.cu, a.B, t0), begin = 0, end = t0;
+  float win[K][V];
+  auto fill = [&](int t) __attribute__((always_inline)) {  // win[1 ..]: the inputs in front of token t of sequence q
+#pragma unroll
+    for (int j = 1; j < K; ++j) {
+      const int s = t - K + j;
+      if (s >= begin) {
+        const Row<Io, V> r = load_row<Io, V>(u + s * a.u_stride);
+#pragma unroll
+        for (int v = 0; v < V; ++v) win[j][v] = to_float<Io>(r.e[v]);
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          win[j][v] = a.state_in ? to_float<Io>(cached[(static_cast<int64_t>(q) * a.C + v) * (K - 1) + K - 1 + s - begin]) : 0.f;
+      }
+    }
+  };
+  // `turn`: the next token at which something changes; `inside`: whether the tokens up to it are in a sequence
+  int turn;
+  bool inside;
+  auto enter = [&](int t) __attribute__((always_inline)) {
+    while (q + 1 < a.B && a.cu[q + 1] <= t) ++q;
+    if (q >= 0) {
+      begin = max(a.cu[q], 0);
+      end = min(a.cu[q + 1], a.T);
+    }
+    inside = q >= 0 && t >= begin && t < end;
+    if (inside) fill(t);
+    turn = inside ? end : q + 1 < a.B ? max(a.cu[q + 1], t + 1) : a.T;
+  };
+  enter(t0);
+
+  const int part = c0 >= a.out.begin[2] ? 2 : c0 >= a.out.begin[1] ? 1 : 0;
+  const int width = a.out.begin[part + 1] - a.out.begin[part];
+  E *const z = static_cast<E *>(a.out.ptr[part]) + (c0 - a.out.begin[part]);
+  auto process = [&](const Rows &r, int tb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int t = tb + i;
+      if (t < t1) {
+        if (t >= turn) enter(t);
+#pragma unroll
+        for (int j = 0; j + 1 < K; ++j)
+#pragma unroll
+          for (int v = 0; v < V; ++v) win[j][v] = win[j + 1][v];
+#pragma unroll
+        for (int v = 0; v < V; ++v) win[K - 1][v] = to_float<Io>(r.r[i].e[v]);
+        float s[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          s[v] = bs[v];
+#pragma unroll
+          for (int j = 0; j < K; ++j) s[v] = fmaf(wt[v][j], win[j][v], s[v]);
+          s[v] = act_apply(s[v], a.act);
+        }
+        if (inside) {
+          E *const zp = z + static_cast<int64_t>(t) * width;
+          if constexpr (V == 1) {
+            Io::store(zp, 0, s[0]);
+          } else if constexpr (sizeof(E) == 2) {
+            *reinterpret_cast<u32x2 *>(zp) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+          } else {
+            *reinterpret_cast<f32x4 *>(zp) = f32x4{s[0], s[1], s[2], s[3]};
+          }
+        }
+      }
+    }
+  };
+  for (int tb = t0; tb < t1; tb += 2 * kBatch) {
+    request(buf[1], tb + kBatch);
+    process(buf[0], tb);
+    request(buf[0], tb + 2 * kBatch);
+    process(buf[1], tb + kBatch);
+  }
+}
+
+template <typename Io, int V, int K>
+int resident_blocks() {
+  static const int blocks = [] {
+    int n = 0;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, conv_varlen_kernel<Io, V, K>, kConvThreads, 0) != hipSuccess || n < 1) n = 4;
+    return n;
+  }();
+  return blocks;
+}
+
+template <typename Io, int K>
+hipError_t varlen_typed(VarlenArgs a, bool four, hipStream_t stream) {
+  const int groups = four ? a.C / 4 : a.C;
+  a.run = choose_run(a.T, groups, K, four ? resident_blocks<Io, 4, K>() : resident_blocks<Io, 1, K>());
+  const auto blocks = [](int64_t threads) { return static_cast<unsigned>((threads + kConvThreads - 1) / kConvThreads); };
+  a.filter_blocks = blocks(static_cast<int64_t>((a.T + a.run - 1) / a.run) * groups);
+  const unsigned cache_blocks = a.state_out ? blocks(static_cast<int64_t>(a.B) * a.C) : 0;
+  const bool in_place = a.state_out != nullptr && a.state_out == a.state_in;
+  const dim3 grid(a.filter_blocks + (in_place ? 0 : cache_blocks));
+  if (four)
+    hipLaunchKernelGGL((conv_varlen_kernel<Io, 4, K>), grid, dim3(kConvThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((conv_varlen_kernel<Io, 1, K>), grid, dim3(kConvThreads), 0, stream, a);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess || !in_place) return e;
+  hipLaunchKernelGGL((conv_cache_kernel<Io, K>), dim3(cache_blocks), dim3(kConvThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Whether the threads of a call, one a channel and run or sequence at most, are no more than a launch takes.
+bool conv_varlen_fits(int B, int T, int64_t C) {
+  return (static_cast<int64_t>(T + kRunMin - 1) / kRunMin + B) * C <= (int64_t{1} << 32) - 3 * kConvThreads;
+}
+
+hipError_t launch_conv_varlen(int B, int T, int ksize, bool bf16, const int32_t *cu, const void *u, int64_t u_stride,
+                              const float *w, const float *bias, const void *state_in, void *const z[3], const int width[3],
+                              void *state_out, int act, hipStream_t stream) {
+  VarlenArgs a = {};
+  a.u = u;
+  a.u_stride = u_stride;
+  a.w = w;
+  a.bias = bias;
+  a.cu = cu;
+  a.state_in = state_in;
+  a.state_out = state_out;
+  a.out = make_out(z, width);
+  a.B = B;
+  a.T = T;
+  a.C = a.out.begin[3];
+  a.act = act;
+  const bool four = width[0] % 4 == 0 && width[1] % 4 == 0 && width[2] % 4 == 0;
+  SSD_CONV_DISPATCH(varlen_typed, a, four, stream)
+}
+
+}  // namespace ssd

@@ -240,6 +240,11 @@ hipError_t launch_prefill_mfma_varlen(const Dims &d, const int32_t *cu_seqlens, 
 hipError_t launch_conv_prefill(int Bt, int T, int ksize, bool bf16, const void *u, const float *w, const float *bias,
                                const void *state_in, void *const z[3], const int width[3], void *state_out, int act,
                                hipStream_t stream);
+// ... of a packed batch: B sequences whose boundaries are on the device; rows of u u_stride elements apart.
+bool conv_varlen_fits(int B, int T, int64_t C);
+hipError_t launch_conv_varlen(int B, int T, int ksize, bool bf16, const int32_t *cu, const void *u, int64_t u_stride,
+                              const float *w, const float *bias, const void *state_in, void *const z[3], const int width[3],
+                              void *state_out, int act, hipStream_t stream);
 hipError_t launch_conv_step(int Bt, int ksize, bool bf16, void *state, const void *u, const float *w, const float *bias,
                             void *const z[3], const int width[3], int act, hipStream_t stream);
 

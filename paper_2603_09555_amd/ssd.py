@@ -22,9 +22,10 @@ SSD_OK = 0
 
 EXPORTS = ["ssd_prefill_workspace_bytes", "ssd_prefill", "ssd_prefill_static", "ssd_decode_step", "ssd_decode_step_layers",
            "ssd_decode_steps_layers", "ssd_prefill_varlen_workspace_bytes", "ssd_prefill_varlen",
-           "ssd_conv1d_prefill", "ssd_conv1d_step", "ssd_prefill_dt", "ssd_prefill_varlen_dt",
+           "ssd_conv1d_prefill", "ssd_conv1d_varlen", "ssd_conv1d_step", "ssd_prefill_dt", "ssd_prefill_varlen_dt",
            "ssd_decode_step_layers_dt", "ssd_decode_steps_layers_dt",
-           "ssd_norm_gated", "ssd_norm_residual", "ssd_attn_append", "ssd_attn_step", "ssd_attn_step_workspace_bytes",
+           "ssd_selective_prefill", "ssd_selective_prefill_workspace_bytes", "ssd_selective_step",
+           "ssd_norm_gated", "ssd_norm_residual", "ssd_attn_append", "ssd_attn_append_norm", "ssd_attn_step", "ssd_attn_step_workspace_bytes",
            "ssd_attn_prefill", "ssd_attn_prefill_workspace_bytes",
            "ssd_prefill_path", "ssd_status_string", "ssd_version",
            "ssd_testing_set_knob", "ssd_testing_reset_knobs", "ssd_testing_prefill_plan", "ssd_testing_varlen_plan",
@@ -44,6 +45,10 @@ class ssd_attn_shape(ctypes.Structure):
 class ssd_rope(ctypes.Structure):
     _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("rotary", ctypes.c_int32), ("positions", ctypes.c_int32),
                 ("interleaved", ctypes.c_int32)]
+
+
+class ssd_selective_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "tokens", "channels", "dstate", "io_dtype", "dt_dtype")]
 
 
 class SSDError(RuntimeError):
@@ -113,6 +118,17 @@ _lib.ssd_norm_residual.restype = ctypes.c_int
 _lib.ssd_norm_residual.argtypes = [_i64, _i32, _i32, _i32, _vp, _vp, _f32, _vp, _f32, _vp, _vp, _vp]
 _lib.ssd_attn_append.restype = ctypes.c_int
 _lib.ssd_attn_append.argtypes = [_ap, ctypes.POINTER(ssd_rope), _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp]
+_lib.ssd_attn_append_norm.restype = ctypes.c_int
+_lib.ssd_attn_append_norm.argtypes = _lib.ssd_attn_append.argtypes[:11] + [_vp, _vp, _f32] + [_vp] * 4
+_lib.ssd_conv1d_varlen.restype = ctypes.c_int
+_lib.ssd_conv1d_varlen.argtypes = [_i32, _i32, _i32, _i32, ctypes.POINTER(_i32), _vp, _vp, _i64] + [_vp] * 7 + [_i32, _vp]
+_ssp = ctypes.POINTER(ssd_selective_shape)
+_lib.ssd_selective_prefill_workspace_bytes.restype = _sz
+_lib.ssd_selective_prefill_workspace_bytes.argtypes = [_ssp]
+_lib.ssd_selective_prefill.restype = ctypes.c_int
+_lib.ssd_selective_prefill.argtypes = [_ssp, ctypes.POINTER(ssd_dt_transform)] + [_vp] * 5 + [_i64, _vp, _i64, _vp, _vp, _i64] + [_vp] * 4 + [_sz, _vp]
+_lib.ssd_selective_step.restype = ctypes.c_int
+_lib.ssd_selective_step.argtypes = [_ssp, ctypes.POINTER(ssd_dt_transform)] + [_vp] * 5 + [_i64, _vp, _i64, _vp, _vp, _i64] + [_vp] * 2
 for _name in ("ssd_attn_step_workspace_bytes", "ssd_attn_prefill_workspace_bytes"):
     getattr(_lib, _name).restype = _sz
     getattr(_lib, _name).argtypes = [_ap]
@@ -138,6 +154,9 @@ try:
     _native.init_block([ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in
                         ("ssd_norm_gated", "ssd_norm_residual", "ssd_attn_append", "ssd_attn_step_workspace_bytes", "ssd_attn_step",
                          "ssd_attn_prefill_workspace_bytes", "ssd_attn_prefill")])
+    _native.init_mixer([ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in
+                        ("ssd_conv1d_varlen", "ssd_selective_prefill_workspace_bytes", "ssd_selective_prefill", "ssd_selective_step",
+                         "ssd_attn_append_norm")])
 except ImportError as e:
     warnings.warn("_ssd_binding.so is missing or does not fit, calls go through Python (some 5 us more host time each): build it "
                   "with `python -m paper_2603_09555_amd.build` (%s)" % e, RuntimeWarning)
@@ -146,6 +165,7 @@ except ImportError as e:
         """Leaves every call to the Python below."""
         prefill = prefill_varlen = decode_step = decode_step_layers = decode_steps_layers = conv1d_prefill = conv1d_step = \
             norm_gated = norm_residual = attn_append = attn_step = attn_prefill = \
+            conv1d_varlen = selective_prefill = selective_step = attn_append_norm = \
             staticmethod(lambda *args: None)
 
 
@@ -492,6 +512,150 @@ def ssd_conv1d_step(conv_state, u, weight, bias=None, split=None, activation="si
     return [o for o in outs if o is not None]
 
 
+def _check_here(*ts):
+    """Device tensors of the current device, on whose current stream the call goes."""
+    here = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+    for t in ts:
+        if t is not None and not (t.is_cuda and t.get_device() == here):
+            raise ValueError("tensors must be on the current device")
+
+
+def _row_stride(t, tokens, width):
+    """Elements between the rows of ``t (tokens,width)``, which are dense."""
+    if t.dim() != 2 or t.shape != (tokens, width):
+        raise ValueError("inconsistent tensor shapes")
+    if (width > 1 and t.stride(1) != 1) or (tokens > 1 and t.stride(0) < width):
+        raise ValueError("rows must be dense and must not overlap")
+    return t.stride(0) if tokens > 1 else width
+
+
+def ssd_conv1d_varlen(u, weight, bias, cu_seqlens, conv_state=None, split=None, activation="silu", outs=None, conv_state_out=None):
+    """``ssd_conv1d_varlen``: the convolution of a packed batch of sequences, ``u (tokens,C)``, which may be a slice of wider rows,
+    sequence q's tokens being ``cu_seqlens[q]`` to ``cu_seqlens[q+1]`` (int32, on the device).  ``conv_state (nseq,C,k-1)`` holds
+    their cached inputs, or is None (zeros); ``conv_state_out`` may be it.  Otherwise as ``ssd_conv1d_prefill``: returns
+    ``(outputs, new_conv_state)``, the outputs being ``outs`` if given."""
+    out = _native.conv1d_varlen(u, weight, bias, cu_seqlens, conv_state, split, activation, outs, conv_state_out)
+    if out is not None:
+        return _done(out, "ssd_conv1d_varlen")
+    tokens, C = u.shape
+    k = weight.shape[1]
+    nseq = cu_seqlens.numel() - 1
+    split = _conv_split(C, split)
+    _check_sizes(nseq, tokens, C)
+    io = _IO_DTYPES.get(u.dtype, -1)
+    state_shape = (nseq, C, k - 1)
+    if cu_seqlens.dtype != torch.int32 or nseq < 1:
+        raise ValueError("cu_seqlens must hold nseq + 1 int32 values")
+    if weight.dtype != torch.float32 or weight.shape != (C, k) or (bias is not None and (bias.dtype != torch.float32 or bias.shape != (C,))) \
+            or (conv_state is not None and (conv_state.dtype != u.dtype or conv_state.shape != state_shape)):
+        raise ValueError("inconsistent tensor shapes or dtypes")
+    stride = _row_stride(u, tokens, C)
+    wide = [w for w in split if w > 0]
+    if outs is None:
+        outs = [u.new_empty((tokens, w)) for w in wide]
+    elif len(outs) != len(wide):
+        raise ValueError("an output for every width of split that is not 0")
+    for o, w in zip(outs, wide):
+        _check_output(o, u.dtype, tokens * w)
+    _check_output(conv_state_out, u.dtype, nseq * C * (k - 1))
+    if conv_state_out is None:
+        conv_state_out = u.new_empty(state_shape)
+    _check_dev(weight, bias, cu_seqlens, conv_state, conv_state_out, *outs)
+    _check_here(u, weight, bias, cu_seqlens, conv_state, conv_state_out, *outs)
+    left = iter(outs)
+    z = [_ptr(next(left)) if w > 0 else None for w in split]
+    st = _lib.ssd_conv1d_varlen(nseq, tokens, k, io, _I32x3(*split), _ptr(cu_seqlens), _ptr(u), stride, _ptr(weight), _ptr(bias),
+                                _ptr(conv_state), *z, _ptr(conv_state_out), _ACTIVATIONS[activation], _stream_ptr())
+    if st != SSD_OK:
+        raise SSDError(st, "ssd_conv1d_varlen")
+    return outs, conv_state_out
+
+
+def make_selective_shape(batch, tokens, channels, dstate, io_dtype, dt_dtype=None) -> ssd_selective_shape:
+    """The ``ssd_selective_shape`` of a call; ``dt_dtype`` is ``io_dtype`` unless given."""
+    _check_sizes(batch, tokens, channels, dstate)
+    io = _IO_DTYPES.get(io_dtype, -1)
+    return ssd_selective_shape(batch, tokens, channels, dstate, io, io if dt_dtype is None else _IO_DTYPES.get(dt_dtype, -1))
+
+
+def selective_prefill_workspace_bytes(shape: ssd_selective_shape) -> int:
+    return int(_lib.ssd_selective_prefill_workspace_bytes(ctypes.byref(shape)))
+
+
+def _selective(x, dt, A, B, C, D, z, batch):
+    """The checks that both selective calls share.  Returns shape and strides of B, C and z."""
+    tokens, channels = x.shape
+    dstate = A.shape[1] if A.dim() == 2 else -1
+    if dt.shape != x.shape or A.shape != (channels, dstate) or (D is not None and D.shape != (channels,)):
+        raise ValueError("inconsistent tensor shapes")
+    if B.dtype != x.dtype or C.dtype != x.dtype or (z is not None and z.dtype != x.dtype) or A.dtype != torch.float32 \
+            or (D is not None and D.dtype != torch.float32):
+        raise ValueError("x, B, C and z must share one dtype; A and D must be fp32")
+    strides = [_row_stride(t, tokens, dstate) for t in (B, C)] + [_row_stride(z, tokens, channels) if z is not None else 0]
+    _check_dev(x, dt, A, D)
+    _check_here(x, dt, A, B, C, D, z)
+    return make_selective_shape(batch, tokens, channels, dstate, x.dtype, dt.dtype), strides
+
+
+def ssd_selective_prefill(x, dt, A, B, C, D, cu_seqlens, z=None, h0=None, y=None, final_state=None, workspace=None,
+                          dt_bias=None, dt_softplus=False, dt_limit=None):
+    """``ssd_selective_prefill``: the selective scan of a packed batch of sequences, ``x (tokens,channels)`` in fp32 or bf16, sequence
+    q's tokens being ``cu_seqlens[q]`` to ``cu_seqlens[q+1]`` (int32, on the device).  ``dt (tokens,channels)`` in fp32 or the type
+    of ``x``, ``A (channels,dstate)`` fp32, ``B, C (tokens,dstate)`` like ``x``, ``D (channels)`` fp32 or None, ``z`` the gate like
+    ``x`` or None; ``B``, ``C`` and ``z`` may be slices of wider rows.  ``h0 (nseq,channels,dstate)`` fp32 or None, which
+    ``final_state`` may be.  ``dt_bias (channels)``, ``dt_softplus``, ``dt_limit``: as for ``ssd_prefill``.  Returns
+    ``(y, final_state)``."""
+    out = _native.selective_prefill(x, dt, A, B, C, D, cu_seqlens, z, h0, y, final_state, workspace, dt_bias, dt_softplus, dt_limit)
+    if out is not None:
+        return _done(out, "ssd_selective_prefill")
+    nseq = cu_seqlens.numel() - 1
+    if cu_seqlens.dtype != torch.int32 or nseq < 1:
+        raise ValueError("cu_seqlens must hold nseq + 1 int32 values")
+    shape, strides = _selective(x, dt, A, B, C, D, z, nseq)
+    state_shape = (nseq, shape.channels, shape.dstate)
+    if h0 is not None and (h0.dtype != torch.float32 or h0.shape != state_shape):
+        raise ValueError("h0 must be fp32 of shape %s" % (state_shape,))
+    _check_output(y, x.dtype, x.numel())
+    _check_output(final_state, torch.float32, nseq * shape.channels * shape.dstate)
+    if y is None:
+        y = torch.empty_like(x)
+    if final_state is None:
+        final_state = torch.empty(state_shape, dtype=torch.float32, device=x.device)
+    if workspace is None:
+        workspace = torch.empty((max(selective_prefill_workspace_bytes(shape), 256),), dtype=torch.uint8, device=x.device)
+    xf = _dt_transform(dt_bias, dt_softplus, dt_limit, (shape.channels,))
+    _check_dev(cu_seqlens, h0, y, final_state, workspace)
+    _check_here(cu_seqlens, h0, y, final_state, workspace, dt_bias)
+    st = _lib.ssd_selective_prefill(ctypes.byref(shape), None if xf is None else ctypes.byref(xf), _ptr(cu_seqlens), _ptr(x), _ptr(dt), _ptr(A),
+                                    _ptr(B), strides[0], _ptr(C), strides[1], _ptr(D), _ptr(z), strides[2], _ptr(h0), _ptr(y),
+                                    _ptr(final_state), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr())
+    if st != SSD_OK:
+        raise SSDError(st, "ssd_selective_prefill")
+    return y, final_state
+
+
+def ssd_selective_step(state, x, dt, A, B, C, D, z=None, y=None, dt_bias=None, dt_softplus=False, dt_limit=None):
+    """``ssd_selective_step``: one token of each sequence, ``x (batch,channels)``; updates ``state (batch,channels,dstate)`` in place.
+    The other arguments are those of ``ssd_selective_prefill``.  Returns ``y`` like ``x``."""
+    out = _native.selective_step(state, x, dt, A, B, C, D, z, y, dt_bias, dt_softplus, dt_limit)
+    if out is not None:
+        return _done(out, "ssd_selective_step")
+    shape, strides = _selective(x, dt, A, B, C, D, z, x.shape[0])
+    if state.dtype != torch.float32 or state.shape != (shape.batch, shape.channels, shape.dstate):
+        raise ValueError("state must be fp32 of shape (batch, channels, dstate)")
+    _check_output(y, x.dtype, x.numel())
+    if y is None:
+        y = torch.empty_like(x)
+    xf = _dt_transform(dt_bias, dt_softplus, dt_limit, (shape.channels,))
+    _check_dev(state, y)
+    _check_here(state, y, dt_bias)
+    st = _lib.ssd_selective_step(ctypes.byref(shape), None if xf is None else ctypes.byref(xf), _ptr(state), _ptr(x), _ptr(dt), _ptr(A), _ptr(B),
+                                 strides[0], _ptr(C), strides[1], _ptr(D), _ptr(z), strides[2], _ptr(y), _stream_ptr())
+    if st != SSD_OK:
+        raise SSDError(st, "ssd_selective_step")
+    return y
+
+
 def ssd_norm_gated(y, z, weight, eps=1e-5, groups=1, norm_first=False, out=None):
     """``ssd_norm_gated``: ``y (rows,width)`` and its gate ``z (rows,width)`` in fp32 or bf16, ``weight (width)`` fp32.  ``z`` may
     be a slice of wider rows.  Each of ``groups`` ranges of a row is normalised by itself, ``y * silu(z)`` or, with
@@ -586,6 +750,23 @@ def ssd_attn_append(q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens=
     out = _native.attn_append(q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved, q_out)
     if out is not None:
         return None if out is False else _done(out, "ssd_attn_append")
+    return _append("ssd_attn_append", q, k, v, None, k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved, q_out)
+
+
+def ssd_attn_append_norm(q, k, v, q_weight, k_weight, k_cache, v_cache, page_table, seq_lens, cu_seqlens=None, rope=None, interleaved=False,
+                         eps=1e-5, q_out=None):
+    """``ssd_attn_append_norm``: ``ssd_attn_append`` with heads of queries and keys normalised in front of the rotation,
+    ``v * rsqrt(mean(v ** 2) + eps) * weight`` over their ``headdim`` values; ``q_weight, k_weight (headdim)`` fp32 (``q_weight`` is None
+    without ``q``)."""
+    out = _native.attn_append_norm(q, k, v, q_weight, k_weight, k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved, eps, q_out)
+    if out is not None:
+        return None if out is False else _done(out, "ssd_attn_append_norm")
+    return _append("ssd_attn_append_norm", q, k, v, (q_weight, k_weight, eps), k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved,
+                   q_out)
+
+
+def _append(where, q, k, v, norm, k_cache, v_cache, page_table, seq_lens, cu_seqlens, rope, interleaved, q_out):
+    """Either call that appends; ``norm``: weights of queries and of keys, and eps, or None."""
     tokens, nkv, D = k.shape
     if v.shape != k.shape or v.dtype != k.dtype or (q is not None and (q.dtype != k.dtype or q.dim() != 3 or q.shape[0] != tokens or q.shape[2] != D)):
         raise ValueError("q, k and v must share one dtype, and agree in tokens and headdim")
@@ -611,11 +792,20 @@ def ssd_attn_append(q, k, v, k_cache, v_cache, page_table, seq_lens, cu_seqlens=
     elif q_out is not None:
         raise ValueError("q_out without q")
     shape = make_attn_shape(page_table.shape[0], tokens, heads, k_cache, page_table)
-    st = _lib.ssd_attn_append(ctypes.byref(shape), ctypes.byref(xr), _ptr(cu_seqlens), _ptr(seq_lens), _ptr(page_table), _ptr(q), q_stride,
-                              _ptr(k), _token_stride(k, nkv, D), _ptr(v), _token_stride(v, nkv, D), _ptr(q_out), _ptr(k_cache),
-                              _ptr(v_cache), _stream_ptr())
+    args = (ctypes.byref(shape), ctypes.byref(xr), _ptr(cu_seqlens), _ptr(seq_lens), _ptr(page_table), _ptr(q), q_stride, _ptr(k),
+            _token_stride(k, nkv, D), _ptr(v), _token_stride(v, nkv, D))
+    tail = (_ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream_ptr())
+    if norm is None:
+        st = _lib.ssd_attn_append(*args, *tail)
+    else:
+        q_weight, k_weight, eps = norm
+        if (q_weight is None) != (q is None) or any(t is not None and (t.dtype != torch.float32 or t.shape != (D,)) for t in (q_weight, k_weight)):
+            raise ValueError("weights of the heads' norms must be fp32 of shape (headdim,), that of the queries as the queries are there")
+        _check_dev(q_weight, k_weight)
+        _check_here(q, k, v, q_weight, k_weight, k_cache, v_cache, page_table, seq_lens, cu_seqlens, q_out, *(rope or ()))
+        st = _lib.ssd_attn_append_norm(*args, _ptr(q_weight), _ptr(k_weight), eps, *tail)
     if st != SSD_OK:
-        raise SSDError(st, "ssd_attn_append")
+        raise SSDError(st, where)
     return q_out
 
 
