@@ -134,6 +134,7 @@ struct Knobs {
   int deal = 0;            // packed bf16 batches: 1 items dealt to the scan's workgroups, 2 an entry each; 0: library's choice
   int split_images = 0;    // fp32 prefill on split operands: 2 no images of blocks; 0: library's choice
   int chunk = 0;           // bf16 prefill by chunk kernels: 1 wherever they can run, 2 never; 0: library's choice
+  int selective_segment = 0;  // > 0: tokens per segment of the selective scan, if the workspace has room for so many segments
   int fold_max_slots = 3;  // most state slots a segment sums by itself instead of a pass over segment states (0: never)
 };
 Knobs &knobs();

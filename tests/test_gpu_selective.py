@@ -101,7 +101,20 @@ def test_long_prompts_of_few_channels(ssd, io, aligned):
     """Many segments, that begin and end anywhere in sequences."""
     for i, lengths in enumerate(([1500], [700, 1, 0, 900, 2], [3] * 200 + [800])):
         print("selective", io, aligned, lengths[:5], flush=True)
-        compare(ssd, make(lengths, 70, 16, io, seed=20 + i, pad=(2, 2) if aligned else (1, 2)), io)
+        s = make(lengths, 70, 16, io, seed=20 + i, pad=(2, 2) if aligned else (1, 2))
+        compare(ssd, s, io)
+        for segment in (200, 10000):
+            ssd.set_knob("selective_segment", segment)
+            compare(ssd, s, io)
+        ssd.reset_knobs()
+
+
+@pytest.mark.parametrize("C,N", [(4000, 16), (1000, 16), (900, 6), (700, 30), (400, 60), (130, 256)])
+def test_every_cut(ssd, C, N):
+    """More or fewer states a wave, by how much work there is."""
+    for tokens in (81, 330):
+        print("selective", C, N, tokens, flush=True)
+        compare(ssd, make([tokens - 20, 0, 20], C, N, "bf16", seed=C + N), "bf16")
 
 
 def test_decays_of_every_size(ssd):
