@@ -343,7 +343,7 @@ SSD_API ssd_status ssd_conv1d_step(int32_t batch, int32_t ksize, int32_t io_dtyp
  *                     must not overlap it otherwise.  A sequence without a token keeps
  *                     its cache
  * Everything else, and every bit of the outputs, is as for ssd_conv1d_prefill of
- * each sequence by itself.  A call of 2^32 threads or more (one a channel and 16
+ * each sequence by itself.  A call of 2^32 threads or more (one a channel and four
  * tokens, or a channel and sequence, at most) is refused with SSD_ERR_SHAPE.
  * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _HIP.
  */
@@ -545,7 +545,7 @@ SSD_API ssd_status ssd_attn_append(const ssd_attn_shape *shape, const ssd_rope *
  *   q_weight, k_weight  (headdim) fp32, 16-byte aligned; q_weight may be NULL if q is
  *   eps               >= 0
  * Everything else is as for ssd_attn_append, but for the sizes that are refused with
- * SSD_ERR_SHAPE: none below 2^24 tokens and 2^27 tokens times heads (of queries, keys
+ * SSD_ERR_SHAPE: none below 2^24 tokens and 2^26 tokens times heads (of queries, keys
  * and values).
  */
 SSD_API ssd_status ssd_attn_append_norm(const ssd_attn_shape *shape, const ssd_rope *rope, const int32_t *cu_seqlens,

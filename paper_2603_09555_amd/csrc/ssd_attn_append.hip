@@ -18,6 +18,8 @@ namespace ssd {
 namespace {
 
 constexpr int kBatch = 2;        // tokens whose pieces a thread has on their way at a time
+constexpr int kMostTokens = 4;   // a workgroup
+constexpr int kFewWorkgroups = 2048;  // more take several tokens each
 
 struct AppendArgs {
   const void *src[3];      // q, k, v
@@ -31,6 +33,11 @@ struct AppendArgs {
   int row_pieces;          // pieces of a token: queries (if any), keys, values
   int q_heads;             // 0: no queries
   int run;                 // tokens a workgroup
+};
+
+struct Place {
+  int pos;       // < 0: none
+  int64_t slot;  // cache row of key head 0, or -1
 };
 
 // kWhole: pieces lie in one half of the pairs (interleaved pairs: in the rotated part) or outside it.

@@ -8,14 +8,6 @@ namespace {
 
 using namespace block;
 
-constexpr int kMostTokens = 4;   // a workgroup
-constexpr int kFewWorkgroups = 2048;  // more take several tokens each
-
-struct Place {
-  int pos;       // < 0: none
-  int64_t slot;  // cache row of key head 0, or -1
-};
-
 template <bool kBf16>
 using Element = typename std::conditional<kBf16, uint16_t, float>::type;
 __device__ __forceinline__ float value(float v) { return v; }

@@ -6,15 +6,20 @@
 //   key, value  ->  page table[b][p / page_size], slot p % page_size;  rounded once
 //
 // A copy in effect, like the append without norms.  A head is held by as many neighbouring lanes as it has pieces of 16 bytes
-// (rounded up to a power of two), so that the sum of its squares stays within a wave; a thread's piece of the head vector, and
-// with it its weights, are the same for all its tokens.  A piece that holds one half of its pairs brings the other halves'
-// piece with it, which a lane nearby brings too, from the first-level cache.
+// (rounded up to a power of two), so that the sum of its squares stays within a wave.  A wave takes some heads of one token, all of
+// them queries, or keys, or values, 64 pieces at a time: what a lane needs beside its piece -- its weights, and the cosines and sines
+// of its pairs, which are four times the piece -- is the same for all its heads and asked for once.  A piece that holds one half of its
+// pairs brings the other halves' piece with it, which a lane nearby brings too, from the first-level cache.
 #include <algorithm>
 
 #include "ssd_attn_append.hpp"
 
 namespace ssd {
 namespace {
+
+constexpr int kBatch = 2;          // heads whose pieces a lane has on their way at a time
+constexpr int kMostTurns = 8;      // heads a lane
+constexpr int64_t kWaves = 4096;  // from twice as many on lanes take several heads
 
 struct AppendNormArgs {
   const void *src[3];      // q, k, v
@@ -26,127 +31,138 @@ struct AppendNormArgs {
   Rope rope;
   float eps, inv_headdim;
   int lg_lanes;            // lanes a head: 2^lg_lanes
-  int q_heads;             // 0: no queries
-  int run;                 // tokens a workgroup
+  int turns;               // heads a lane, at most
+  int units[2], all_units; // waves that a token's queries take (none: 0), its keys or its values; all of them
+  uint32_t inv_all_units;
 };
+
+// The sum over the 2^lg neighbouring lanes of a head, in all of them.  Within a row of 16 without LDS: neighbours, pairs, halves
+// and rows mirrored, in each of which every group of lanes has its sum already.
+template <int kControl>
+__device__ __forceinline__ float moved(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), kControl, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float sum_of_head(float v, int lg) {
+  if (lg > 0) v += moved<0xb1>(v);   // lanes 1 0 3 2
+  if (lg > 1) v += moved<0x4e>(v);   // lanes 2 3 0 1
+  if (lg > 2) v += moved<0x141>(v);  // 7 .. 0
+  if (lg > 3) v += moved<0x140>(v);  // 15 .. 0
+  if (lg > 4) v += __shfl_xor(v, 16);
+  if (lg > 5) v += __shfl_xor(v, 32);
+  return v;
+}
 
 // kWhole: pieces lie in one half of the pairs (interleaved pairs: in the rotated part) or outside it.
 template <bool kBf16, bool kWhole>
 __global__ __launch_bounds__(256) void append_norm_kernel(const AppendNormArgs a) {
   using E = Element<kBf16>;
   constexpr int W = 16 / sizeof(E);
-  __shared__ Place place[kMostTokens];
-  const int first_token = blockIdx.x * a.run, tokens = min(a.run, a.d.T - first_token);
-  if (static_cast<int>(threadIdx.x) < tokens) {
-    const Token t = find_token(a.d, a.cu, a.lens, first_token + threadIdx.x);
-    place[threadIdx.x] = {t.pos, t.pos < 0 ? -1 : slot_of(a.d, a.table, t.seq, t.pos, 0)};
-  }
-  __syncthreads();
-  // this thread's head -- of q, k or v -- and its piece's first value; lanes of a head enter and leave together
-  const int lanes = 1 << a.lg_lanes;
-  int head = static_cast<int>((blockIdx.y * 256 + threadIdx.x) >> a.lg_lanes), what = 0;
-  const int first = (static_cast<int>(threadIdx.x) & (lanes - 1)) * W;
-  if (head >= a.q_heads + 2 * a.d.Hk) return;
-  if (head >= a.q_heads) {
-    head -= a.q_heads;
+  // this wave's token, and which heads of what
+  const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int token = quotient(wave, a.all_units, a.inv_all_units);
+  if (token >= a.d.T) return;
+  int unit = wave - token * a.all_units, what = 0;
+  if (unit >= a.units[0]) {
+    unit -= a.units[0];
     what = 1;
-    if (head >= a.d.Hk) {
-      head -= a.d.Hk;
+    if (unit >= a.units[1]) {
+      unit -= a.units[1];
       what = 2;
     }
   }
+  const Token t = find_token(a.d, a.cu, a.lens, token);
+  if (t.pos < 0) return;
+  const int64_t slot = what == 0 ? 0 : slot_of(a.d, a.table, t.seq, t.pos, 0);  // cache row of key head 0
+  if (slot < 0) return;
+  const int heads = what == 0 ? a.d.H : a.d.Hk, at_once = 64 >> a.lg_lanes;
+  const int first_head = unit * a.turns * at_once + (lane >> a.lg_lanes), first = (lane & ((1 << a.lg_lanes) - 1)) * W;
   const bool piece = first < a.d.D;  // (the others only take part in the sum)
-  const int64_t stride = a.stride[what];
-  const E *const src = static_cast<const E *>(a.src[what]) + first_token * stride + static_cast<int64_t>(head) * a.d.D;
-  E *const out = what == 0 ? static_cast<E *>(a.q_out) + (static_cast<int64_t>(first_token) * a.d.H + head) * a.d.D + first
-                           : static_cast<E *>(a.cache[what - 1]) + (static_cast<int64_t>(head) << a.d.lg_page) * a.d.D + first;
-  const int64_t out_stride = static_cast<int64_t>(a.d.H) * a.d.D;
+  const E *const src = static_cast<const E *>(a.src[what]) + token * a.stride[what];
+  E *const out = what == 0 ? static_cast<E *>(a.q_out) + static_cast<int64_t>(token) * a.d.H * a.d.D : static_cast<E *>(a.cache[what - 1]) + slot * a.d.D;
+  const int64_t out_stride = what == 0 ? a.d.D : static_cast<int64_t>(a.d.D) << a.d.lg_page;  // between heads
   const int half = a.rope.half;
   const bool rotated = what < 2 && first < 2 * half && piece, second = !a.rope.interleaved && first >= half;
   const bool split = kWhole && rotated && !a.rope.interleaved;  // pairs with another piece
   const int partner = second ? first - half : first + half, pair = a.rope.interleaved ? first / 2 : second ? first - half : first;
+  const int64_t angles = static_cast<int64_t>(t.pos) * half;
   const float *const weight = a.weight[what == 0 ? 0 : 1];
-  float w[W], wp[W];
+  // weights, cosines, and sines as they join: the other one's weight with them, and their sign
+  float w[W], cs[W], sn[W];
 #pragma unroll
-  for (int i = 0; i < W; ++i) w[i] = wp[i] = 0.f;
+  for (int i = 0; i < W; ++i) w[i] = cs[i] = sn[i] = 0.f;
   if (what < 2 && piece) {
     load_rope<W>(weight + first, w);
-    if (split) load_rope<W>(weight + partner, wp);
-  }
-  u32x4 q[kMostTokens], other[kMostTokens];
-  Place at[kMostTokens];
+    if (split) {
+      float wp[W];
+      load_rope<W>(weight + partner, wp);
+      load_rope<W>(a.rope.cos + angles + pair, cs);
+      load_rope<W>(a.rope.sin + angles + pair, sn);
 #pragma unroll
-  for (int k = 0; k < kMostTokens; ++k) {
-    at[k].pos = -1;
-    q[k] = other[k] = u32x4{0u, 0u, 0u, 0u};
-    if (k >= tokens) continue;
-    at[k] = place[k];
-    if (at[k].pos < 0 || (what > 0 && at[k].slot < 0)) {
-      at[k].pos = -1;
-      continue;
+      for (int i = 0; i < W; ++i) sn[i] = second ? sn[i] * wp[i] : -sn[i] * wp[i];
+    } else if (kWhole && rotated) {
+      load_rope<W / 2>(a.rope.cos + angles + pair, cs);
+      load_rope<W / 2>(a.rope.sin + angles + pair, sn);
     }
-    const E *const row = src + k * stride;
-    if (piece) q[k] = *reinterpret_cast<const u32x4 *>(row + first);
-    if (split) other[k] = *reinterpret_cast<const u32x4 *>(row + partner);
   }
+  for (int turn = 0; turn < a.turns; turn += kBatch) {
+    u32x4 q[kBatch], other[kBatch];
+    int head[kBatch];
 #pragma unroll
-  for (int k = 0; k < kMostTokens; ++k) {
-    if (at[k].pos < 0) continue;  // (alike for the lanes of a head)
-    if (what < 2) {
-      float v[W], r[W];
-      unpack<kBf16>(q[k], v);
-      float sum = 0.f;
+    for (int k = 0; k < kBatch; ++k) {
+      head[k] = turn + k < a.turns ? first_head + (turn + k) * at_once : heads;
+      q[k] = other[k] = u32x4{0u, 0u, 0u, 0u};
+      if (head[k] >= heads || !piece) continue;
+      const E *const row = src + static_cast<int64_t>(head[k]) * a.d.D;
+      q[k] = *reinterpret_cast<const u32x4 *>(row + first);
+      if (split) other[k] = *reinterpret_cast<const u32x4 *>(row + partner);
+    }
 #pragma unroll
-      for (int i = 0; i < W; ++i) sum = fmaf(v[i], v[i], sum);
-      for (int m = 1; m < lanes; m <<= 1) sum += __shfl_xor(sum, m);
-      const float scale = 1.f / sqrtf(fmaf(sum, a.inv_headdim, a.eps));
+    for (int k = 0; k < kBatch; ++k) {
+      if (head[k] >= heads) continue;  // (alike for the lanes of a head)
+      if (what < 2) {
+        float v[W], r[W];
+        unpack<kBf16>(q[k], v);
+        float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < W; ++i) r[i] = v[i] = v[i] * scale * w[i];
-      if (rotated) {
-        const float *const cs = a.rope.cos + static_cast<int64_t>(at[k].pos) * half, *const sn = a.rope.sin + static_cast<int64_t>(at[k].pos) * half;
+        for (int i = 0; i < W; ++i) sum = fmaf(v[i], v[i], sum);
+        const float scale = __builtin_amdgcn_rsqf(fmaf(sum_of_head(sum, a.lg_lanes), a.inv_headdim, a.eps));
+#pragma unroll
+        for (int i = 0; i < W; ++i) r[i] = v[i] = v[i] * scale * w[i];
         if (split) {
-          float o[W], c[W], s[W];
+          float o[W];
           unpack<kBf16>(other[k], o);
-          load_rope<W>(cs + pair, c);
-          load_rope<W>(sn + pair, s);
 #pragma unroll
-          for (int i = 0; i < W; ++i) {
-            const float u = o[i] * scale * wp[i];
-            r[i] = fmaf(v[i], c[i], second ? u * s[i] : -u * s[i]);
-          }
-        } else if (kWhole) {
-          float c[W / 2], s[W / 2];
-          load_rope<W / 2>(cs + pair, c);
-          load_rope<W / 2>(sn + pair, s);
+          for (int i = 0; i < W; ++i) r[i] = fmaf(v[i], cs[i], o[i] * scale * sn[i]);
+        } else if (kWhole && rotated) {
 #pragma unroll
           for (int i = 0; i < W; i += 2) {
-            r[i] = fmaf(v[i], c[i / 2], -v[i + 1] * s[i / 2]);
-            r[i + 1] = fmaf(v[i + 1], c[i / 2], v[i] * s[i / 2]);
+            r[i] = fmaf(v[i], cs[i / 2], -v[i + 1] * sn[i / 2]);
+            r[i + 1] = fmaf(v[i + 1], cs[i / 2], v[i] * sn[i / 2]);
           }
-        } else {
-          const E *const row = src + k * stride;
+        } else if (rotated) {
+          const E *const row = src + static_cast<int64_t>(head[k]) * a.d.D;
 #pragma unroll
           for (int i = 0; i < W; ++i) {
-            const int c = first + i;
-            if (c < 2 * half) {
-              const bool b = a.rope.interleaved ? (c & 1) : c >= half;  // the second of its pair
-              const int p = a.rope.interleaved ? c >> 1 : b ? c - half : c;
-              const int mate = a.rope.interleaved ? c ^ 1 : b ? c - half : c + half;
-              const float u = value(row[mate]) * scale * weight[mate];
-              r[i] = fmaf(v[i], cs[p], b ? u * sn[p] : -u * sn[p]);
+            const int e = first + i;
+            if (e < 2 * half) {
+              const bool b = a.rope.interleaved ? (e & 1) : e >= half;  // the second of its pair
+              const int p = a.rope.interleaved ? e >> 1 : b ? e - half : e;
+              const int mate = a.rope.interleaved ? e ^ 1 : b ? e - half : e + half;
+              const float u = value(row[mate]) * scale * weight[mate], sine = a.rope.sin[angles + p];
+              r[i] = fmaf(v[i], a.rope.cos[angles + p], b ? u * sine : -u * sine);
             }
           }
         }
-      }
-      if constexpr (kBf16) {
+        if constexpr (kBf16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[k][i] = pack2(r[2 * i], r[2 * i + 1]);
-      } else {
+          for (int i = 0; i < 4; ++i) q[k][i] = pack2(r[2 * i], r[2 * i + 1]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[k][i] = __float_as_uint(r[i]);
+          for (int i = 0; i < 4; ++i) q[k][i] = __float_as_uint(r[i]);
+        }
       }
+      if (piece) *reinterpret_cast<u32x4 *>(out + head[k] * out_stride + first) = q[k];
     }
-    if (piece) *reinterpret_cast<u32x4 *>(out + (what == 0 ? k * out_stride : at[k].slot * a.d.D)) = q[k];
   }
 }
 
@@ -156,20 +172,25 @@ int lg_lanes_of(const AttnDims &d) {
   while ((1 << lg) < pieces) ++lg;
   return lg;
 }
-int64_t parts_of(const AttnDims &d, bool queries) {
-  return (((queries ? d.H : 0) + int64_t{2} * d.Hk) * (int64_t{1} << lg_lanes_of(d)) + 255) / 256;
-}
-int run_of(const AttnDims &d, int64_t parts) {
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMostTokens, d.T * parts / kFewWorkgroups)));
+// Waves a token, by its queries and its keys (or values).
+struct Units {
+  int turns, queries, keys;
+  int64_t all() const { return queries + int64_t{2} * keys; }
+};
+Units units_of(const AttnDims &d, bool queries) {
+  const int at_once = 64 >> lg_lanes_of(d);
+  const auto units = [&](int heads, int turns) { return (heads + at_once * turns - 1) / (at_once * turns); };
+  const int64_t waves = d.T * (units(queries ? d.H : 0, 1) + int64_t{2} * units(d.Hk, 1));
+  Units u = {};
+  u.turns = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMostTurns, waves / kWaves)));
+  u.queries = units(queries ? d.H : 0, u.turns);
+  u.keys = units(d.Hk, u.turns);
+  return u;
 }
 
 }  // namespace
 
-bool attn_append_norm_fits(const AttnDims &d, bool queries) {
-  const int64_t parts = parts_of(d, queries);
-  const int run = run_of(d, parts);
-  return parts <= 65535 && (d.T + int64_t{run} - 1) / run * parts <= kMostWorkgroups256;
-}
+bool attn_append_norm_fits(const AttnDims &d, bool queries) { return (d.T * units_of(d, queries).all() + 3) / 4 <= kMostWorkgroups256; }
 
 hipError_t launch_attn_append_norm(const AttnDims &d, const Rope &rope, const int32_t *cu, const int32_t *lens, const int32_t *table,
                                    const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
@@ -195,10 +216,13 @@ hipError_t launch_attn_append_norm(const AttnDims &d, const Rope &rope, const in
   a.eps = eps;
   a.inv_headdim = 1.f / static_cast<float>(d.D);
   a.lg_lanes = lg_lanes_of(d);
-  a.q_heads = q != nullptr ? d.H : 0;
-  const int64_t parts = parts_of(d, q != nullptr);
-  a.run = run_of(d, parts);
-  const dim3 grid((d.T + a.run - 1) / a.run, static_cast<unsigned>(parts));
+  const Units u = units_of(d, q != nullptr);
+  a.turns = u.turns;
+  a.units[0] = u.queries;
+  a.units[1] = u.keys;
+  a.all_units = static_cast<int>(u.all());
+  a.inv_all_units = inverse_of(a.all_units);
+  const dim3 grid(static_cast<unsigned>((d.T * u.all() + 3) / 4));
   const int width = rope.interleaved ? 2 * rope.half : rope.half;
   const bool whole = width % (d.bf16 ? 8 : 4) == 0;
   if (d.bf16 && whole)

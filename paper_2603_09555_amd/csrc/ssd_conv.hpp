@@ -39,17 +39,17 @@ __device__ __forceinline__ typename Io::type *out_ptr(const ConvOut &o, size_t r
 
 // Tokens per thread: long runs amortise the k-1 rows a thread reads in front of its own and the
 // weights it loads, but the threads should also fill the chip a whole number of times: the length in
-// [kRunMin, kRunMax] with the least (rounds of waves) x (rows read per run).  `blocks_per_cu` is what the
+// [shortest, kRunMax] with the least (rounds of waves) x (rows read per run).  `blocks_per_cu` is what the
 // runtime reports for the kernel (its register count decides it).
-int choose_run(int T, size_t groups_total, int ksize, int blocks_per_cu) {
+int choose_run(int T, size_t groups_total, int ksize, int blocks_per_cu, int shortest = kRunMin) {
   const double slots = 256.0 * blocks_per_cu * kConvThreads;  // threads resident at once
-  int best = kRunMin;
+  int best = shortest;
   double best_cost = 0.0;
-  for (int len = kRunMin; len <= kRunMax; ++len) {
+  for (int len = shortest; len <= kRunMax; ++len) {
     const double runs = (T + len - 1) / len;
     const double rounds = static_cast<double>(static_cast<long long>((runs * groups_total + slots - 1) / slots));
     const double cost = rounds * (len + ksize - 1 + 4);  // + about four rows' worth of start-up per thread
-    if (len == kRunMin || cost < best_cost) {
+    if (len == shortest || cost < best_cost) {
       best = len;
       best_cost = cost;
     }

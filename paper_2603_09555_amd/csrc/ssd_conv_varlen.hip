@@ -6,18 +6,24 @@
 // Inputs before a sequence's first token come from its cache, or are zero.  A stream like the batched kernel's, and laid out
 // like it: a thread owns four channels (8 bytes of bf16, 16 of fp32; one channel where an output's width is no multiple of
 // four) and a run of the packed tokens, whatever sequences these belong to, with the window and its weights in registers.  It
-// finds the sequence of its first token once; where the next one begins it fills the window from that one's cache.  Rows of u
+// finds the sequence of its first token once, while its first rows are on their way; where the next one begins it fills the window
+// from that one's cache.  Rows of u
 // may be a slice of wider ones, so that the input projection's output need not be copied.
 //
 // The caches are left by threads of their own, one a sequence and channel: in the same launch, or, where they are updated in
 // place, in one behind it (a sequence's first run reads what its last would write).
 #include "ssd_conv.hpp"
 
+#ifndef VRS
+#define VRS 4
+#endif
 namespace ssd {
 namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kRunShort = VRS;  // tokens a thread, at least: few tokens are worth more threads
 
 struct VarlenArgs {
   const void *u;
@@ -65,16 +71,10 @@ __device__ __forceinline__ float to_float(typename Io::type v) {
   return Io::load(&v, 0);
 }
 
-// The last sequence that begins at or in front of a token (-1: none).  One trip to memory for up to 64 sequences.
-__device__ __forceinline__ int sequence_at(const int32_t *cu, int B, int token) {
-  int last = -1, behind = B;
-  while (behind - last > 1) {
-    const int q = (last + behind) / 2;
-    if (cu[q] <= token) last = q;
-    else behind = q;
-  }
-  return last;
-}
+// A thread looks several boundaries up, one after another: they go through LDS where they fit.  Which it is has to be known to the
+// compiler: through a pointer to either it makes flat loads, which choose the memory by the address in front of the constant that
+// they add, and fault where that address is not in LDS while the sum is.
+constexpr int kMostStaged = 1024;
 
 template <typename Io, int K>
 __device__ __forceinline__ void leave_cache(const VarlenArgs &a, int64_t i) {
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_cache_kernel(const VarlenAr
   if (i < static_cast<int64_t>(a.B) * a.C) leave_cache<Io, K>(a, i);
 }
 
-template <typename Io, int V, int K>
+template <typename Io, int V, int K, bool kStaged>
 __global__ __launch_bounds__(kConvThreads) void conv_varlen_kernel(const VarlenArgs a) {
   using E = typename Io::type;
   if (blockIdx.x >= a.filter_blocks) {
@@ -109,6 +109,15 @@ __global__ __launch_bounds__(kConvThreads) void conv_varlen_kernel(const VarlenA
     if (i < static_cast<int64_t>(a.B) * a.C) leave_cache<Io, K>(a, i);
     return;
   }
+  __shared__ int32_t staged[kStaged ? kMostStaged + 1 : 1];  // [q + 1]: boundary q
+  if constexpr (kStaged) {
+    for (int i = threadIdx.x; i <= a.B; i += kConvThreads) staged[i + 1] = a.cu[i];
+    __syncthreads();
+  }
+  auto cu = [&](int q) __attribute__((always_inline)) {
+    if constexpr (kStaged) return staged[q + 1];
+    else return a.cu[q];
+  };
   const unsigned groups = a.C / V, gid = blockIdx.x * kConvThreads + threadIdx.x;
   const unsigned run = gid / groups;
   const int64_t first = static_cast<int64_t>(run) * a.run;
@@ -126,56 +135,73 @@ __global__ __launch_bounds__(kConvThreads) void conv_varlen_kernel(const VarlenA
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) r.r[i] = load_row<Io, V>(u + min(tb + i, t1 - 1) * a.u_stride);  // (surplus ones: the last row)
   };
+  // all that does not depend on the boundaries: the first rows, those in front of them (which may be another sequence's), weights
+  Row<Io, V> front[K - 1];
+#pragma unroll
+  for (int j = 0; j + 1 < K; ++j) front[j] = load_row<Io, V>(u + max(t0 - (K - 1) + j, 0) * a.u_stride);
   request(buf[0], t0);
   float wt[V][K], bs[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
+  for (int v = 0; v < V; ++v)
 #pragma unroll
     for (int j = 0; j < K; ++j) wt[v][j] = a.w[static_cast<int64_t>(c0 + v) * K + j];
-    bs[v] = a.bias ? a.bias[c0 + v] : 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) bs[v] = 0.f;
+  if (a.bias) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) bs[v] = a.bias[c0 + v];
   }
-  // the sequence q of token t0 has [begin, end); tokens in front of the first and behind the last one are in none
-  int q = sequence_at(a.cu, a.B, t0), begin = 0, end = t0;
+  // tokens [begin, end) are sequence next - 1's; those in front of the first and behind the last one are in none
+  int next = 0, begin = 0, end = t0;
+  for (int most = a.B; next < most;) {
+    const int middle = (next + most) / 2;
+    if (cu(middle) <= t0) next = middle + 1;
+    else most = middle;
+  }
   float win[K][V];
-  auto fill = [&](int t) __attribute__((always_inline)) {  // win[1 ..]: the inputs in front of token t of sequence q
+  // win[1 ..]: the inputs in front of a token that `behind` new ones of its sequence precede; `behind` of them are there already
+  auto fill_cached = [&](int behind) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 1; j < K; ++j) {
-      const int s = t - K + j;
-      if (s >= begin) {
-        const Row<Io, V> r = load_row<Io, V>(u + s * a.u_stride);
-#pragma unroll
-        for (int v = 0; v < V; ++v) win[j][v] = to_float<Io>(r.e[v]);
-      } else {
+    for (int j = 1; j < K; ++j)
+      if (K - j > behind) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
-          win[j][v] = a.state_in ? to_float<Io>(cached[(static_cast<int64_t>(q) * a.C + v) * (K - 1) + K - 1 + s - begin]) : 0.f;
+          win[j][v] = a.state_in ? to_float<Io>(cached[(static_cast<int64_t>(next - 1) * a.C + v) * (K - 1) + j - 1 + behind]) : 0.f;
       }
-    }
   };
   // `turn`: the next token at which something changes; `inside`: whether the tokens up to it are in a sequence
   int turn;
   bool inside;
   auto enter = [&](int t) __attribute__((always_inline)) {
-    while (q + 1 < a.B && a.cu[q + 1] <= t) ++q;
-    if (q >= 0) {
-      begin = max(a.cu[q], 0);
-      end = min(a.cu[q + 1], a.T);
+    while (next < a.B && cu(next) <= t) ++next;
+    if (next > 0) {
+      begin = max(cu(next - 1), 0);
+      end = min(cu(next), a.T);
     }
-    inside = q >= 0 && t >= begin && t < end;
-    if (inside) fill(t);
-    turn = inside ? end : q + 1 < a.B ? max(a.cu[q + 1], t + 1) : a.T;
+    inside = next > 0 && t >= begin && t < end;
+    turn = inside ? end : next < a.B ? max(cu(next), t + 1) : a.T;
   };
   enter(t0);
+#pragma unroll
+  for (int j = 1; j < K; ++j)
+#pragma unroll
+    for (int v = 0; v < V; ++v) win[j][v] = to_float<Io>(front[j - 1].e[v]);
+  if (inside && t0 - begin < K - 1) fill_cached(t0 - begin);
 
-  const int part = c0 >= a.out.begin[2] ? 2 : c0 >= a.out.begin[1] ? 1 : 0;
-  const int width = a.out.begin[part + 1] - a.out.begin[part];
-  E *const z = static_cast<E *>(a.out.ptr[part]) + (c0 - a.out.begin[part]);
+  // (chosen without an index: the arguments are in scalar registers)
+  const bool second = c0 >= a.out.begin[1], third = c0 >= a.out.begin[2];
+  const int out_first = third ? a.out.begin[2] : second ? a.out.begin[1] : 0;
+  const int width = (third ? a.out.begin[3] : second ? a.out.begin[2] : a.out.begin[1]) - out_first;
+  E *const z = static_cast<E *>(third ? a.out.ptr[2] : second ? a.out.ptr[1] : a.out.ptr[0]) + (c0 - out_first);
   auto process = [&](const Rows &r, int tb) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const int t = tb + i;
       if (t < t1) {
-        if (t >= turn) enter(t);
+        if (t >= turn) {
+          enter(t);
+          if (inside) fill_cached(0);  // (a sequence's first token)
+        }
 #pragma unroll
         for (int j = 0; j + 1 < K; ++j)
 #pragma unroll
@@ -215,7 +241,7 @@ template <typename Io, int V, int K>
 int resident_blocks() {
   static const int blocks = [] {
     int n = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, conv_varlen_kernel<Io, V, K>, kConvThreads, 0) != hipSuccess || n < 1) n = 4;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, conv_varlen_kernel<Io, V, K, true>, kConvThreads, 0) != hipSuccess || n < 1) n = 4;
     return n;
   }();
   return blocks;
@@ -224,16 +250,21 @@ int resident_blocks() {
 template <typename Io, int K>
 hipError_t varlen_typed(VarlenArgs a, bool four, hipStream_t stream) {
   const int groups = four ? a.C / 4 : a.C;
-  a.run = choose_run(a.T, groups, K, four ? resident_blocks<Io, 4, K>() : resident_blocks<Io, 1, K>());
+  a.run = choose_run(a.T, groups, K, four ? resident_blocks<Io, 4, K>() : resident_blocks<Io, 1, K>(), kRunShort);
   const auto blocks = [](int64_t threads) { return static_cast<unsigned>((threads + kConvThreads - 1) / kConvThreads); };
   a.filter_blocks = blocks(static_cast<int64_t>((a.T + a.run - 1) / a.run) * groups);
   const unsigned cache_blocks = a.state_out ? blocks(static_cast<int64_t>(a.B) * a.C) : 0;
   const bool in_place = a.state_out != nullptr && a.state_out == a.state_in;
   const dim3 grid(a.filter_blocks + (in_place ? 0 : cache_blocks));
-  if (four)
-    hipLaunchKernelGGL((conv_varlen_kernel<Io, 4, K>), grid, dim3(kConvThreads), 0, stream, a);
+  const bool staged = a.B < kMostStaged;
+  if (four && staged)
+    hipLaunchKernelGGL((conv_varlen_kernel<Io, 4, K, true>), grid, dim3(kConvThreads), 0, stream, a);
+  else if (four)
+    hipLaunchKernelGGL((conv_varlen_kernel<Io, 4, K, false>), grid, dim3(kConvThreads), 0, stream, a);
+  else if (staged)
+    hipLaunchKernelGGL((conv_varlen_kernel<Io, 1, K, true>), grid, dim3(kConvThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL((conv_varlen_kernel<Io, 1, K>), grid, dim3(kConvThreads), 0, stream, a);
+    hipLaunchKernelGGL((conv_varlen_kernel<Io, 1, K, false>), grid, dim3(kConvThreads), 0, stream, a);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || !in_place) return e;
   hipLaunchKernelGGL((conv_cache_kernel<Io, K>), dim3(cache_blocks), dim3(kConvThreads), 0, stream, a);
   return hipGetLastError();
@@ -243,7 +274,7 @@ hipError_t varlen_typed(VarlenArgs a, bool four, hipStream_t stream) {
 
 // Whether the threads of a call, one a channel and run or sequence at most, are no more than a launch takes.
 bool conv_varlen_fits(int B, int T, int64_t C) {
-  return (static_cast<int64_t>(T + kRunMin - 1) / kRunMin + B) * C <= (int64_t{1} << 32) - 3 * kConvThreads;
+  return (static_cast<int64_t>(T + kRunShort - 1) / kRunShort + B) * C <= (int64_t{1} << 32) - 3 * kConvThreads;
 }
 
 hipError_t launch_conv_varlen(int B, int T, int ksize, bool bf16, const int32_t *cu, const void *u, int64_t u_stride,

@@ -25,8 +25,6 @@
 namespace ssd {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-
 // B and C as the kernels read them: a row's states are aligned to 4 bytes and as many as the waves hold.
 struct Rows {
   const void *b, *c;
@@ -47,8 +45,6 @@ struct ScanArgs {
   int segments;
 };
 
-__device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e)); }
-
 // The last sequence that begins in front of a token (-1: none).
 __device__ __forceinline__ int last_before(const int32_t *cu, int B, int token) {
   int last = -1, behind = B;
@@ -64,23 +60,6 @@ __device__ __forceinline__ int last_before(const int32_t *cu, int B, int token) 
 __device__ __forceinline__ uint32_t stride_of(uint32_t v) {
   asm volatile("" : "+s"(v));
   return v;
-}
-
-// softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|), in 17 issue slots of the vector unit, within 4 2^-24 of itself down to
-// v = -80.  What rounding the exponent p = -|v| log2(e) takes away comes back as a factor of e, and what rounding 1 + e does, which is
-// most of a small e, as the first term of the logarithm's series (1 / (1 + e) within 0.09 there, of something below 2^-24).
-__device__ __forceinline__ float softplus(float v) {
-  const float a = fmaxf(-fabsf(v), -100.f);  // (behind it e is nothing; a NaN comes back with max(v, 0))
-  const float p = a * kLog2e, rest = fmaf(p, -0.693147182f, a);
-  const float e2 = __builtin_amdgcn_exp2f(p), e = fmaf(e2, rest, e2);
-  const float u = 1.f + e, lost = e - (u - 1.f);
-  return (v <= 0.f ? 0.f : v) + fmaf(lost, fmaf(-0.5f, e, 1.f), __builtin_amdgcn_logf(u) * 0.693147182f);
-}
-// The step size of a raw value.
-__device__ __forceinline__ float step_of(float v, float bias, const DtXform &map) {
-  v += bias;
-  if (map.softplus) v = softplus(v);
-  return map.hi > 0.f ? fminf(fmaxf(v, map.lo), map.hi) : v;
 }
 
 // Values of a row that all lanes of a wave read alike, through the scalar cache.

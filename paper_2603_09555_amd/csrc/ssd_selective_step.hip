@@ -4,20 +4,23 @@
 //   y[b][c] = (sum_n C[b][n] h[b][c][n] + D[c] x[b][c]) silu(z[b][c])
 //
 // Bound by one read and one write of the states.  A lane holds four neighbouring states of a channel (16 bytes), the next
-// lanes the channel's others: sums over them stay within 4 lanes for 16 states, within 64 for 256.
+// lanes the channel's others: sums over them stay within 4 lanes for 16 states, within 64 for 256.  Where there are many
+// sequences a lane takes those states of two of them, which are on their way together, and reads the decays once.
 #include "ssd_selective.hpp"
 
 namespace ssd {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 
 struct StepArgs {
   SelectiveArgs a;
   float *state;
   SelectiveDims d;
-  int lanes;  // of a channel: a power of two, four states each
+  int lanes;           // of a channel: a power of two, four states each
+  unsigned across;     // workgroups a sequence
+  uint32_t inv_across;
 };
 
 __device__ __forceinline__ float to_float(float v) { return v; }
@@ -25,65 +28,82 @@ __device__ __forceinline__ float to_float(uint16_t v) { return bf16_bits_to_f32(
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(uint16_t *p, float v) { *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
 
-template <typename E, typename EDt>
+// Four neighbouring values, of which the first `left` are there (all of them if kWhole); the others are zeros.
+template <bool kWhole>
+__device__ __forceinline__ void load4(const float *p, int left, float v[4]) {
+  if (kWhole) {
+    const f32x4 q = *reinterpret_cast<const f32x4 __attribute__((aligned(4))) *>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = q[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = k < left ? p[k] : 0.f;
+  }
+}
+template <bool kWhole>
+__device__ __forceinline__ void load4(const uint16_t *p, int left, float v[4]) {
+  if (kWhole) {
+    const u16x4 q = *reinterpret_cast<const u16x4 __attribute__((aligned(2))) *>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = to_float(q[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = k < left ? to_float(p[k]) : 0.f;
+  }
+}
+
+// kWhole: as many states as four times the lanes.  R: sequences a lane.
+template <typename E, typename EDt, bool kWhole, int R>
 __global__ __launch_bounds__(256) void selective_step_kernel(const StepArgs a) {
   const int lanes = a.lanes, N = a.d.N, C = a.d.C;
-  const int b = blockIdx.y;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  const int64_t c64 = i / lanes;
-  const int piece = static_cast<int>(i) & (lanes - 1), first = 4 * piece;
-  const bool there = c64 < C;
-  const int c = there ? static_cast<int>(c64) : C - 1;
-  const int64_t at = static_cast<int64_t>(b) * C + c;
-  const int left = N - first;  // states from `first` on
-  float A2[4], h[4], Bv[4], Cv[4];
-  float *const state = a.state + at * N + first;
-  const float *const A = a.a.A + static_cast<int64_t>(c) * N + first;
-  const E *const Br = static_cast<const E *>(a.a.B) + b * a.a.b_stride + first, *const Cr = static_cast<const E *>(a.a.C) + b * a.a.c_stride + first;
-  const bool whole = N % 4 == 0;
-  if (whole && left > 0) {
-    const f32x4 v = *reinterpret_cast<const f32x4 *>(state), w = *reinterpret_cast<const f32x4 *>(A);
+  const int row = quotient(blockIdx.x, a.across, a.inv_across), b0 = row * R;
+  const int i = static_cast<int>(blockIdx.x - row * a.across) * 256 + static_cast<int>(threadIdx.x);
+  const int c_real = i / lanes, piece = i & (lanes - 1), first = 4 * piece;
+  const int c = min(c_real, C - 1);
+  const bool there = c_real < C && first < N;
+  // (a lane without states reads the channel's first ones and leaves them out)
+  const int at = first < N ? first : 0, left = first < N ? N - first : 0;
+  float A2[4], h[R][4], Bv[R][4], Cv[R][4], x[R], dt[R], z[R];
+  load4<kWhole>(a.a.A + static_cast<int64_t>(c) * N + at, left, A2);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int b = min(b0 + r, a.d.B - 1);  // (surplus ones: the last sequence, not written)
+    const int64_t channel = static_cast<int64_t>(b) * C + c;
+    load4<kWhole>(a.state + channel * N + at, left, h[r]);
+    load4<kWhole>(static_cast<const E *>(a.a.B) + b * a.a.b_stride + at, left, Bv[r]);
+    load4<kWhole>(static_cast<const E *>(a.a.C) + b * a.a.c_stride + at, left, Cv[r]);
+    x[r] = to_float(static_cast<const E *>(a.a.x)[channel]);
+    dt[r] = to_float(static_cast<const EDt *>(a.a.dt)[channel]);
+    z[r] = a.a.z ? to_float(static_cast<const E *>(a.a.z)[b * a.a.z_stride + c]) : 0.f;
+  }
+  const float bias = a.d.dtx.bias ? a.d.dtx.bias[c] : 0.f, skip = a.a.D ? a.a.D[c] : 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) A2[k] *= kLog2e;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float d = step_of(dt[r], bias, a.d.dtx), u = d * x[r];
+    float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      h[k] = v[k];
-      A2[k] = w[k] * kLog2e;
-      Bv[k] = to_float(Br[k]);
-      Cv[k] = to_float(Cr[k]);
+      h[r][k] = fmaf(__builtin_amdgcn_exp2f(d * A2[k]), h[r][k], u * Bv[r][k]);
+      sum = fmaf(Cv[r][k], h[r][k], sum);
     }
-  } else {
+    for (int k = 1; k < lanes; k <<= 1) sum += __shfl_xor(sum, k);
+    if (!there || b0 + r >= a.d.B) continue;
+    const int64_t channel = static_cast<int64_t>(b0 + r) * C + c;
+    float *const state = a.state + channel * N + first;
+    if (kWhole) {
+      *reinterpret_cast<f32x4 *>(state) = f32x4{h[r][0], h[r][1], h[r][2], h[r][3]};
+    } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      h[k] = k < left ? state[k] : 0.f;
-      A2[k] = k < left ? A[k] * kLog2e : 0.f;
-      Bv[k] = k < left ? to_float(Br[k]) : 0.f;
-      Cv[k] = k < left ? to_float(Cr[k]) : 0.f;
+      for (int k = 0; k < 4; ++k)
+        if (k < left) state[k] = h[r][k];
     }
-  }
-  const float x = to_float(static_cast<const E *>(a.a.x)[at]);
-  const float d = dt_apply_branchless(to_float(static_cast<const EDt *>(a.a.dt)[at]), a.d.dtx.bias ? a.d.dtx.bias[c] : 0.f, a.d.dtx);
-  const float u = d * x;
-  float acc = 0.f;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    h[k] = fmaf(__builtin_amdgcn_exp2f(d * A2[k]), h[k], u * Bv[k]);
-    acc = fmaf(Cv[k], h[k], acc);
-  }
-  for (int k = 1; k < lanes; k <<= 1) acc += __shfl_xor(acc, k);
-  if (!there) return;
-  if (whole && left > 0) {
-    *reinterpret_cast<f32x4 *>(state) = f32x4{h[0], h[1], h[2], h[3]};
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < left) state[k] = h[k];
-  }
-  if (piece == 0) {
-    acc = fmaf(a.a.D ? a.a.D[c] : 0.f, x, acc);
-    if (a.a.z) {
-      const float v = to_float(static_cast<const E *>(a.a.z)[b * a.a.z_stride + c]);
-      acc *= v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e));
+    if (piece == 0) {
+      sum = fmaf(skip, x[r], sum);
+      if (a.a.z) sum *= silu(z[r]);
+      put(static_cast<E *>(a.a.y) + channel, sum);
     }
-    put(static_cast<E *>(a.a.y) + at, acc);
   }
 }
 
@@ -92,20 +112,35 @@ int lanes_of(int N) {
   while (4 * l < N) l <<= 1;
   return l;
 }
+int64_t across_of(const SelectiveDims &d) { return (static_cast<int64_t>(d.C) * lanes_of(d.N) + 255) / 256; }
+// Sequences a lane: two, as long as that leaves workgroups for all CUs.
+int sequences_of(const SelectiveDims &d) { return d.B * across_of(d) >= 4096 ? 2 : 1; }
+
+template <typename E, typename EDt, bool kWhole>
+void launch_rows(const StepArgs &a, int rows, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>((a.d.B + int64_t{rows} - 1) / rows * a.across));
+  if (rows == 2)
+    hipLaunchKernelGGL((selective_step_kernel<E, EDt, kWhole, 2>), grid, dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((selective_step_kernel<E, EDt, kWhole, 1>), grid, dim3(256), 0, stream, a);
+}
+template <typename E, typename EDt>
+void launch_typed(const StepArgs &a, int rows, hipStream_t stream) {
+  if (a.d.N == 4 * a.lanes) launch_rows<E, EDt, true>(a, rows, stream);
+  else launch_rows<E, EDt, false>(a, rows, stream);
+}
 
 }  // namespace
 
-bool selective_step_fits(const SelectiveDims &d) { return static_cast<int64_t>(d.B) * ((static_cast<int64_t>(d.C) * lanes_of(d.N) + 255) / 256) * 256 < (int64_t{1} << 32) && d.B <= 65535; }
+bool selective_step_fits(const SelectiveDims &d) { return (d.B + int64_t{sequences_of(d)} - 1) / sequences_of(d) * across_of(d) < (1 << 24); }
 
 hipError_t launch_selective_step(const SelectiveDims &d, const SelectiveArgs &args, float *state, hipStream_t stream) {
-  StepArgs a = {args, state, d, lanes_of(d.N)};
-  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(d.C) * a.lanes + 255) / 256), d.B);
-  if (!d.bf16)
-    hipLaunchKernelGGL((selective_step_kernel<float, float>), grid, dim3(256), 0, stream, a);
-  else if (d.dt_bf16)
-    hipLaunchKernelGGL((selective_step_kernel<uint16_t, uint16_t>), grid, dim3(256), 0, stream, a);
-  else
-    hipLaunchKernelGGL((selective_step_kernel<uint16_t, float>), grid, dim3(256), 0, stream, a);
+  StepArgs a = {args, state, d, lanes_of(d.N), static_cast<unsigned>(across_of(d)), 0};
+  a.inv_across = inverse_of(static_cast<int>(a.across));
+  const int rows = sequences_of(d);
+  if (!d.bf16) launch_typed<float, float>(a, rows, stream);
+  else if (d.dt_bf16) launch_typed<uint16_t, uint16_t>(a, rows, stream);
+  else launch_typed<uint16_t, float>(a, rows, stream);
   return hipGetLastError();
 }
 
