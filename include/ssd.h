@@ -372,7 +372,7 @@ SSD_API ssd_status ssd_conv1d_varlen(int32_t batch, int32_t tokens, int32_t ksiz
  *   z                 (tokens, channels) io dtype, rows z_stride >= channels elements apart,
  *                     aligned to its elements; or NULL: no gate
  *   state, h0, final_state  (batch, channels, dstate) fp32
- * dstate is at most 256, strides at most 2^26 (SSD_ERR_UNSUPPORTED), channels at most 2^22;
+ * dstate is at most 256, strides at most 2^24 (SSD_ERR_UNSUPPORTED), channels at most 2^22;
  * the other pointers are 16-byte aligned.  Arithmetic, sums and states are fp32; y is rounded once.
  *
  * ssd_selective_prefill scans a packed batch; cu_seqlens as for ssd_conv1d_varlen.

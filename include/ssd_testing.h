@@ -45,8 +45,10 @@ typedef enum {
   SSD_KNOB_DEAL = 11,          /* packed bf16 batches: 1 the full scan's workgroups are dealt items of two heads, however few
                                  these are, unless the decay records take 4 GiB; 2 they take an entry each; 0: library's choice */
   SSD_KNOB_SPLIT_IMAGES = 12,  /* fp32 io on split operands: 2 no images of blocks; 0: library's choice */
-  SSD_KNOB_SELECTIVE_SEGMENT = 13 /* k > 0: k tokens per segment of the selective scan (a multiple of 8 is taken, and no fewer than
-                                 the workspace has room for); 0: library's choice */
+  SSD_KNOB_SELECTIVE_SEGMENT = 13, /* k > 0: k tokens per segment of the selective scan (a multiple of 8 or 16 is taken, and no fewer
+                                 than the workspace has room for); 0: library's choice */
+  SSD_KNOB_SELECTIVE_BY_STATE = 14 /* selective scan with a lane a state (up to 64 of a channel): 1 wherever it can, 2 never; 0: library's
+                                 choice */
 } ssd_knob;
 
 /* Sets one knob.  Errors: SSD_ERR_SHAPE for an unknown knob. */

@@ -478,6 +478,7 @@ ssd_status ssd_testing_set_knob(int32_t knob, int32_t value) {
     case SSD_KNOB_SPLIT_IMAGES: k.split_images = value == 2 ? 2 : 0; return SSD_OK;
     case SSD_KNOB_SCAN_HEADS: k.scan_heads = value == 2 || value == 4 ? value : 0; return SSD_OK;
     case SSD_KNOB_SELECTIVE_SEGMENT: k.selective_segment = value > 0 && value <= (1 << 30) ? value : 0; return SSD_OK;
+    case SSD_KNOB_SELECTIVE_BY_STATE: k.selective_by_state = value == 1 || value == 2 ? value : 0; return SSD_OK;
     default: return SSD_ERR_SHAPE;
   }
 }

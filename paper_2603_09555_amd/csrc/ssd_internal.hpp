@@ -135,6 +135,7 @@ struct Knobs {
   int split_images = 0;    // fp32 prefill on split operands: 2 no images of blocks; 0: library's choice
   int chunk = 0;           // bf16 prefill by chunk kernels: 1 wherever they can run, 2 never; 0: library's choice
   int selective_segment = 0;  // > 0: tokens per segment of the selective scan, if the workspace has room for so many segments
+  int selective_by_state = 0;   // selective scan, a lane a state: 1 wherever it can, 2 never; 0: library's choice
   int fold_max_slots = 3;  // most state slots a segment sums by itself instead of a pass over segment states (0: never)
 };
 Knobs &knobs();

@@ -39,7 +39,7 @@ ssd_status selective_args(SelectiveDims *d, const ssd_dt_transform *dtx, const v
   }
   if (B_stride < d->N || C_stride < d->N || (z && z_stride < d->C)) return SSD_ERR_SHAPE;
   for (const int64_t stride : {B_stride, C_stride, z ? z_stride : 0})
-    if (stride > (1 << 26)) return SSD_ERR_UNSUPPORTED;  // (eight rows are addressed with 32 bits)
+    if (stride > (1 << 24)) return SSD_ERR_UNSUPPORTED;  // (sixteen rows are addressed with 31 bits)
   if (!x || !dt || !A || !B || !C || !y) return SSD_ERR_NULL;
   const uintptr_t element = d->bf16 ? 2 : 4;
   for (const void *p : {B, C, z})

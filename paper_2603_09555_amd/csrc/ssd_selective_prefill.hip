@@ -3,12 +3,12 @@
 //   d = step(dt[t][c]),  h[c][n] = exp(d A[c][n]) h[c][n] + d x[t][c] B[t][n]
 //   y[t][c] = (sum_n C[t][n] h[c][n] + D[c] x[t][c]) silu(z[t][c])
 //
-// A lane is a channel and holds its states in registers; B and C are the same for all of a wave's lanes and come through the
-// scalar unit.
+// The decay differs from state to state, so nothing here is a matrix product.  Bound by the vector unit: an exponential, two issue
+// slots on this card (16 of them 154 cycles a wave, 16 fused products 70), and four products for each token, channel and state, where
+// a matrix instruction for d x B would save a tenth (it does not overlap with them).
 //
-// The decay differs from state to state, so nothing here is a matrix product: an exponential (a quarter of the vector rate) and
-// four vector operations for each token, channel and state, which bounds the kernel where memory does not.  There are too few
-// channels to fill the chip, so time is cut into segments of the packed tokens, whatever sequences these belong to:
+// Two kernels: a lane is a channel and holds states of it in registers, or a lane is a state (see by_state_kernel).  There are too few
+// channels to fill the chip either way, so time is cut into segments of the packed tokens, whatever sequences these belong to:
 //
 //   states:  the state at each segment's end, from zero, or from h0 where the last sequence in it begins there, and the sum of
 //            that stretch's step sizes (the decay across it is exp(A sum))
@@ -16,9 +16,13 @@
 //   scan:    the outputs, from the state that enters
 //
 // A segment whose last token ends a sequence (or is in none) needs no states pass, so that batches of short prompts do little
-// twice.  Where all tokens are one segment only the scan runs.
+// twice.  Where all tokens are one segment only the scan runs.  States, sums and step sizes are fp32; y is rounded once.
+//
+// 16 states, bf16: 16384 tokens x 5120 channels 540 us (states 220, carry 15, scan 310; the issue slots of both passes alone are 510),
+// 9938 tokens of 12 prompts 345, 61 tokens x 1536 channels 5.6; 2048 x 1536 in fp32 46.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "ssd_selective.hpp"
 
@@ -80,6 +84,7 @@ struct Uniform {
 };
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 __device__ __forceinline__ Rsrc buffer_at(const void *base) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, 0x7fffffff, 0x00020000);
@@ -96,10 +101,51 @@ template <bool kBf16>
 __device__ __forceinline__ float to_float(uint32_t raw) {
   return __uint_as_float(kBf16 ? raw << 16 : raw);
 }
+__device__ __forceinline__ float value(float v) { return v; }
+__device__ __forceinline__ float value(uint16_t v) { return bf16_bits_to_f32(v); }
+__device__ __forceinline__ void put(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put(uint16_t *p, float v) { *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
 template <bool kBf16>
 __device__ __forceinline__ void store(Rsrc r, uint32_t lane_at, uint32_t row_at, float v) {
   if constexpr (kBf16) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, static_cast<__bf16>(v)), r, lane_at, row_at, 0);
   else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, lane_at, row_at, 0);
+}
+
+// What either kernel does with a segment s, of tokens [t0, t1).  A sequence has `size` states; this lane's channel begins at slot in the
+// workspace's arrays and at `at` in a sequence's states: `load` and `save` are told which of the two an address is.
+template <bool kStates, typename Load, typename Save, typename Walk, typename Total>
+__device__ __forceinline__ void scan_segment(const ScanArgs &a, int s, int t0, int t1, int64_t size, int64_t slot, int64_t at, const Load &load,
+                                             const Save &save, const Walk &walk, const Total &total, bool writes_total, int c) {
+  const int T = a.d.T;
+  int q = kStates || s > 0 ? last_before(a.cu, a.d.B, kStates ? t1 : t0) : 0;
+  if constexpr (kStates) {
+    int begin = 0, end = 0;
+    if (q >= 0) {
+      begin = max(a.cu[q], 0);
+      end = min(a.cu[q + 1], T);
+    }
+    const bool goes_on = q >= 0 && begin < t1 && end > t1, begins = begin >= t0;
+    load(goes_on && begins && a.h0 ? a.h0 + q * size + at : nullptr, false);
+    if (goes_on) {
+      if (begins && a.begun) save(a.begun + slot, true);
+      walk(max(begin, t0), t1);
+    }
+    save(a.entering + slot, true);
+    const float sum = total();
+    if (writes_total) a.steps[static_cast<int64_t>(s) * a.d.C + c] = goes_on && !begins ? sum : -1.f;
+  } else {
+    // the sequence that goes on into this segment, if any, and those that begin in it (at its end, too, if it is the last)
+    const int last = s == a.segments - 1 ? T : t1 - 1;
+    for (q = max(q, 0); q < a.d.B; ++q) {
+      const int begin = min(max(a.cu[q], 0), T), end = min(a.cu[q + 1], T);
+      if (begin > last) break;
+      const bool begins = begin >= t0, kept = begins && end > t1 && a.begun;
+      if (!begins && end <= t0) continue;
+      load(!begins ? a.entering + slot - size : kept ? a.begun + slot : a.h0 ? a.h0 + q * size + at : nullptr, !begins || kept);
+      walk(max(begin, t0), min(end, t1));
+      if (end <= t1) save(a.final_state + q * size + at, false);
+    }
+  }
 }
 
 constexpr int block_of(int waves) { return waves >= 4 ? 16 : 8; }
@@ -108,20 +154,16 @@ constexpr int waves_a_simd(int states) { return states <= 16 ? 4 : 2; }
 // kIo, kDt, kBc: bf16 (x, z, y; dt; rows of B and C).  NS states a wave, W waves for a channel's states.  kStates: the states
 // pass.
 //
-// Tokens are taken in blocks of eight.  A wave turns the rows of its share of a block's tokens into step sizes and inflows, which
+// Tokens are taken in blocks of eight or sixteen.  B and C are the same for all of a wave's lanes and come through the scalar unit.  A wave turns the rows of its share of a block's tokens into step sizes and inflows, which
 // go to all waves through LDS, and into skip terms and gates, which it keeps; then it asks for its rows of the next block.  The
 // waves walk the block's tokens one by one, each on its states, with the next token's step, inflow, B and C on their way, and
 // leave the parts of the outputs' sums in LDS, which the wave that prepared a token adds up.
 template <bool kIo, bool kDt, bool kBc, int NS, int W, bool kStates>
-__global__ __launch_bounds__(64 * W, kStates ? 1 : waves_a_simd(NS)) void selective_kernel(const ScanArgs a) {
-    constexpr int kBlock = block_of(W), kOwn = kBlock / W;  // tokens of a block; those that a wave prepares and finishes
+__global__ __launch_bounds__(64 * W, kStates ? 1 : waves_a_simd(NS)) void by_channel_kernel(const ScanArgs a) {
+  constexpr int kBlock = block_of(W), kOwn = kBlock / W;  // tokens of a block; those that a wave prepares and finishes
   static_assert(kBlock % W == 0, "a wave's tokens are as many as any other's");
   constexpr uint32_t kSize = kIo ? 2 : 4, kDtSize = kDt ? 2 : 4, kBcSize = kBc ? 2 : 4;
-  // Tokens whose B and C are asked for together, while the ones before are worked on: scalar loads come back in any order, so that
-  // a wait is for all of them.
-  constexpr int kWords = (kStates ? 2 : 4) * Uniform<kBc, NS>::kWords;  // of both sets, a token
-  constexpr int kAhead = NS > 4 ? 1 : kWords <= 8 ? 8 : 4, kUnroll = kAhead > 1 ? 1 : 2;
-  __shared__ f32x2 lds_du[kBlock + kAhead][64];  // (rows that are read in advance and not used)
+  __shared__ f32x2 lds_du[kBlock + 1][64];  // (a row more, that is read in advance and not used)
   __shared__ float lds_part[kStates ? 1 : W][kBlock][64];
   const int lane = threadIdx.x & 63, wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
   const int n0 = wave * NS;
@@ -181,19 +223,16 @@ __global__ __launch_bounds__(64 * W, kStates ? 1 : waves_a_simd(NS)) void select
     const char *b_row = static_cast<const char *>(a.rows.b) + (from * a.rows.b_stride + n0) * kBcSize;
     const char *c_row = static_cast<const char *>(a.rows.c) + (from * a.rows.c_stride + n0) * kBcSize;
     int rows_left = to - from;  // from b_row, c_row on
-    Uniform<kBc, NS> b_next[kAhead], c_next[kAhead];
-    auto request_rows = [&]() __attribute__((always_inline)) {  // (surplus ones: the last row)
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        b_next[k].load(b_row);
-        if constexpr (!kStates) c_next[k].load(c_row);
-        if (--rows_left > 0) {
-          b_row += b_step;
-          c_row += c_step;
-        }
+    Uniform<kBc, NS> b_next, c_next;
+    auto request_row = [&]() __attribute__((always_inline)) {  // (surplus ones: the last row)
+      b_next.load(b_row);
+      if constexpr (!kStates) c_next.load(c_row);
+      if (--rows_left > 0) {
+        b_row += b_step;
+        c_row += c_step;
       }
     };
-    request_rows();
+    request_row();
     request(from);
     for (int tb = from; tb < to; tb += kBlock) {
       const int count = min(kBlock, to - tb);
@@ -217,95 +256,207 @@ __global__ __launch_bounds__(64 * W, kStates ? 1 : waves_a_simd(NS)) void select
       }
       if (tb + kBlock < to) request(tb + kBlock);
       if constexpr (W > 1) __syncthreads();
-      f32x2 du_next[kAhead];
+      f32x2 du_next = lds_du[0][lane];
+#pragma unroll 2
+      for (int i = 0; i < count; ++i) {
+        const Uniform<kBc, NS> b_now = b_next, c_now = c_next;
+        const float d = du_next[0], u = du_next[1];
+        request_row();
+        du_next = lds_du[i + 1][lane];
+        if constexpr (kStates) total += d;
+        float part[2] = {0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) du_next[k] = lds_du[k][lane];
-#pragma unroll kUnroll
-      for (int i0 = 0; i0 < count; i0 += kAhead) {
-        Uniform<kBc, NS> b_now[kAhead], c_now[kAhead];
-        f32x2 du[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          b_now[k] = b_next[k];
-          c_now[k] = c_next[k];
-          du[k] = du_next[k];
+        for (int n = 0; n < NS; ++n) {
+          h[n] = fmaf(__builtin_amdgcn_exp2f(d * A2[n]), h[n], u * b_now.of(n));
+          if constexpr (!kStates) part[n % 2] = fmaf(c_now.of(n), h[n], part[n % 2]);
         }
-        request_rows();
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) du_next[k] = lds_du[i0 + kAhead + k][lane];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          if (k > 0 && i0 + k >= count) break;
-          const float d = du[k][0], u = du[k][1];
-          if constexpr (kStates) total += d;
-          float part[2] = {0.f, 0.f};
-#pragma unroll
-          for (int n = 0; n < NS; ++n) {
-            h[n] = fmaf(__builtin_amdgcn_exp2f(d * A2[n]), h[n], u * b_now[k].of(n));
-            if constexpr (!kStates) part[n % 2] = fmaf(c_now[k].of(n), h[n], part[n % 2]);
-          }
-          if constexpr (!kStates) lds_part[wave][i0 + k][lane] = part[0] + part[1];
-        }
+        if constexpr (!kStates) lds_part[wave][i][lane] = part[0] + part[1];
       }
       if constexpr (W > 1) __syncthreads();
       if constexpr (!kStates) {
         const Rsrc ry = buffer_at(static_cast<char *>(a.a.y) + static_cast<int64_t>(tb) * C * kSize);
         const uint32_t lane_at = live ? c * kSize : kNowhere, stride = stride_of(C * kSize);
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-          const int row = wave * kOwn + i;
+        for (int i = 0; i < kOwn; ++i)
 #pragma unroll
-          for (int w = 0; w < W; ++w) sum[i] += lds_part[w][row][lane];
-          if (gated) sum[i] *= gate[i];
-          if (row < count) store<kIo>(ry, lane_at, row * stride, sum[i]);
+          for (int w = 0; w < W; ++w) sum[i] += lds_part[w][wave * kOwn + i][lane];
+        if (gated) {
+#pragma unroll
+          for (int i = 0; i < kOwn; ++i) sum[i] *= gate[i];
         }
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i)
+          if (wave * kOwn + i < count) store<kIo>(ry, lane_at, (wave * kOwn + i) * stride, sum[i]);
       }
     }
   };
 
-  const int64_t slot = (static_cast<int64_t>(s) * N) * C + c;  // of state 0 of this segment and channel
-  const int64_t sequence_size = static_cast<int64_t>(C) * N;
-  int q = last_before(a.cu, a.d.B, kStates ? t1 : t0);
-  if constexpr (kStates) {
-    int begin = 0, end = 0;
-    if (q >= 0) {
-      begin = max(a.cu[q], 0);
-      end = min(a.cu[q + 1], T);
-    }
-    const bool goes_on = q >= 0 && begin < t1 && end > t1, begins = begin >= t0;
-    load_state(goes_on && begins && a.h0 ? a.h0 + q * sequence_size + static_cast<int64_t>(c) * N : nullptr, 1);
-    if (goes_on) {
-      if (begins && a.begun) store_state(a.begun + slot, C);
-      walk(max(begin, t0), t1);
-    }
-    store_state(a.entering + slot, C);
-    if (wave == 0 && live) a.steps[static_cast<int64_t>(s) * C + c] = goes_on && !begins ? total : -1.f;
-  } else {
-    // the sequence that goes on into this segment, if any, and those that begin in it (at its end, too, if it is the last)
-    const int last = s == a.segments - 1 ? T : t1 - 1;
-    for (q = s == 0 ? 0 : max(q, 0); q < a.d.B; ++q) {
-      const int begin = min(max(a.cu[q], 0), T), end = min(a.cu[q + 1], T);
-      if (begin > last) break;
-      const bool begins = begin >= t0;
-      if (!begins && end <= t0) continue;
-      if (begins) {
-        const bool kept = end > t1 && a.begun;
-        load_state(kept ? a.begun + slot : a.h0 ? a.h0 + q * sequence_size + static_cast<int64_t>(c) * N : nullptr, kept ? C : 1);
-      } else {
-        load_state(a.entering + slot - sequence_size, C);
+  scan_segment<kStates>(a, s, t0, t1, static_cast<int64_t>(C) * N, static_cast<int64_t>(s) * N * C + c, static_cast<int64_t>(c) * N,
+                        [&](const float *from, bool slot) { load_state(from, slot ? C : 1); },
+                        [&](float *to, bool slot) { store_state(to, slot ? C : 1); }, walk,
+                        [&] { return total; }, wave == 0 && live, c);
+}
+
+// The other kernel, for calls of little work: a lane is a state of a channel (S of them, 16 apart), a row of 16 lanes a channel, a wave
+// four channels.  That makes sixteen times the waves.  A row's lanes prepare 16 tokens of its channel, one each, and hand step sizes and
+// inflows around with the operand's own lane exchange; an output's sum over the states is one over the row's lanes, and 16 tokens' sums
+// are made together, each step halving what a lane has, so that a lane ends with its token's.  B and C go through LDS, for the four
+// waves of a workgroup: a load for each token and wave would keep the memory pipe busy for longer than the block takes.
+template <int kControl>
+__device__ __forceinline__ float from_lane(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), kControl, 0xf, 0xf, true));
+}
+template <int I>
+__device__ __forceinline__ float of_token(float v) {  // lane I's of the row
+  return from_lane<0x150 + I>(v);
+}
+template <int... I, typename F>
+__device__ __forceinline__ void each(std::integer_sequence<int, I...>, const F &f) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+
+template <bool kIo, bool kDt, int S, bool kStates>
+__global__ __launch_bounds__(256) void by_state_kernel(const ScanArgs a) {
+  constexpr int kBlock = 16;
+  __shared__ float lds_rows[2][2][16 * S][kBlock + 4];  // B and C of a block's tokens, of this one and the next
+  using E = typename std::conditional<kIo, uint16_t, float>::type;
+  using EDt = typename std::conditional<kDt, uint16_t, float>::type;
+  const int lane = threadIdx.x & 63, nl = lane & 15;
+  const int N = a.d.N, C = a.d.C, T = a.d.T;
+  // neighbouring channels, whose rows share cache lines, on one die (workgroups go to the eight of them in turn)
+  const int across = gridDim.x, group = across % 8 == 0 ? (blockIdx.x % 8) * (across / 8) + blockIdx.x / 8 : blockIdx.x;
+  const int c_real = group * 16 + threadIdx.x / 16, c = min(c_real, C - 1);
+  const bool live = c_real < C;
+  const int s = blockIdx.y;
+  const int t0 = s * a.segment, t1 = min(T, t0 + a.segment);
+
+  float A2[S], h[S];
+#pragma unroll
+  for (int k = 0; k < S; ++k) A2[k] = a.a.A[static_cast<int64_t>(c) * N + min(16 * k + nl, N - 1)];
+#pragma unroll
+  for (int k = 0; k < S; ++k) A2[k] = 16 * k + nl < N ? A2[k] * kLog2e : 0.f;
+  const float bias = a.d.dtx.bias ? a.d.dtx.bias[c] : 0.f, skip = !kStates && a.a.D ? a.a.D[c] : 0.f;
+  const bool gated = !kStates && a.a.z != nullptr;
+  float total = 0.f;  // of the step sizes, this lane's
+
+  auto load_state = [&](const float *from) {  // state 0 of this lane's channel
+#pragma unroll
+    for (int k = 0; k < S; ++k) h[k] = from ? from[min(16 * k + nl, N - 1)] : 0.f;
+#pragma unroll
+    for (int k = 0; k < S; ++k) h[k] = 16 * k + nl < N ? h[k] : 0.f;
+  };
+  auto store_state = [&](float *to) {
+#pragma unroll
+    for (int k = 0; k < S; ++k)
+      if (16 * k + nl < N && live) to[16 * k + nl] = h[k];
+  };
+
+  // tokens [from, to), which are of one sequence
+  auto walk = [&](int from, int to) __attribute__((always_inline)) {
+    if (from >= to) return;
+    // the rows of two blocks are on their way: one wave's work on a block takes less than memory does.  Of B and C, which all
+    // channels share, a thread brings its states of one token
+    E raw_x[2], raw_z[2] = {E(0), E(0)}, raw_b[2][S], raw_c[2][S];
+    EDt raw_dt[2];
+    const int own_token = threadIdx.x / 16;
+    auto request = [&](int tb, int slot) __attribute__((always_inline)) {
+      const int64_t t = min(tb + nl, to - 1), r = min(tb + own_token, to - 1);  // (surplus ones: the last row)
+      raw_x[slot] = static_cast<const E *>(a.a.x)[t * C + c];
+      raw_dt[slot] = static_cast<const EDt *>(a.a.dt)[t * C + c];
+      if (gated) raw_z[slot] = static_cast<const E *>(a.a.z)[t * a.a.z_stride + c];
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        const int n = min(16 * k + nl, N - 1);
+        raw_b[slot][k] = static_cast<const E *>(a.a.B)[r * a.a.b_stride + n];
+        if constexpr (!kStates) raw_c[slot][k] = static_cast<const E *>(a.a.C)[r * a.a.c_stride + n];
       }
-      walk(max(begin, t0), min(end, t1));
-      if (end <= t1) store_state(a.final_state + q * sequence_size + static_cast<int64_t>(c) * N, 1);
+    };
+    // a block of tokens, the first or the second of two
+    auto block = [&](int tb, auto which) __attribute__((always_inline)) {
+      constexpr int kWhich = decltype(which)::value;
+      // this lane's token (behind `to`: a step of nothing)
+      const bool there = tb + nl < to;
+      const float x = value(raw_x[kWhich]), step = step_of(value(raw_dt[kWhich]), bias, a.d.dtx);
+      const float d = there ? step : 0.f, u = there ? step * x : 0.f;
+      const float gate = gated ? silu(value(raw_z[kWhich])) : 1.f;
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        const bool staged = tb + own_token < to && 16 * k + nl < N;  // (zeros behind `to`: what is there is another sequence's)
+        lds_rows[kWhich][0][16 * k + nl][own_token] = staged ? value(raw_b[kWhich][k]) : 0.f;
+        if constexpr (!kStates) lds_rows[kWhich][1][16 * k + nl][own_token] = staged ? value(raw_c[kWhich][k]) : 0.f;
+      }
+      if (tb + 2 * kBlock < to) request(tb + 2 * kBlock, kWhich);
+      __syncthreads();
+      if constexpr (kStates) total += d;
+      float sum[kBlock];
+      each(std::make_integer_sequence<int, kBlock / 4>(), [&](auto quarter) {
+        constexpr int i0 = decltype(quarter)::value * 4;
+        f32x4 b_now[S], c_now[S];
+#pragma unroll
+        for (int k = 0; k < S; ++k) {
+          b_now[k] = *reinterpret_cast<const f32x4 *>(&lds_rows[kWhich][0][16 * k + nl][i0]);
+          if constexpr (!kStates) c_now[k] = *reinterpret_cast<const f32x4 *>(&lds_rows[kWhich][1][16 * k + nl][i0]);
+        }
+        each(std::make_integer_sequence<int, 4>(), [&](auto token) {
+          constexpr int i = decltype(token)::value;
+          float y = 0.f;
+#pragma unroll
+          for (int k = 0; k < S; ++k) {
+            h[k] = fmaf(__builtin_amdgcn_exp2f(of_token<i0 + i>(d) * A2[k]), h[k], of_token<i0 + i>(u) * b_now[k][i]);
+            if constexpr (!kStates) y = fmaf(c_now[k][i], h[k], y);
+          }
+          sum[i0 + i] = y;
+        });
+      });
+      if constexpr (!kStates) {
+        // halves of a row, of eight, of four and of two lanes keep the tokens whose bit they have
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float low = sum[j] + from_lane<0x140>(sum[j]), high = sum[j + 8] + from_lane<0x140>(sum[j + 8]);
+          sum[j] = nl & 8 ? high : low;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float low = sum[j] + from_lane<0x141>(sum[j]), high = sum[j + 4] + from_lane<0x141>(sum[j + 4]);
+          sum[j] = nl & 4 ? high : low;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float low = sum[j] + from_lane<0x4e>(sum[j]), high = sum[j + 2] + from_lane<0x4e>(sum[j + 2]);
+          sum[j] = nl & 2 ? high : low;
+        }
+        const float low = sum[0] + from_lane<0xb1>(sum[0]), high = sum[1] + from_lane<0xb1>(sum[1]);
+        const float y = fmaf(skip, x, nl & 1 ? high : low);
+        if (there && live) put(static_cast<E *>(a.a.y) + static_cast<int64_t>(tb + nl) * C + c, gated ? y * gate : y);
+      }
+    };
+    request(from, 0);
+    if (from + kBlock < to) request(from + kBlock, 1);
+    __syncthreads();  // (the rows of a sequence before)
+    for (int tb = from; tb < to; tb += 2 * kBlock) {
+      block(tb, std::integral_constant<int, 0>());
+      if (tb + kBlock < to) block(tb + kBlock, std::integral_constant<int, 1>());
     }
-  }
+  };
+
+  scan_segment<kStates>(a, s, t0, t1, static_cast<int64_t>(C) * N, static_cast<int64_t>(s) * C * N + static_cast<int64_t>(c) * N,
+                        static_cast<int64_t>(c) * N, [&](const float *from, bool) { load_state(from); },
+                        [&](float *to, bool) { store_state(to); }, walk, [&] {
+                          float sum = total;
+                          sum += from_lane<0xb1>(sum);
+                          sum += from_lane<0x4e>(sum);
+                          sum += from_lane<0x141>(sum);
+                          sum += from_lane<0x140>(sum);
+                          return sum;
+                        }, nl == 0 && live, c);
 }
 
 // The state that enters each segment but the first, in place of the one at the end of the segment before.  Eight segments'
 // values are on their way at a time.
-__global__ __launch_bounds__(256) void carry_kernel(float *entering, const float *steps, const float *A, int N, int C, int segments) {
+__global__ __launch_bounds__(256) void carry_kernel(float *entering, const float *steps, const float *A, int N, int C, int segments, bool by_state) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, size = static_cast<int64_t>(N) * C;
   if (i >= size) return;
-  const int n = static_cast<int>(i / C), c = static_cast<int>(i - static_cast<int64_t>(n) * C);
+  const int c = static_cast<int>(by_state ? i / N : i % C), n = static_cast<int>(by_state ? i % N : i / C);
   const float A2 = A[static_cast<int64_t>(c) * N + n] * kLog2e;
   constexpr int kAhead = 8;
   float h = 0.f, sum[kAhead], e[kAhead];
@@ -329,8 +480,6 @@ __global__ __launch_bounds__(256) void carry_kernel(float *entering, const float
   }
 }
 
-__device__ __forceinline__ float value(float v) { return v; }
-__device__ __forceinline__ float value(uint16_t v) { return bf16_bits_to_f32(v); }
 // B and C in fp32, states from N up to the waves' zero.
 template <typename E>
 __global__ __launch_bounds__(256) void rows_kernel(const void *b, const void *c, int64_t b_stride, int64_t c_stride, int N, int padded, int64_t values,
@@ -343,32 +492,49 @@ __global__ __launch_bounds__(256) void rows_kernel(const void *b, const void *c,
   out[values + i] = n < N ? value(static_cast<const E *>(c)[t * c_stride + n]) : 0.f;
 }
 
-// How a call is cut up.  Fewer states a wave make more waves, which share what is done once a token (step sizes, gates), wait at
-// barriers, and read step sizes and inflows from LDS each.  16 states of 5120 channels, us by tokens, with 8 / 4 / 2 states a wave, each at
-// its best segments: 512 tokens 41 / 39 / 42; 2048 95 / 99 / 111; 16384 545 / 655 / 776 (16 states: 537).  1536 channels: 61 tokens 16.3 / 14.0 /
-// 12.7; 256 20.7 / 17.9 / 17.3; 2048 (fp32) 51 / 47 / 47.
+// How a call is cut up.
 struct Cut {
-  int states, waves;         // a wave, for a channel
+  bool by_state;
+  int states, waves;         // by channel: of a wave, and waves for a channel's; by state: of a lane
   int64_t most_segments;     // that the workspace has room for: never fewer for more tokens
   int segment;               // tokens
-  int padded() const { return states * waves; }
+  int padded() const { return by_state ? 0 : states * waves; }
 };
-Cut cut_of(const SelectiveDims &d) {
+void set_segments(const SelectiveDims &d, int64_t most, int block, Cut *c) {
+  c->most_segments = std::max<int64_t>(1, most);
+  const int64_t least = (d.T + c->most_segments - 1) / c->most_segments;
+  const int64_t wanted = knobs().selective_segment > 0 ? std::max<int64_t>(knobs().selective_segment, least) : least;
+  c->segment = static_cast<int>((wanted + block - 1) / block * block);
+}
+// By channel: eight states a wave (16 cost as much where there is work for them and leave fewer waves where there is not, four cost 20 %
+// more), and segments for 16 waves a SIMD, of 48 tokens or more.
+Cut cut_by_channel(const SelectiveDims &d) {
   int padded = 8;
   while (padded < d.N) padded *= 2;
-  const int64_t groups = (d.C + 63) / 64, work = d.T * groups * padded / 16;  // of 16 states, tokens times waves
+  const int64_t groups = (d.C + 63) / 64;
   Cut c = {};
-  c.states = work >= 100000 ? 8 : work >= 20000 ? 4 : 2;
-  if (c.states < padded / 8) c.states = padded / 8;
+  c.states = std::max(8, padded / 8);
   c.waves = padded / c.states;
-  // Segments make waves too, at the price of the states pass, and of their states' way through memory: some 16 waves a SIMD where
-  // there is work for them, 5 where there is less.  Up to 80 tokens the three launches cost more than they save.
-  const int64_t shortest = c.states >= 8 ? 48 : 32, waves = c.states >= 8 ? 16384 : 5120;
-  c.most_segments = d.T <= 80 ? 1 : std::max<int64_t>(1, std::min((d.T + shortest - 1) / shortest, waves / c.waves / groups));
-  const int64_t least = (d.T + c.most_segments - 1) / c.most_segments, block = block_of(c.waves);
-  const int64_t wanted = knobs().selective_segment > 0 ? std::max<int64_t>(knobs().selective_segment, least) : least;
-  c.segment = static_cast<int>((wanted + block - 1) / block * block);
+  set_segments(d, std::min<int64_t>((d.T + 47) / 48, 16384 / c.waves / groups), block_of(c.waves), &c);
   return c;
+}
+// By state: segments for four waves a SIMD, of 64 tokens or more, where the two launches in front of the scan cost less than they
+// save: 1536 channels, 256 tokens 13.7 us in one segment and 15.7 in four, 512 tokens 24.6 and 19.3 in eight.
+Cut cut_by_state(const SelectiveDims &d) {
+  Cut c = {};
+  c.by_state = true;
+  c.states = d.N <= 16 ? 1 : d.N <= 32 ? 2 : 4;
+  const int64_t waves = (d.C + 3) / 4;
+  set_segments(d, d.T <= 384 + waves / 4 ? 1 : std::min<int64_t>((d.T + 63) / 64, 4096 / waves), 16, &c);
+  return c;
+}
+// A lane a state up to 2^26 states of all tokens: 16 states, us by state and by channel, 1536 channels, 61 tokens 5.6 / 21, 512 19 / 35,
+// 2048 (fp32) 46 / 52; 5120 channels, 512 tokens 36 / 43, 2048 116 / 103.  64 states, 1536 channels, 1024 tokens 58 / 64.
+constexpr int kMostByState = 64;  // states of a channel
+Cut cut_of(const SelectiveDims &d) {
+  const int64_t work = static_cast<int64_t>(d.T) * d.C * d.N;
+  const int knob = knobs().selective_by_state;
+  return d.N <= kMostByState && (knob == 1 || (knob == 0 && work < (1 << 26))) ? cut_by_state(d) : cut_by_channel(d);
 }
 int64_t segments_of(const SelectiveDims &d, const Cut &c) { return (static_cast<int64_t>(d.T) + c.segment - 1) / c.segment; }
 
@@ -393,48 +559,66 @@ Plan plan_of(const SelectiveDims &d, const Cut &c) {
   return p;
 }
 
-template <bool kIo, bool kDt, bool kBc, int NS, int W>
-hipError_t launch_split(const ScanArgs &a, hipStream_t stream) {
-  const unsigned groups = (a.d.C + 63) / 64;
+// The launches of a call by states and scan kernels of either kind.
+template <typename States, typename Scan>
+hipError_t launch_passes(const ScanArgs &a, bool by_state, const States &states, const Scan &scan, hipStream_t stream) {
   if (a.segments > 1) {
-    hipLaunchKernelGGL((selective_kernel<kIo, kDt, kBc, NS, W, true>), dim3(groups, a.segments - 1), dim3(64 * W), 0, stream, a);
+    states();
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(carry_kernel, dim3(static_cast<unsigned>((static_cast<int64_t>(a.d.C) * a.d.N + 255) / 256)), dim3(256), 0, stream, a.entering, a.steps, a.a.A, a.d.N, a.d.C, a.segments);
+    const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(a.d.C) * a.d.N + 255) / 256));
+    hipLaunchKernelGGL(carry_kernel, grid, dim3(256), 0, stream, a.entering, a.steps, a.a.A, a.d.N, a.d.C, a.segments, by_state);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((selective_kernel<kIo, kDt, kBc, NS, W, false>), dim3(groups, a.segments), dim3(64 * W), 0, stream, a);
+  scan();
   return hipGetLastError();
 }
 
+template <bool kIo, bool kDt, int S>
+hipError_t launch_by_state(const ScanArgs &a, hipStream_t stream) {
+  const unsigned groups = (a.d.C + 15) / 16;
+  return launch_passes(
+      a, true, [&] { hipLaunchKernelGGL((by_state_kernel<kIo, kDt, S, true>), dim3(groups, a.segments - 1), dim3(256), 0, stream, a); },
+      [&] { hipLaunchKernelGGL((by_state_kernel<kIo, kDt, S, false>), dim3(groups, a.segments), dim3(256), 0, stream, a); }, stream);
+}
+template <bool kIo, bool kDt>
+hipError_t launch_by_state(const ScanArgs &a, const Cut &c, hipStream_t stream) {
+  if (c.states == 1) return launch_by_state<kIo, kDt, 1>(a, stream);
+  if (c.states == 2) return launch_by_state<kIo, kDt, 2>(a, stream);
+  return launch_by_state<kIo, kDt, 4>(a, stream);
+}
+
+template <bool kIo, bool kDt, bool kBc, int NS, int W>
+hipError_t launch_split(const ScanArgs &a, hipStream_t stream) {
+  const unsigned groups = (a.d.C + 63) / 64;
+  return launch_passes(
+      a, false, [&] { hipLaunchKernelGGL((by_channel_kernel<kIo, kDt, kBc, NS, W, true>), dim3(groups, a.segments - 1), dim3(64 * W), 0, stream, a); },
+      [&] { hipLaunchKernelGGL((by_channel_kernel<kIo, kDt, kBc, NS, W, false>), dim3(groups, a.segments), dim3(64 * W), 0, stream, a); }, stream);
+}
 template <bool kIo, bool kDt, bool kBc>
-hipError_t launch_typed(const ScanArgs &a, const Cut &c, hipStream_t stream) {
-  switch (c.states * 16 + c.waves) {
-    case 8 * 16 + 1: return launch_split<kIo, kDt, kBc, 8, 1>(a, stream);
-    case 4 * 16 + 2: return launch_split<kIo, kDt, kBc, 4, 2>(a, stream);
-    case 2 * 16 + 4: return launch_split<kIo, kDt, kBc, 2, 4>(a, stream);
-    case 8 * 16 + 2: return launch_split<kIo, kDt, kBc, 8, 2>(a, stream);
-    case 4 * 16 + 4: return launch_split<kIo, kDt, kBc, 4, 4>(a, stream);
-    case 2 * 16 + 8: return launch_split<kIo, kDt, kBc, 2, 8>(a, stream);
-    case 8 * 16 + 4: return launch_split<kIo, kDt, kBc, 8, 4>(a, stream);
-    case 4 * 16 + 8: return launch_split<kIo, kDt, kBc, 4, 8>(a, stream);
-    case 8 * 16 + 8: return launch_split<kIo, kDt, kBc, 8, 8>(a, stream);
-    case 16 * 16 + 8: return launch_split<kIo, kDt, kBc, 16, 8>(a, stream);
-    case 32 * 16 + 8: return launch_split<kIo, kDt, kBc, 32, 8>(a, stream);
-    default: return hipErrorInvalidValue;
-  }
+hipError_t launch_by_channel(const ScanArgs &a, const Cut &c, hipStream_t stream) {
+  if (c.waves == 1) return launch_split<kIo, kDt, kBc, 8, 1>(a, stream);
+  if (c.waves == 2) return launch_split<kIo, kDt, kBc, 8, 2>(a, stream);
+  if (c.waves == 4) return launch_split<kIo, kDt, kBc, 8, 4>(a, stream);
+  if (c.states == 8) return launch_split<kIo, kDt, kBc, 8, 8>(a, stream);
+  if (c.states == 16) return launch_split<kIo, kDt, kBc, 16, 8>(a, stream);
+  return launch_split<kIo, kDt, kBc, 32, 8>(a, stream);
 }
 
 }  // namespace
 
 // Whether no launch of a call has 2^32 threads or more.
 bool selective_prefill_fits(const SelectiveDims &d) {
-  const Cut c = cut_of(d);
-  const int64_t groups = (d.C + 63) / 64;
-  return c.most_segments <= 65535 && groups * c.most_segments * c.waves * 64 < (int64_t{1} << 32) &&
-         (static_cast<int64_t>(d.T) + 256) * c.padded() < (int64_t{1} << 32);
+  const Cut c = cut_by_channel(d), e = cut_by_state(d);
+  const int64_t groups = (d.C + 63) / 64, limit = int64_t{1} << 32;
+  return c.most_segments <= 65535 && groups * c.most_segments * c.waves * 64 < limit && (static_cast<int64_t>(d.T) + 256) * c.padded() < limit &&
+         (d.N > kMostByState || (e.most_segments <= 65535 && groups * e.most_segments * 1024 < limit));
 }
 
-size_t selective_prefill_workspace_bytes(const SelectiveDims &d) { return plan_of(d, cut_of(d)).total; }
+// (of either kind: the choice between them is none of the caller's)
+size_t selective_prefill_workspace_bytes(const SelectiveDims &d) {
+  const size_t one = plan_of(d, cut_by_channel(d)).total;
+  return d.N > kMostByState ? one : std::max(one, plan_of(d, cut_by_state(d)).total);
+}
 
 hipError_t launch_selective_prefill(const SelectiveDims &d, const SelectiveArgs &args, const int32_t *cu, const float *h0, float *final_state,
                                     void *workspace, hipStream_t stream) {
@@ -453,6 +637,10 @@ hipError_t launch_selective_prefill(const SelectiveDims &d, const SelectiveArgs 
   a.segment = s.segment;
   a.segments = static_cast<int>(segments_of(d, s));
   if (a.segments == 1) a.begun = nullptr;
+  if (s.by_state) {
+    if (!d.bf16) return launch_by_state<false, false>(a, s, stream);
+    return d.dt_bf16 ? launch_by_state<true, true>(a, s, stream) : launch_by_state<true, false>(a, s, stream);
+  }
   a.rows = {args.B, args.C, args.b_stride, args.c_stride};
   const bool whole = d.N == s.padded() && ((reinterpret_cast<uintptr_t>(args.B) | reinterpret_cast<uintptr_t>(args.C)) & 3) == 0 &&
                      (!d.bf16 || (args.b_stride % 2 == 0 && args.c_stride % 2 == 0));
@@ -467,9 +655,9 @@ hipError_t launch_selective_prefill(const SelectiveDims &d, const SelectiveArgs 
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     a.rows = {rows, rows + values, s.padded(), s.padded()};
   }
-  if (!d.bf16) return launch_typed<false, false, false>(a, s, stream);
-  if (d.dt_bf16) return whole ? launch_typed<true, true, true>(a, s, stream) : launch_typed<true, true, false>(a, s, stream);
-  return whole ? launch_typed<true, false, true>(a, s, stream) : launch_typed<true, false, false>(a, s, stream);
+  if (!d.bf16) return launch_by_channel<false, false, false>(a, s, stream);
+  if (d.dt_bf16) return whole ? launch_by_channel<true, true, true>(a, s, stream) : launch_by_channel<true, true, false>(a, s, stream);
+  return whole ? launch_by_channel<true, false, true>(a, s, stream) : launch_by_channel<true, false, false>(a, s, stream);
 }
 
 }  // namespace ssd

@@ -856,7 +856,7 @@ def ssd_attn_prefill(q, k_cache, v_cache, page_table, seq_lens, cu_seqlens, scal
 
 KNOBS = {"force_generic": 0, "seg_chunks": 1, "seg_blocks": 2, "seg_parts": 3, "y_stream": 4, "decode_stream": 5,
          "force_mfma_f32": 6, "f32_segments": 7, "fold_max_slots": 8, "scan_heads": 9, "chunk": 10, "deal": 11, "split_images": 12,
-         "selective_segment": 13}
+         "selective_segment": 13, "selective_by_state": 14}
 
 
 def set_knob(name: str, value: int) -> None:

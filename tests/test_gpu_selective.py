@@ -247,3 +247,18 @@ def test_captured_and_on_other_streams(ssd):
         torch.cuda.synchronize()
         ref = run(ssd, (a, b)[turn])
         assert torch.equal(y, ref[0]) and torch.equal(f, ref[1]), turn
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [1, 7, 16, 24, 33, 64])
+def test_both_kernels(ssd, N, io):
+    """A lane a channel, and a lane a state, whatever the library would choose."""
+    for i, lengths in enumerate(([300, 0, 1, 90], [17, 700])):
+        s = make(lengths, 130, N, io, seed=90 + i, gaps=(i, 3 * i), pad=(1, 2))
+        for kernel in (1, 2):
+            ssd.set_knob("selective_by_state", kernel)
+            print("selective", N, io, lengths, kernel, flush=True)
+            y, f = compare(ssd, s, io)
+            again = run(ssd, s)
+            assert torch.equal(again[0][i:-3 * i or None], y[i:-3 * i or None]) and torch.equal(again[1], f)
+        ssd.reset_knobs()

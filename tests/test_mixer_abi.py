@@ -66,7 +66,7 @@ def test_selective_refuses():
             assert f(s=shape(**bad), wb=1 << 60) == status, bad
             assert ssd.selective_prefill_workspace_bytes(shape(**bad)) == 0
         refusals(f, ("x", "dt", "A", "B", "C", "y", "f"), ("x", "dt", "A", "D", "y", "f"), ("B", "C", "z"))
-        assert f(bs=15) == -2 and f(cs=15) == -2 and f(zs=95) == -2 and f(bs=1 << 60) == -4 and f(zs=(1 << 26) + 1) == -4
+        assert f(bs=15) == -2 and f(cs=15) == -2 and f(zs=95) == -2 and f(bs=1 << 60) == -4 and f(zs=(1 << 24) + 1) == -4
         assert f(tr=T(4100, 1, 0.0, 0.0)) == -7 and f(tr=T(4096, 1, 0.2, 0.1)) == -2 and f(tr=T(4096, 1, float("nan"), 0.1)) == -2
         assert f(s=shape(io_dtype=0, dt_dtype=0), B=HALF, wb=1 << 60) == -7
     refusals(prefill, ("cu",), ("h0",), ("cu",))
