@@ -343,8 +343,9 @@ SSD_API ssd_status ssd_conv1d_step(int32_t batch, int32_t ksize, int32_t io_dtyp
  *                     must not overlap it otherwise.  A sequence without a token keeps
  *                     its cache
  * Everything else, and every bit of the outputs, is as for ssd_conv1d_prefill of
- * each sequence by itself.  A call of 2^32 threads or more (one a channel and four
- * tokens, or a channel and sequence, at most) is refused with SSD_ERR_SHAPE.
+ * each sequence by itself.  u must not overlap z0..z2.  A call of more than some 2^38
+ * tokens times channels, or 2^31 sequences times channels, is refused with
+ * SSD_ERR_SHAPE.
  * Errors: SSD_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _HIP.
  */
 SSD_API ssd_status ssd_conv1d_varlen(int32_t batch, int32_t tokens, int32_t ksize, int32_t io_dtype,
@@ -364,7 +365,7 @@ SSD_API ssd_status ssd_conv1d_varlen(int32_t batch, int32_t tokens, int32_t ksiz
  *   x, y              (tokens, channels) io dtype, dense; y must not overlap an input
  *   dt                (tokens, channels) of dt_dtype (SSD_F32, or io_dtype), dense; the map
  *                     of dt_transform is applied as for ssd_prefill_dt (dt_bias is
- *                     (channels)); dt_transform may be NULL: dt is the step size
+ *                     (channels)); dt_transform may be NULL: dt is the step size, >= 0
  *   A                 (channels, dstate) fp32, <= 0
  *   B, C              (tokens, dstate) io dtype, rows B_stride, C_stride >= dstate elements
  *                     apart (slices of one projection's output), aligned to their elements

@@ -14,12 +14,16 @@
 //
 // The caches are left by threads of their own, one a sequence and channel: in the same launch, or, where they are updated in
 // place, in one behind it (a sequence's first run reads what its last would write).
+#include <algorithm>
+
 #include "ssd_conv.hpp"
 
 namespace ssd {
 namespace {
 
-constexpr int kRunShort = 4;  // tokens a thread, at least
+// Tokens a thread, at least: few tokens are worth more threads, and a launch takes 2^32.
+constexpr int64_t kMostThreads = int64_t{1} << 31;
+int shortest_run(int T, int64_t groups) { return static_cast<int>(std::max<int64_t>(4, (T * groups + kMostThreads - 1) / kMostThreads)); }
 
 struct VarlenArgs {
   const void *u;
@@ -231,7 +235,7 @@ int resident_blocks() {
 template <typename Io, int V, int K>
 hipError_t varlen_launch(VarlenArgs a, hipStream_t stream) {
   const int groups = a.C / V;
-  a.run = choose_run(a.T, groups, K, resident_blocks<Io, V, K>(), kRunShort);
+  a.run = choose_run(a.T, groups, K, resident_blocks<Io, V, K>(), shortest_run(a.T, groups));
   const auto blocks = [](int64_t threads) { return static_cast<unsigned>((threads + kConvThreads - 1) / kConvThreads); };
   a.filter_blocks = blocks(static_cast<int64_t>((a.T + a.run - 1) / a.run) * groups);
   const unsigned cache_blocks = a.state_out ? blocks(static_cast<int64_t>(a.B) * a.C) : 0;
@@ -255,10 +259,8 @@ hipError_t varlen_typed(const VarlenArgs &a, bool pairs, hipStream_t stream) {
 
 }  // namespace
 
-// Whether the threads of a call, one a channel and run or sequence at most, are no more than a launch takes.
-bool conv_varlen_fits(int B, int T, int64_t C) {
-  return (static_cast<int64_t>(T + kRunShort - 1) / kRunShort + B) * C <= (int64_t{1} << 32) - 3 * kConvThreads;
-}
+// Whether the threads of a call, one a channel and run, and one a channel and sequence, are no more than a launch takes.
+bool conv_varlen_fits(int B, int T, int64_t C) { return shortest_run(T, C) <= kRunMax && B * C <= kMostThreads - 3 * kConvThreads; }
 
 hipError_t launch_conv_varlen(int B, int T, int ksize, bool bf16, const int32_t *cu, const void *u, int64_t u_stride,
                               const float *w, const float *bias, const void *state_in, void *const z[3], const int width[3],

@@ -35,6 +35,8 @@ struct Rows {
   int64_t b_stride, c_stride;  // in elements
 };
 
+constexpr float kNothing = -__builtin_inff();
+
 struct ScanArgs {
   SelectiveArgs a;
   Rows rows;
@@ -42,7 +44,7 @@ struct ScanArgs {
   const float *h0;
   float *final_state;
   float *entering;   // (segments, N, C): at a segment's end (states), then the state that enters the next one (carry)
-  float *steps;      // (segments, C): sum of the step sizes; negative: the state at the end owes nothing to the segments before
+  float *steps;      // (segments, C): sum of the step sizes; kNothing: the state at the end owes nothing to the segments before
   float *begun;      // (segments, N, C): h0 of the sequence that begins in the segment and outlasts it; null: read h0
   SelectiveDims d;
   int segment;       // tokens
@@ -132,13 +134,16 @@ __device__ __forceinline__ void scan_segment(const ScanArgs &a, int s, int t0, i
     }
     save(a.entering + slot, true);
     const float sum = total();
-    if (writes_total) a.steps[static_cast<int64_t>(s) * a.d.C + c] = goes_on && !begins ? sum : -1.f;
+    if (writes_total) a.steps[static_cast<int64_t>(s) * a.d.C + c] = goes_on && !begins ? sum : kNothing;
   } else {
     // the sequence that goes on into this segment, if any, and those that begin in it (at its end, too, if it is the last)
     const int last = s == a.segments - 1 ? T : t1 - 1;
-    for (q = max(q, 0); q < a.d.B; ++q) {
-      const int begin = min(max(a.cu[q], 0), T), end = min(a.cu[q + 1], T);
+    q = max(q, 0);
+    for (int boundary = a.cu[q], next = a.cu[q + 1]; q < a.d.B; ++q) {
+      const int begin = min(max(boundary, 0), T), end = min(next, T);
       if (begin > last) break;
+      boundary = next;
+      next = a.cu[min(q + 2, a.d.B)];  // (on its way while this sequence is walked)
       const bool begins = begin >= t0, kept = begins && end > t1 && a.begun;
       if (!begins && end <= t0) continue;
       load(!begins ? a.entering + slot - size : kept ? a.begun + slot : a.h0 ? a.h0 + q * size + at : nullptr, !begins || kept);
@@ -391,6 +396,11 @@ __global__ __launch_bounds__(256) void by_state_kernel(const ScanArgs a) {
       float sum[kBlock];
       each(std::make_integer_sequence<int, kBlock / 4>(), [&](auto quarter) {
         constexpr int i0 = decltype(quarter)::value * 4;
+        if (i0 > 0 && tb + i0 >= to) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i0 + i] = 0.f;
+          return;
+        }
         f32x4 b_now[S], c_now[S];
 #pragma unroll
         for (int k = 0; k < S; ++k) {
@@ -472,7 +482,7 @@ __global__ __launch_bounds__(256) void carry_kernel(float *entering, const float
   for (int s0 = 0; s0 < segments - 1; s0 += kAhead) {
     float out[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) out[k] = h = sum[k] < 0.f ? e[k] : fmaf(__builtin_amdgcn_exp2f(sum[k] * A2), h, e[k]);
+    for (int k = 0; k < kAhead; ++k) out[k] = h = sum[k] == kNothing ? e[k] : fmaf(__builtin_amdgcn_exp2f(sum[k] * A2), h, e[k]);
     if (s0 + kAhead < segments - 1) request(s0 + kAhead);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
@@ -500,10 +510,11 @@ struct Cut {
   int segment;               // tokens
   int padded() const { return by_state ? 0 : states * waves; }
 };
-void set_segments(const SelectiveDims &d, int64_t most, int block, Cut *c) {
+// `most` segments, of `shortest` tokens or more.
+void set_segments(const SelectiveDims &d, int64_t most, int64_t shortest, int block, Cut *c) {
   c->most_segments = std::max<int64_t>(1, most);
   const int64_t least = (d.T + c->most_segments - 1) / c->most_segments;
-  const int64_t wanted = knobs().selective_segment > 0 ? std::max<int64_t>(knobs().selective_segment, least) : least;
+  const int64_t wanted = std::max<int64_t>(knobs().selective_segment > 0 ? knobs().selective_segment : shortest, least);
   c->segment = static_cast<int>((wanted + block - 1) / block * block);
 }
 // By channel: eight states a wave (16 cost as much where there is work for them and leave fewer waves where there is not, four cost 20 %
@@ -515,17 +526,20 @@ Cut cut_by_channel(const SelectiveDims &d) {
   Cut c = {};
   c.states = std::max(8, padded / 8);
   c.waves = padded / c.states;
-  set_segments(d, std::min<int64_t>((d.T + 47) / 48, 16384 / c.waves / groups), block_of(c.waves), &c);
+  set_segments(d, std::min<int64_t>((d.T + 47) / 48, 16384 / c.waves / groups), 1, block_of(c.waves), &c);
   return c;
 }
 // By state: segments for four waves a SIMD, of 64 tokens or more, where the two launches in front of the scan cost less than they
-// save: 1536 channels, 256 tokens 13.7 us in one segment and 15.7 in four, 512 tokens 24.6 and 19.3 in eight.
+// save: 1536 channels, 256 tokens 13.7 us in one segment and 15.7 in four, 512 tokens 24.6 and 19.3 in eight.  To begin a sequence
+// takes as long as some 40 tokens, so that a segment shall not hold many: 512 tokens of 32 sequences 68 us in one, 38 in eight.
 Cut cut_by_state(const SelectiveDims &d) {
   Cut c = {};
   c.by_state = true;
   c.states = d.N <= 16 ? 1 : d.N <= 32 ? 2 : 4;
   const int64_t waves = (d.C + 3) / 4;
-  set_segments(d, d.T <= 384 + waves / 4 ? 1 : std::min<int64_t>((d.T + 63) / 64, 4096 / waves), 16, &c);
+  const bool one = d.T + int64_t{40} * (d.B - 1) <= 384 + waves / 4;
+  const int64_t shortest = one ? d.T : std::min<int64_t>(64, int64_t{4} * d.T / d.B);
+  set_segments(d, std::min<int64_t>((d.T + 15) / 16, 4096 / waves), shortest, 16, &c);
   return c;
 }
 // A lane a state up to 2^26 states of all tokens: 16 states, us by state and by channel, 1536 channels, 61 tokens 5.6 / 21, 512 19 / 35,

@@ -28,27 +28,39 @@ __device__ __forceinline__ float to_float(uint16_t v) { return bf16_bits_to_f32(
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(uint16_t *p, float v) { *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
 
-// Four neighbouring values, of which the first `left` are there (all of them if kWhole); the others are zeros.
-template <bool kWhole>
-__device__ __forceinline__ void load4(const float *p, int left, float v[4]) {
-  if (kWhole) {
-    const f32x4 q = *reinterpret_cast<const f32x4 __attribute__((aligned(4))) *>(p);
+// Four neighbouring values of `n` in a row, from `at` on, of which those behind the n-th are zeros.  kWhole: they are all there.
+// Otherwise the last four of the row are taken where four from `at` are not there, and moved up.
+__device__ __forceinline__ void raw4(const float *p, float v[4]) {
+  const f32x4 q = *reinterpret_cast<const f32x4 __attribute__((aligned(4))) *>(p);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = q[k];
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = k < left ? p[k] : 0.f;
-  }
+  for (int k = 0; k < 4; ++k) v[k] = q[k];
 }
-template <bool kWhole>
-__device__ __forceinline__ void load4(const uint16_t *p, int left, float v[4]) {
+__device__ __forceinline__ void raw4(const uint16_t *p, float v[4]) {
+  const u16x4 q = *reinterpret_cast<const u16x4 __attribute__((aligned(2))) *>(p);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = to_float(q[k]);
+}
+template <bool kWhole, typename E>
+__device__ __forceinline__ void load4(const E *row, int at, int n, float v[4]) {
   if (kWhole) {
-    const u16x4 q = *reinterpret_cast<const u16x4 __attribute__((aligned(2))) *>(p);
+    raw4(row + at, v);
+  } else if (n < 4) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = to_float(q[k]);
+    for (int k = 0; k < 4; ++k) v[k] = at + k < n ? to_float(row[at + k]) : 0.f;
   } else {
+    const int from = min(at, n - 4), by = at - from;
+    raw4(row + from, v);
+    if (by >= 2) {
+      v[0] = v[2];
+      v[1] = v[3];
+    }
+    if (by & 1) {
+      v[0] = v[1];
+      v[1] = v[2];
+      v[2] = v[3];
+    }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = k < left ? to_float(p[k]) : 0.f;
+    for (int k = 0; k < 4; ++k) v[k] = at + k < n ? v[k] : 0.f;
   }
 }
 
@@ -61,17 +73,15 @@ __global__ __launch_bounds__(256) void selective_step_kernel(const StepArgs a) {
   const int c_real = i / lanes, piece = i & (lanes - 1), first = 4 * piece;
   const int c = min(c_real, C - 1);
   const bool there = c_real < C && first < N;
-  // (a lane without states reads the channel's first ones and leaves them out)
-  const int at = first < N ? first : 0, left = first < N ? N - first : 0;
   float A2[4], h[R][4], Bv[R][4], Cv[R][4], x[R], dt[R], z[R];
-  load4<kWhole>(a.a.A + static_cast<int64_t>(c) * N + at, left, A2);
+  load4<kWhole>(a.a.A + static_cast<int64_t>(c) * N, first, N, A2);
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int b = min(b0 + r, a.d.B - 1);  // (surplus ones: the last sequence, not written)
     const int64_t channel = static_cast<int64_t>(b) * C + c;
-    load4<kWhole>(a.state + channel * N + at, left, h[r]);
-    load4<kWhole>(static_cast<const E *>(a.a.B) + b * a.a.b_stride + at, left, Bv[r]);
-    load4<kWhole>(static_cast<const E *>(a.a.C) + b * a.a.c_stride + at, left, Cv[r]);
+    load4<kWhole>(a.state + channel * N, first, N, h[r]);
+    load4<kWhole>(static_cast<const E *>(a.a.B) + b * a.a.b_stride, first, N, Bv[r]);
+    load4<kWhole>(static_cast<const E *>(a.a.C) + b * a.a.c_stride, first, N, Cv[r]);
     x[r] = to_float(static_cast<const E *>(a.a.x)[channel]);
     dt[r] = to_float(static_cast<const EDt *>(a.a.dt)[channel]);
     z[r] = a.a.z ? to_float(static_cast<const E *>(a.a.z)[b * a.a.z_stride + c]) : 0.f;
@@ -97,7 +107,7 @@ __global__ __launch_bounds__(256) void selective_step_kernel(const StepArgs a) {
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (k < left) state[k] = h[r][k];
+        if (first + k < N) state[k] = h[r][k];
     }
     if (piece == 0) {
       sum = fmaf(skip, x[r], sum);

@@ -111,3 +111,26 @@ def test_captured(ssd):
         torch.cuda.synchronize()
         z, new = call(ssd, v, (64, 8), in_place=True)
         assert torch.equal(torch.cat(outs, dim=1), z) and torch.equal(state, new)
+
+
+def test_more_sequences_than_fit_lds(ssd):
+    compare(ssd, make([1, 2, 0, 5] * 400, (20, 4), 4, "bf16", seed=13, gaps=(2, 1)), (20, 4), 4, "bf16", "silu")
+    compare(ssd, make([3, 0] * 600, (5,), 3, "f32", seed=14, gaps=(0, 7)), (5,), 3, "f32", "none")
+
+
+def test_offsets_beyond_32_bits(ssd):
+    """4.4 GiB of input: rows around 2 and 4 GiB and at the end are those of the batched call on slices."""
+    T, C = 288000, 8192
+    g = torch.Generator(device="cuda").manual_seed(15)
+    u = torch.randn((T, C), generator=g, device="cuda", dtype=torch.bfloat16)
+    w, b = torch.randn((C, 4), generator=g, device="cuda") / 4, torch.randn((C,), generator=g, device="cuda")
+    cu = torch.tensor([0, 1000, 262200, T], dtype=torch.int32, device="cuda")
+    print("conv", T, C, flush=True)
+    (z,), new = ssd.ssd_conv1d_varlen(u, w, b, cu)
+    torch.cuda.synchronize()
+    for at in (131072, 262144, T):
+        lo = at - 64
+        one, state = ssd.ssd_conv1d_prefill(u[None, lo - 3:at].contiguous(), w, b)
+        assert torch.equal(z[lo:at], one[0][0, 3:]), at
+    assert torch.equal(new[2], u[T - 3:].t())
+    assert torch.equal(z[262200:262203], ssd.ssd_conv1d_prefill(u[None, 262200:262203].contiguous(), w, b)[0][0][0])

@@ -262,3 +262,35 @@ def test_both_kernels(ssd, N, io):
             again = run(ssd, s)
             assert torch.equal(again[0][i:-3 * i or None], y[i:-3 * i or None]) and torch.equal(again[1], f)
         ssd.reset_knobs()
+
+
+def test_many_sequences(ssd):
+    """More sequences than channels, many of one token or none."""
+    compare(ssd, make([1, 0, 2, 3, 1] * 300, 40, 16, "f32", seed=100, gaps=(1, 2)), "f32")
+
+
+@pytest.mark.parametrize("kernel", [1, 2])
+def test_offsets_beyond_32_bits(ssd, kernel):
+    """4.4 GiB each of x, dt and y.  States forget within 60 tokens (exp(-60 x 0.5 x 4) is nothing in fp32), so that the oracle may start
+    from zeros 120 tokens in front of what is compared."""
+    T, C, N = 288000, 8192, 16
+    g = torch.Generator(device="cuda").manual_seed(110)
+    x = torch.randn((T, C), generator=g, device="cuda", dtype=torch.bfloat16)
+    dt = torch.rand((T, C), generator=g, device="cuda", dtype=torch.bfloat16) + 0.5
+    bc = torch.randn((T, 2 * N), generator=g, device="cuda", dtype=torch.bfloat16)
+    A, D = -4.0 - torch.rand((C, N), generator=g, device="cuda"), torch.randn((C,), generator=g, device="cuda")
+    cu = torch.tensor([0, 1000, T], dtype=torch.int32, device="cuda")
+    ssd.set_knob("selective_by_state", kernel)
+    print("selective", T, C, N, kernel, flush=True)
+    y, f = ssd.ssd_selective_prefill(x, dt, A, bc[:, :N], bc[:, N:], D, cu)
+    torch.cuda.synchronize()
+    ssd.reset_knobs()
+    for at in (131072 + 8, 262144 + 8, T):
+        rows, cols = slice(at - 140, at), slice(C - 70, C)
+        s = dict(x=x[rows, cols].cpu(), A=A[cols].cpu(), B=bc[rows, :N].cpu(), C=bc[rows, N:].cpu(), D=D[cols].cpu(), z=None, h0=None,
+                 cu=torch.tensor([0, 140], dtype=torch.int32))
+        d = dt[rows, cols].double().cpu().numpy()
+        ref, h_ref = mixer_oracle.selective_scan(s["x"], d, s["A"], s["B"], s["C"], s["D"], s["cu"])
+        ly, lh = limits(s, d, ref, h_ref, "bf16", 140)
+        check(y[at - 20:at, cols], ref[-20:], ly[-20:], "y")
+    check(f[1, cols], h_ref[0], lh[0], "states")

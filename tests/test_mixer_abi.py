@@ -29,7 +29,7 @@ def test_conv_varlen_refuses():
 
     for bad in (dict(batch=0), dict(tokens=0), dict(tokens=(1 << 30) + 1), dict(batch=(1 << 30) + 1), dict(k=1), dict(k=9), dict(split=(0, 8, 8)),
                 dict(split=(8, -1, 8)), dict(us=47), dict(act=2), dict(us=1 << 60), dict(tokens=1 << 30, split=(1 << 20, 0, 0), us=1 << 20),
-                dict(batch=1 << 27)):
+                dict(batch=1 << 26)):
         assert call(**bad) == -2, bad
     assert call(io=2) == -3
     refusals(call, ("split", "cu", "u", "w", "z0", "z1", "z2"), ("w", "bias", "si", "so", "z0", "z1", "z2"), ("u", "cu"))
