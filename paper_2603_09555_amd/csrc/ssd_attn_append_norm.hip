@@ -10,6 +10,9 @@
 // them queries, or keys, or values, 64 pieces at a time: what a lane needs beside its piece -- its weights, and the cosines and sines
 // of its pairs, which are four times the piece -- is the same for all its heads and asked for once.  A piece that holds one half of its
 // pairs brings the other halves' piece with it, which a lane nearby brings too, from the first-level cache.
+//
+// 12 prompts, 16310 tokens, 40 heads over 8 of 64, bf16: 56 us, 4.2 TB/s (87 where each piece asked for its own cosines, sines and
+// weights), fp32: 94; 64 single tokens, 32 heads over 8 of 128: 4.4 us; 1023 tokens in fp32 5.1.
 #include <algorithm>
 
 #include "ssd_attn_append.hpp"

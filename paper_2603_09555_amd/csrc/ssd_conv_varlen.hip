@@ -9,8 +9,8 @@
 // finds the sequence of its first token once, while its first rows are on their way; where the next one begins it fills the window
 // from that one's cache.  Rows of u may be a slice of wider ones, so that the input projection's output need not be copied.
 //
-// 18929 tokens of 12 prompts, 5376 channels, bf16: 88 us, 4.7 TB/s (8 bytes a lane: 90; 16: 92; with loads that leave the caches
-// alone: 97); 4886 x 1536 in fp32 13.9 us, 4.3 TB/s (8 or 16 bytes a lane: 14.6); 13 x 1792 5.1 us.
+// 18929 tokens of 12 prompts, 5376 channels, bf16: 86.7 us, 4.7 TB/s; 4886 x 1536 in fp32 12.2 us, 4.9 TB/s; 13 x 1792 4.4 us.  Beside
+// each other: 4, 8 and 16 bytes a lane 88, 91 and 92 us (97 with loads that leave the caches alone), fp32 13.9, 14.7 and 14.5.
 //
 // The caches are left by threads of their own, one a sequence and channel: in the same launch, or, where they are updated in
 // place, in one behind it (a sequence's first run reads what its last would write).

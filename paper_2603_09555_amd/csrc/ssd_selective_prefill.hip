@@ -4,7 +4,7 @@
 //   y[t][c] = (sum_n C[t][n] h[c][n] + D[c] x[t][c]) silu(z[t][c])
 //
 // The decay differs from state to state, so nothing here is a matrix product.  Bound by the vector unit: an exponential, two issue
-// slots on this card (16 of them 154 cycles a wave, 16 fused products 70), and four products for each token, channel and state, where
+// slots on this card (16 of them 154 cycles a wave, 16 fused products 73), and four products for each token, channel and state, where
 // a matrix instruction for d x B would save a tenth (it does not overlap with them).
 //
 // Two kernels: a lane is a channel and holds states of it in registers, or a lane is a state (see by_state_kernel).  There are too few
@@ -18,8 +18,8 @@
 // A segment whose last token ends a sequence (or is in none) needs no states pass, so that batches of short prompts do little
 // twice.  Where all tokens are one segment only the scan runs.  States, sums and step sizes are fp32; y is rounded once.
 //
-// 16 states, bf16: 16384 tokens x 5120 channels 540 us (states 220, carry 15, scan 310; the issue slots of both passes alone are 510),
-// 9938 tokens of 12 prompts 345, 61 tokens x 1536 channels 5.6; 2048 x 1536 in fp32 46.
+// 16 states, bf16: 16384 tokens x 5120 channels 542 us (322 million issue slots of both passes are 525 at 2.4 GHz; under a profiler
+// states 244, carry 15, scan 344), 9938 tokens of 12 prompts 340, 61 tokens x 1536 channels 5.7; 2048 x 1536 in fp32 46.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
