@@ -366,7 +366,7 @@ SSD_API ssd_status ssd_conv1d_varlen(int32_t batch, int32_t tokens, int32_t ksiz
  *   dt                (tokens, channels) of dt_dtype (SSD_F32, or io_dtype), dense; the map
  *                     of dt_transform is applied as for ssd_prefill_dt (dt_bias is
  *                     (channels)); dt_transform may be NULL: dt is the step size, >= 0
- *   A                 (channels, dstate) fp32, <= 0
+ *   A                 (channels, dstate) fp32, <= 0; -inf: the state keeps nothing of before
  *   B, C              (tokens, dstate) io dtype, rows B_stride, C_stride >= dstate elements
  *                     apart (slices of one projection's output), aligned to their elements
  *   D                 (channels) fp32, or NULL = zeros

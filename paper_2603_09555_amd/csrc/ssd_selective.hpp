@@ -23,6 +23,12 @@ struct SelectiveArgs {
 
 constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e)); }
+// A state's decay in powers of two a unit of step size.  -inf, a state that keeps nothing, becomes the lowest finite value: it decays to
+// nothing just so, and steps of zero, as the by-state kernel takes behind a sequence's end, do not make it NaN.  A NaN stays one.
+__device__ __forceinline__ float decay_rate(float A) {
+  const float rate = A * kLog2e;
+  return rate < -3.4028235e38f ? -3.4028235e38f : rate;
+}
 // softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|), in 18 issue slots of the vector unit, within 4 2^-24 of itself down to
 // v = -80.  What rounding the exponent p = -|v| log2(e) takes away comes back as a factor of e, and what rounding 1 + e does, which is
 // most of a small e, as the first term of the logarithm's series (1 / (1 + e) within 0.09 there, of something below 2^-24).

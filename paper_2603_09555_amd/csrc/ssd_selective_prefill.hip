@@ -159,9 +159,9 @@ constexpr int waves_a_simd(int states) { return states <= 16 ? 4 : 2; }
 // kIo, kDt, kBc: bf16 (x, z, y; dt; rows of B and C).  NS states a wave, W waves for a channel's states.  kStates: the states
 // pass.
 //
-// Tokens are taken in blocks of eight or sixteen.  B and C are the same for all of a wave's lanes and come through the scalar unit.  A wave turns the rows of its share of a block's tokens into step sizes and inflows, which
-// go to all waves through LDS, and into skip terms and gates, which it keeps; then it asks for its rows of the next block.  The
-// waves walk the block's tokens one by one, each on its states, with the next token's step, inflow, B and C on their way, and
+// Tokens are taken in blocks of eight or sixteen.  B and C are the same for all of a wave's lanes and come through the scalar unit.
+// A wave turns the rows of its share of a block's tokens into step sizes and inflows, which go to all waves through LDS, and into skip
+// terms and gates, which it keeps; then it asks for its rows of the next block.  The waves walk the block's tokens one by one, each on its states, with the next token's step, inflow, B and C on their way, and
 // leave the parts of the outputs' sums in LDS, which the wave that prepared a token adds up.
 template <bool kIo, bool kDt, bool kBc, int NS, int W, bool kStates>
 __global__ __launch_bounds__(64 * W, kStates ? 1 : waves_a_simd(NS)) void by_channel_kernel(const ScanArgs a) {
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(64 * W, kStates ? 1 : waves_a_simd(NS)) void by_cha
 #pragma unroll
   for (int n = 0; n < NS; ++n) A2[n] = a.a.A[static_cast<int64_t>(c) * N + min(n0 + n, N - 1)];
 #pragma unroll
-  for (int n = 0; n < NS; ++n) A2[n] = n0 + n < N ? A2[n] * kLog2e : 0.f;
+  for (int n = 0; n < NS; ++n) A2[n] = n0 + n < N ? decay_rate(A2[n]) : 0.f;
   const float bias = a.d.dtx.bias ? a.d.dtx.bias[c] : 0.f, skip = !kStates && a.a.D ? a.a.D[c] : 0.f;
   const bool gated = !kStates && a.a.z != nullptr, softplus_alone = a.d.dtx.softplus && !(a.d.dtx.hi > 0.f);
   float total = 0.f;  // of the step sizes
@@ -339,7 +339,7 @@ __global__ __launch_bounds__(256) void by_state_kernel(const ScanArgs a) {
 #pragma unroll
   for (int k = 0; k < S; ++k) A2[k] = a.a.A[static_cast<int64_t>(c) * N + min(16 * k + nl, N - 1)];
 #pragma unroll
-  for (int k = 0; k < S; ++k) A2[k] = 16 * k + nl < N ? A2[k] * kLog2e : 0.f;
+  for (int k = 0; k < S; ++k) A2[k] = 16 * k + nl < N ? decay_rate(A2[k]) : 0.f;
   const float bias = a.d.dtx.bias ? a.d.dtx.bias[c] : 0.f, skip = !kStates && a.a.D ? a.a.D[c] : 0.f;
   const bool gated = !kStates && a.a.z != nullptr;
   float total = 0.f;  // of the step sizes, this lane's
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(256) void carry_kernel(float *entering, const float
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, size = static_cast<int64_t>(N) * C;
   if (i >= size) return;
   const int c = static_cast<int>(by_state ? i / N : i % C), n = static_cast<int>(by_state ? i % N : i / C);
-  const float A2 = A[static_cast<int64_t>(c) * N + n] * kLog2e;
+  const float A2 = decay_rate(A[static_cast<int64_t>(c) * N + n]);
   constexpr int kAhead = 8;
   float h = 0.f, sum[kAhead], e[kAhead];
   auto request = [&](int s0) {

@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void selective_step_kernel(const StepArgs a) {
   }
   const float bias = a.d.dtx.bias ? a.d.dtx.bias[c] : 0.f, skip = a.a.D ? a.a.D[c] : 0.f;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) A2[k] *= kLog2e;
+  for (int k = 0; k < 4; ++k) A2[k] = decay_rate(A2[k]);
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const float d = step_of(dt[r], bias, a.d.dtx), u = d * x[r];

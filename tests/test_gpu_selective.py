@@ -294,3 +294,37 @@ def test_offsets_beyond_32_bits(ssd, kernel):
         ly, lh = limits(s, d, ref, h_ref, "bf16", 140)
         check(y[at - 20:at, cols], ref[-20:], ly[-20:], "y")
     check(f[1, cols], h_ref[0], lh[0], "states")
+
+
+@pytest.mark.parametrize("by", [1, 2], ids=["by state", "by channel"])
+@pytest.mark.parametrize("N", [5, 16, 40])
+def test_states_that_keep_nothing(ssd, N, by):
+    """A of -inf: exp(d A) is 0, and such a state is its last inflow, d x B; sequences end anywhere in a block of tokens, and segments
+    in sequences.  The oracle multiplies 0 by what was there, so that its A of -1e30 says the same."""
+    lengths = [1, 7, 0, 16, 90, 35]
+    s = make(lengths, 70, N, "f32", seed=7)
+    s["A"][::2, ::3] = float("-inf")
+    ref = dict(s, A=torch.where(torch.isinf(s["A"]), torch.tensor(-1e30), s["A"]))
+    d = ssd_oracle.dt_transform(s["dt"], s["dt_bias"], True, None)
+    y_ref, h_ref = mixer_oracle.selective_scan(s["x"], d, ref["A"], s["B"], s["C"], s["D"], s["cu"], s["z"], s["h0"], y=np.full(s["x"].shape, 7.0))
+    ly, lh = limits(ref, d, y_ref, h_ref, "f32", max(lengths))
+    try:
+        for segment in (0, 32):
+            ssd.set_knob("selective_by_state", by)
+            ssd.set_knob("selective_segment", segment)
+            y, f = run(ssd, s)
+            check(y, y_ref, ly, "y")
+            check(f, h_ref, lh, "states")
+    finally:
+        ssd.reset_knobs()
+    # single tokens of as many sequences
+    batch = len(lengths)
+    t1 = dict(ref, cu=torch.arange(batch + 1, dtype=torch.int32), **{k: s[k][:batch] for k in ("x", "dt", "B", "C", "z")})
+    d = ssd_oracle.dt_transform(t1["dt"], s["dt_bias"], True, None)
+    y_ref, h_ref = mixer_oracle.selective_scan(t1["x"], d, ref["A"], t1["B"], t1["C"], s["D"], t1["cu"], t1["z"], s["h0"])
+    ly, lh = limits(t1, d, y_ref, h_ref, "f32", 1)
+    state, g = s["h0"].cuda(), {k: to_gpu(s[k])[:batch] for k in ("x", "dt", "B", "C", "z")}
+    y = ssd.ssd_selective_step(state, g["x"], g["dt"], s["A"].cuda(), g["B"], g["C"], s["D"].cuda(), z=g["z"], dt_bias=s["dt_bias"].cuda(),
+                               dt_softplus=True)
+    check(y, y_ref, ly, "y of a token")
+    check(state, h_ref, lh, "states of a token")
