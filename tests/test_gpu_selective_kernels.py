@@ -1,0 +1,51 @@
+"""Both kernels of the selective scan, a lane a state (1) and a lane a channel (2), on what test_gpu_selective.py asks of the one
+that the library takes: calls of so little work all go to the first.  Limits are derived there."""
+import pytest
+import torch
+
+from test_gpu_selective import compare, make, to_gpu
+
+pytestmark = pytest.mark.gpu
+BY_STATE, BY_CHANNEL = 1, 2
+
+
+class Forced:
+    """The binding, with one of the kernels wherever it can run: also where a test takes the library's choices back."""
+
+    def __init__(self, binding, kernel):
+        self._binding, self._kernel = binding, kernel
+        self.reset_knobs()
+
+    def __getattr__(self, name):
+        return getattr(self._binding, name)
+
+    def reset_knobs(self):
+        self._binding.reset_knobs()
+        self._binding.set_knob("selective_by_state", self._kernel)
+
+
+@pytest.fixture
+def forced():
+    from paper_2603_09555_amd import ssd
+    yield lambda kernel: Forced(ssd, kernel)
+    ssd.reset_knobs()
+
+
+@pytest.mark.parametrize("kernel,C,N", [(BY_STATE, 64, 16), (BY_STATE, 70, 33), (BY_CHANNEL, 64, 16), (BY_CHANNEL, 130, 8), (BY_CHANNEL, 70, 33),
+                                        (BY_CHANNEL, 70, 100), (BY_CHANNEL, 66, 256)])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_final_states_in_place(forced, kernel, C, N, io):
+    """Sequences that begin in one segment and end in another, or in the same one, states updated where they are."""
+    ssd = forced(kernel)
+    s = make([5, 900, 0, 300, 299, 1], C, N, io, seed=40 + N, pad=(2, 4), gaps=(3, 2))
+    d = {k: to_gpu(v) for k, v in s.items()}
+    for segment in (0, 200, 10000):
+        ssd.set_knob("selective_segment", segment)
+        print("in place", kernel, C, N, io, segment, flush=True)
+        y, f = compare(ssd, s, io)
+        for _ in range(2):
+            held, y2 = d["h0"].clone(), torch.full_like(y, 7.0)
+            _, f2 = ssd.ssd_selective_prefill(d["x"], d["dt"], d["A"], d["B"], d["C"], d["D"], d["cu"], z=d["z"], h0=held, final_state=held, y=y2,
+                                              dt_bias=d["dt_bias"], dt_softplus=True)
+            torch.cuda.synchronize()
+            assert f2 is held and torch.equal(f2, f) and torch.equal(y2, y)
