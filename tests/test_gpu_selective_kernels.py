@@ -3,7 +3,8 @@ that the library takes: calls of so little work all go to the first.  Limits are
 import pytest
 import torch
 
-from test_gpu_selective import compare, make, to_gpu
+import test_gpu_selective as library_choice
+from test_gpu_selective import compare, make, run, to_gpu
 
 pytestmark = pytest.mark.gpu
 BY_STATE, BY_CHANNEL = 1, 2
@@ -31,6 +32,31 @@ def forced():
     ssd.reset_knobs()
 
 
+@pytest.mark.parametrize("kernel", [BY_STATE, BY_CHANNEL])
+@pytest.mark.parametrize("name", ["decays_of_every_size", "boundaries_that_no_batch_has", "what_a_sequence_does_not_hold_is_not_used", "plain_steps",
+                                  "captured_and_on_other_streams", "many_sequences"])
+def test_either_kernel(forced, name, kernel):
+    print(name, kernel, flush=True)
+    getattr(library_choice, "test_" + name)(forced(kernel))
+
+
+@pytest.mark.parametrize("io,dt", [("f32", "same"), ("bf16", "same"), ("bf16", "f32")])
+@pytest.mark.parametrize("C,N", [(64, 16), (1, 1), (65, 7), (130, 8), (63, 13), (7, 24), (96, 32), (40, 33), (64, 64)])
+def test_prompts_by_channel(forced, C, N, io, dt):
+    library_choice.test_prompts(forced(BY_CHANNEL), C, N, io, dt)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("aligned", [True, False])
+def test_long_prompts_by_channel(forced, io, aligned):
+    library_choice.test_long_prompts_of_few_channels(forced(BY_CHANNEL), io, aligned)
+
+
+@pytest.mark.parametrize("C,N", [(4000, 8), (4000, 16), (1000, 16), (900, 6), (700, 32), (400, 64)])
+def test_every_cut_by_channel(forced, C, N):
+    library_choice.test_every_cut(forced(BY_CHANNEL), C, N)
+
+
 @pytest.mark.parametrize("kernel,C,N", [(BY_STATE, 64, 16), (BY_STATE, 70, 33), (BY_CHANNEL, 64, 16), (BY_CHANNEL, 130, 8), (BY_CHANNEL, 70, 33),
                                         (BY_CHANNEL, 70, 100), (BY_CHANNEL, 66, 256)])
 @pytest.mark.parametrize("io", ["f32", "bf16"])
@@ -49,3 +75,20 @@ def test_final_states_in_place(forced, kernel, C, N, io):
                                               dt_bias=d["dt_bias"], dt_softplus=True)
             torch.cuda.synchronize()
             assert f2 is held and torch.equal(f2, f) and torch.equal(y2, y)
+
+
+@pytest.mark.parametrize("kernel", [BY_STATE, BY_CHANNEL])
+@pytest.mark.parametrize("io,dt", [("f32", "same"), ("bf16", "same"), ("bf16", "f32")])
+@pytest.mark.parametrize("N", [8, 16, 32, 64])
+def test_rows_of_either_alignment(forced, N, io, dt, kernel):
+    """B and C where they can be read as they lie (of even strides and places) and where they cannot, with every part of a call; step
+    sizes clamped and not."""
+    ssd = forced(kernel)
+    for i, lengths in enumerate(([300, 0, 1, 90], [17, 700])):
+        for pad in ((2, 4), (1, 2)):
+            s = make(lengths, 130, N, io, dt, seed=120 + i, gaps=(i, 3 * i), pad=pad)
+            for limit in (None, (1e-3, 0.05)):
+                print("selective", N, io, dt, lengths, pad, limit, kernel, flush=True)
+                y, f = compare(ssd, s, io, limit)
+                again = run(ssd, s, limit)
+                assert torch.equal(again[0], y) and torch.equal(again[1], f)
