@@ -13,6 +13,15 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu on the GPU box)")
 
 
+@pytest.fixture(autouse=True)
+def library_choices():
+    """A test that fails with knobs set leaves none of them to the next."""
+    yield
+    ssd = sys.modules.get("paper_2603_09555_amd.ssd")
+    if ssd is not None:
+        ssd.reset_knobs()
+
+
 def pytest_collection_modifyitems(config, items):
     # GPU tests are skipped (not failed) where no device exists, so a plain `pytest tests/` works anywhere.
     try:
