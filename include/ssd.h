@@ -367,6 +367,8 @@ SSD_API ssd_status ssd_conv1d_varlen(int32_t batch, int32_t tokens, int32_t ksiz
  *                     of dt_transform is applied as for ssd_prefill_dt (dt_bias is
  *                     (channels)); dt_transform may be NULL: dt is the step size, >= 0
  *   A                 (channels, dstate) fp32, <= 0; -inf: the state keeps nothing of before
+ *                     at a step of 2^-120 or more, and may keep part of it at a smaller one.
+ *                     A step of zero leaves every state as it is, these too
  *   B, C              (tokens, dstate) io dtype, rows B_stride, C_stride >= dstate elements
  *                     apart (slices of one projection's output), aligned to their elements
  *   D                 (channels) fp32, or NULL = zeros

@@ -23,8 +23,10 @@ struct SelectiveArgs {
 
 constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e)); }
-// A state's decay in powers of two a unit of step size.  -inf, a state that keeps nothing, becomes the lowest finite value: it decays to
-// nothing just so, and steps of zero, as the by-state kernel takes behind a sequence's end, do not make it NaN.  A NaN stays one.
+// A state's decay in powers of two a unit of step size.  -inf, a state that keeps nothing, becomes the lowest finite value, which says
+// the same of steps from 2^-120 on (2^(-2^8) is nothing in fp32).  A step of zero then leaves such a state as it is, like all others,
+// where 0 x -inf would make it NaN: that is what steps driven to zero mean, and what the by-state kernel takes behind a sequence's end.
+// A NaN stays one.
 __device__ __forceinline__ float decay_rate(float A) {
   const float rate = A * kLog2e;
   return rate < -3.4028235e38f ? -3.4028235e38f : rate;

@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import test_gpu_selective as library_choice
-from test_gpu_selective import compare, make, run, to_gpu
+from oracle import mixer_oracle
+from test_gpu_selective import check, compare, limits, make, run, to_gpu
 
 pytestmark = pytest.mark.gpu
 BY_STATE, BY_CHANNEL = 1, 2
@@ -92,3 +93,57 @@ def test_rows_of_either_alignment(forced, N, io, dt, kernel):
                 y, f = compare(ssd, s, io, limit)
                 again = run(ssd, s, limit)
                 assert torch.equal(again[0], y) and torch.equal(again[1], f)
+
+
+@pytest.mark.parametrize("kernel,N", [(BY_STATE, 5), (BY_STATE, 16), (BY_STATE, 40), (BY_CHANNEL, 5), (BY_CHANNEL, 16), (BY_CHANNEL, 40), (BY_CHANNEL, 100)])
+def test_steps_of_zero_keep_all_states(forced, kernel, N):
+    """A of -inf leaves nothing of a state at any step from 2^-120 on, and all of it at a step of zero: single ones, and so many that
+    they fill segments.  The oracle's A of -1e300 says both (its products are in fp64)."""
+    ssd = forced(kernel)
+    lengths = [7, 150, 0, 40]
+    s = make(lengths, 70, N, "f32", seed=130 + N)
+    small = 2.0 ** -120
+    s["dt"], s["dt_bias"] = s["dt"].abs(), None
+    s["dt"][2:4] = s["dt"][20:125] = s["dt"][-3:] = 0.0
+    s["dt"][130:150:3] = small
+    s["x"][130:150:3] *= 2.0 ** 40      # (inflows that fp32 holds as normal values)
+    s["A"][::2, ::3] = float("-inf")
+    ref = dict(s, A=torch.where(torch.isinf(s["A"]), -1e300, s["A"].double()))
+    d = s["dt"].double().numpy()
+    y_ref, h_ref = mixer_oracle.selective_scan(s["x"], d, ref["A"], s["B"], s["C"], s["D"], s["cu"], s["z"], s["h0"])
+    ly, lh = limits(ref, d, y_ref, h_ref, "f32", max(lengths))
+    g = {k: to_gpu(v) for k, v in s.items()}
+    for segment in (0, 32):
+        ssd.set_knob("selective_segment", segment)
+        print("steps of zero", kernel, N, segment, flush=True)
+        y, f = ssd.ssd_selective_prefill(g["x"], g["dt"], g["A"], g["B"], g["C"], g["D"], g["cu"], z=g["z"], h0=g["h0"])
+        torch.cuda.synchronize()
+        check(y, y_ref, ly, "y")
+        check(f, h_ref, lh, "states")
+    # nothing but steps of zero: the states come through as they are
+    y, f = ssd.ssd_selective_prefill(g["x"], torch.zeros_like(g["dt"]), g["A"], g["B"], g["C"], g["D"], g["cu"], z=g["z"], h0=g["h0"])
+    torch.cuda.synchronize()
+    assert torch.equal(f, g["h0"])
+
+
+@pytest.mark.parametrize("N", [5, 16, 40])
+def test_single_steps_of_zero_keep_all_states(forced, N):
+    ssd = forced(BY_STATE)
+    s = make([1] * 6, 70, N, "f32", seed=140 + N)
+    s["dt"] = s["dt"].abs()
+    s["dt"][1] = s["dt"][4] = 0.0
+    s["dt"][2] = 2.0 ** -120
+    s["x"][2] *= 2.0 ** 40
+    s["A"][::2, ::3] = float("-inf")
+    ref = dict(s, A=torch.where(torch.isinf(s["A"]), -1e300, s["A"].double()))
+    d = s["dt"].double().numpy()
+    y_ref, h_ref = mixer_oracle.selective_scan(s["x"], d, ref["A"], s["B"], s["C"], s["D"], s["cu"], s["z"], s["h0"])
+    ly, lh = limits(ref, d, y_ref, h_ref, "f32", 1)
+    g = {k: to_gpu(v) for k, v in s.items()}
+    state = g["h0"].clone()
+    print("single steps of zero", N, flush=True)
+    y = ssd.ssd_selective_step(state, g["x"], g["dt"], g["A"], g["B"], g["C"], g["D"], z=g["z"])
+    torch.cuda.synchronize()
+    check(y, y_ref, ly, "y")
+    check(state, h_ref, lh, "states")
+    assert torch.equal(state[1], g["h0"][1]) and torch.equal(state[4], g["h0"][4])
