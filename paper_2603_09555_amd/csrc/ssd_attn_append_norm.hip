@@ -12,7 +12,8 @@
 // pairs brings the other halves' piece with it, which a lane nearby brings too, from the first-level cache.
 //
 // 12 prompts, 16310 tokens, 40 heads over 8 of 64, bf16: 56 us, 4.2 TB/s (87 where each piece asked for its own cosines, sines and
-// weights), fp32: 94; 64 single tokens, 32 heads over 8 of 128: 4.4 us; 1023 tokens in fp32 5.1.
+// weights), fp32: 94; 64 single tokens, 32 heads over 8 of 128: 4.4 us; 1023 tokens in fp32 5.1.  Heads of 80, bf16: 85 us with 32 or 80
+// values rotated, 292 with 40: rotated halves whose pieces hold values of both are joined value by value, four loads each.
 #include <algorithm>
 
 #include "ssd_attn_append.hpp"

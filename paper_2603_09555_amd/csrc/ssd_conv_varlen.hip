@@ -13,7 +13,8 @@
 // each other: 4, 8 and 16 bytes a lane 88, 91 and 92 us (97 with loads that leave the caches alone), fp32 13.9, 14.7 and 14.5.
 //
 // The caches are left by threads of their own, one a sequence and channel: in the same launch, or, where they are updated in
-// place, in one behind it (a sequence's first run reads what its last would write).
+// place, in one behind it (a sequence's first run reads what its last would write), which takes 3.3 us: 13 x 1792 7.4 us in place and
+// 4.1 out of place, 18929 x 5376 89.8 and 86.5.
 #include <algorithm>
 
 #include "ssd_conv.hpp"

@@ -19,7 +19,10 @@
 // twice.  Where all tokens are one segment only the scan runs.  States, sums and step sizes are fp32; y is rounded once.
 //
 // 16 states, bf16: 16384 tokens x 5120 channels 542 us (322 million issue slots of both passes are 525 at 2.4 GHz; under a profiler
-// states 244, carry 15, scan 344), 9938 tokens of 12 prompts 340, 61 tokens x 1536 channels 5.7; 2048 x 1536 in fp32 46.
+// states 244, carry 15, scan 344), 9938 tokens of 12 prompts 340, 61 tokens x 1536 channels 5.7.  States updated in place: the same.
+// fp32, 16384 x 5120: 656; 360 million slots, 585 us: the compiler copies B and C, read for the next token, into vector registers, one or
+// two moves a state.  fp32, 2048 x 1536: 46, of which the slots, 17 million, are 28; three launches and trips to memory that some four
+// waves a SIMD do not hide are the rest.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -161,8 +164,9 @@ constexpr int waves_a_simd(int states) { return states <= 16 ? 4 : 2; }
 //
 // Tokens are taken in blocks of eight or sixteen.  B and C are the same for all of a wave's lanes and come through the scalar unit.
 // A wave turns the rows of its share of a block's tokens into step sizes and inflows, which go to all waves through LDS, and into skip
-// terms and gates, which it keeps; then it asks for its rows of the next block.  The waves walk the block's tokens one by one, each on its states, with the next token's step, inflow, B and C on their way, and
-// leave the parts of the outputs' sums in LDS, which the wave that prepared a token adds up.
+// terms and gates, which it keeps; then it asks for its rows of the next block.  The waves walk the block's tokens one by one, each on
+// its states, with the next token's step, inflow, B and C on their way, and leave the parts of the outputs' sums in LDS, which the wave
+// that prepared a token adds up.
 template <bool kIo, bool kDt, bool kBc, int NS, int W, bool kStates>
 __global__ __launch_bounds__(64 * W, kStates ? 1 : waves_a_simd(NS)) void by_channel_kernel(const ScanArgs a) {
   constexpr int kBlock = block_of(W), kOwn = kBlock / W;  // tokens of a block; those that a wave prepares and finishes
@@ -543,7 +547,9 @@ Cut cut_by_state(const SelectiveDims &d) {
   return c;
 }
 // A lane a state up to 2^26 states of all tokens: 16 states, us by state and by channel, 1536 channels, 61 tokens 5.6 / 21, 512 19 / 35,
-// 2048 (fp32) 46 / 52; 5120 channels, 512 tokens 36 / 43, 2048 116 / 103.  64 states, 1536 channels, 1024 tokens 58 / 64.
+// 2048 (fp32) 46 / 52; 5120 channels, 512 tokens 36 / 43, 2048 116 / 103.  At 2^26, bf16: 16 states, 256 to 8192 channels 60 / 87, 61 / 70,
+// 63 / 64, 62 / 63, 37 / 53; 32 states 49 / 52, 64 states 40 / 56.  At 2^27 by state takes 0.88 to 1.3 of by channel.  8 states leave half
+// of a row's lanes without one: 1536 channels, 2730 tokens (2^25) 62 / 54, 5461 tokens (2^26) 111 / 70.
 constexpr int kMostByState = 64;  // states of a channel
 Cut cut_of(const SelectiveDims &d) {
   const int64_t work = static_cast<int64_t>(d.T) * d.C * d.N;

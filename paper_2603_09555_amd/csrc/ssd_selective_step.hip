@@ -7,7 +7,9 @@
 // lanes the channel's others: sums over them stay within 4 lanes for 16 states, within 64 for 256.  Where there are many
 // sequences a lane takes those states of two of them, which are on their way together, and reads the decays once.
 //
-// 256 sequences x 5120 channels x 16 states, bf16: 35 us, 5.1 TB/s (44 with one sequence a lane); one sequence 4.3 us, the launch.
+// 256 sequences x 5120 channels x 16 states, bf16 or fp32: 36 us, 4.9 TB/s, where eight batches take turns, so that states come from
+// memory; 30 where one batch's do, of which the last-level cache holds what it can.  (Inputs in turn, between the two: 35, and 44 with
+// one sequence a lane.)  One sequence 4.3 us, the launch.
 #include "ssd_selective.hpp"
 
 namespace ssd {
